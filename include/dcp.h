@@ -392,13 +392,102 @@ dcp_status_t dcp_comm_volume(const int32_t* cu_seqlens_host, int32_t n_seq, int3
                              int64_t kv_bytes_per_token, int64_t o_bytes_per_token, int64_t* pairwise,
                              int64_t* connectivity, int64_t* n_hyperedges, int64_t* send, int64_t* recv);
 
+/* ---------------------------------------------------------------------------------------------
+ * Paged key-value cache and the attention of one new token over it (serving).  A page is a slot of a block buffer (see
+ * dcp_plan_set_block_buffers): with k_stride_p = page_size * k_stride_t a layer of the cache is the KV-type buffer of a plan with
+ * block_size = page_size and kv_slot = page number, so dcp_block_attn_fwd reads a prompt from the pages that the calls below filled.
+ * Everything lies in device memory and every call only enqueues kernels on `stream`: no allocation, no copy to the host, no
+ * wait; a decoding step (reserve, and append and attention for every layer) may be recorded into a HIP graph and replayed.
+ *   k, v        [n_layers, n_pages, page_size, hkv, d] with element strides (any order; multiples of 8, d contiguous)
+ *   page_ref    int32 [n_pages]: how many sequences hold the page (0: free)
+ *   page_table  int32 [n_seqs, max_pages] contiguous: page of the tokens [p * page_size, (p + 1) * page_size) of a sequence
+ *   seq_len     int32 [n_seqs]: tokens of a sequence; it holds the first ceil(seq_len / page_size) entries of its row
+ * An empty cache has page_ref and seq_len all 0.  A page that is partly filled is held by one sequence alone.
+ *
+ * `seqs` (int32 [n], device) names the sequence of each place of a batch, or is NULL: place i is sequence i (n <= n_seqs).  A
+ * place with a negative number is padding: nothing is read or written for it.  A number >= n_seqs is no sequence: the place
+ * gets DCP_PLACE_BAD where the call has a status array and is padding elsewhere.  Page numbers outside [0, n_pages) and lengths outside
+ * [0, max_pages * page_size] are never followed: such a page holds nothing, such a length is cut.
+ * `status` (int32 [n], device) receives DCP_PLACE_*; a place that is not OK leaves its sequence and every page as they were.
+ * At most DCP_CACHE_MAX_SEQS sequences in a cache and places in a call; n == 0 is legal.  Calls that change one cache, and
+ * those that read it meanwhile, must be ordered (one stream, or events).  Errors of the host's checks as elsewhere. */
+#define DCP_CACHE_MAX_SEQS 16384
+typedef enum {
+  DCP_PLACE_OK = 0,    /* done, or padding                                                                   */
+  DCP_PLACE_FULL = 1,  /* not enough free pages                                                              */
+  DCP_PLACE_BAD = 2    /* no such sequence, one that an earlier place of the call names, or that has no room */
+                       /* left in its row of the table; dcp_cache_fork: see there                            */
+} dcp_place_t;
+typedef struct {
+  int32_t n_layers, n_pages, page_size, hkv, d;
+  int32_t dtype;              /* dcp_dtype_t of k and v */
+  int32_t n_seqs, max_pages;
+  void* k; int64_t k_stride_l, k_stride_p, k_stride_t, k_stride_h;
+  void* v; int64_t v_stride_l, v_stride_p, v_stride_t, v_stride_h;
+  int32_t* page_ref;
+  int32_t* page_table;
+  int32_t* seq_len;
+} dcp_cache_t;
+
+/* Room for n_new[i] >= 0 more tokens (NULL: one each) of every place's sequence: seq_len advances and the pages that the new
+ * tokens reach are taken, the lowest free ones first, in the order of the places.  Places are served in order until one finds too few
+ * pages left: it and the later places that need any are FULL.  Once per step, for all layers. */
+dcp_status_t dcp_cache_reserve(const dcp_cache_t* cache, const int32_t* seqs, const int32_t* n_new, int32_t n,
+                               int32_t* status, void* stream);
+
+/* Writes the keys and values of the tokens that dcp_cache_reserve made room for into the pages of one layer: place i has
+ * the tokens [cu_new[i], cu_new[i + 1]) of k_new and v_new (cu_new NULL: token i alone), the last ones of its sequence.
+ *   cu_new  int32 [n + 1], device, ascending; tokens that it leaves out or that are not below n_tokens are not read
+ *   status  of dcp_cache_reserve (places that are not OK are left out), or NULL
+ *   k_new, v_new  [n_tokens, hkv, d] of the cache's dtype, strides as for k and v of dcp_tensors_t; not part of the cache;
+ *                n_tokens at most 2^26 */
+dcp_status_t dcp_cache_append(const dcp_cache_t* cache, int32_t layer, const int32_t* seqs, const int32_t* cu_new, int32_t n,
+                              const int32_t* status, const void* k_new, int64_t k_stride_t, int64_t k_stride_h,
+                              const void* v_new, int64_t v_stride_t, int64_t v_stride_h, int64_t n_tokens, void* stream);
+
+/* Sequence dst[i], which must be empty, becomes a copy of src[i]: it shares the whole pages (page_ref + 1) and gets a page of its own,
+ * the lowest free one, with the tokens of the page that src[i] is filling, in all layers (the rest of that page stays as it is).  One
+ * source may be forked many times.  src[i] < 0: padding.  BAD: src or dst no sequence, dst not empty or named by an earlier place, src
+ * named as a destination in the same call.  FULL as above.  Two launches. */
+dcp_status_t dcp_cache_fork(const dcp_cache_t* cache, const int32_t* src, const int32_t* dst, int32_t n, int32_t* status,
+                            void* stream);
+
+/* The places' sequences give up their pages (page_ref - 1, the table's entries become -1) and are empty.  One that is named twice is freed once. */
+dcp_status_t dcp_cache_free(const dcp_cache_t* cache, const int32_t* seqs, int32_t n, void* stream);
+
+/* Moves the pages in use to the front: with u pages in use, the k-th page in use at or behind u goes to the k-th free page before u, in
+ * all layers, whole, and page_table and page_ref follow.  counts: int32 [2], device: pages in use, pages moved.  The order of
+ * the free pages, and so the pages that later calls take, is ascending again; n_pages of a smaller cache may be u.
+ *   workspace  device, >= dcp_cache_workspace_bytes, 256-byte aligned.  Two launches. */
+size_t dcp_cache_workspace_bytes(const dcp_cache_t* cache);
+dcp_status_t dcp_cache_compact(const dcp_cache_t* cache, int32_t* counts, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Attention of one new token per place over its sequence: the query is the token at position seq_len - 1 (appended already) and
+ * sees key j iff j < seq_len and, with window > 0, seq_len - 1 - j < window or j < sink (the predicate of WINDOW rows; window 0: no
+ * window).  Keys in pages that do not exist are not seen.  Out and LSE as in dcp_block_attn_fwd: a place that sees no key gets
+ * O = 0, LSE = -inf; padding is not written.  Inf and NaN in q, k and v reach the places that see them and no others.
+ *   q, out  [n, hq, d] of the cache's dtype, strides as in dcp_tensors_t; out must not overlap q;  lse float [hq, n] contiguous
+ *   workspace  device, >= dcp_paged_attn_workspace_bytes, 256-byte aligned; scratch: calls that may run at the same time need one each */
+typedef struct {
+  int32_t n, hq, layer;
+  float softmax_scale;
+  int32_t window, sink;       /* 0 <= window, 0 <= sink */
+  const int32_t* seqs;
+  const void* q; int64_t q_stride_t, q_stride_h;
+  void* out;     int64_t o_stride_t, o_stride_h;
+  float* lse;
+} dcp_paged_attn_t;
+size_t dcp_paged_attn_workspace_bytes(const dcp_cache_t* cache, int32_t n, int32_t hq);
+dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t* args, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Per-kernel timing for benchmarks.  While enabled, every kernel the library launches is
  * bracketed by hipEvents recorded on the launch stream (the kernels of one backward call are timed
  * one by one; the one launch that small batches take for dQ and dK/dV together counts as DCP_K_DKV, and
  * DCP_K_DQ has no launch then).  dcp_profile_read synchronises on the recorded events, returns the summed duration
  * and the number of launches of one kernel since the last enable, and leaves the records in place;
  * dcp_profile_enable(1) clears them.  Not thread-safe; meant for a single benchmarking thread. */
-typedef enum { DCP_K_FWD = 0, DCP_K_MERGE = 1, DCP_K_DELTA = 2, DCP_K_DQ = 3, DCP_K_DKV = 4, DCP_K_SUM = 5, DCP_K_COPY = 6 } dcp_kernel_id_t;
+typedef enum { DCP_K_FWD = 0, DCP_K_MERGE = 1, DCP_K_DELTA = 2, DCP_K_DQ = 3, DCP_K_DKV = 4, DCP_K_SUM = 5, DCP_K_COPY = 6,
+               DCP_K_PAGED_ATTN = 7, DCP_K_CACHE = 8 /* a call that changes a cache */ } dcp_kernel_id_t;
 dcp_status_t dcp_profile_enable(int32_t enable);
 dcp_status_t dcp_profile_read(int32_t kernel_id, double* total_ms, int64_t* launches);
 

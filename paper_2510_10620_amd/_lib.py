@@ -46,6 +46,27 @@ class Instr(ctypes.Structure):
     ]
 
 
+class Cache(ctypes.Structure):
+    """dcp_cache_t"""
+    _fields_ = [
+        ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("hkv", ctypes.c_int32),
+        ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("k", vp), ("k_stride_l", ctypes.c_int64), ("k_stride_p", ctypes.c_int64), ("k_stride_t", ctypes.c_int64), ("k_stride_h", ctypes.c_int64),
+        ("v", vp), ("v_stride_l", ctypes.c_int64), ("v_stride_p", ctypes.c_int64), ("v_stride_t", ctypes.c_int64), ("v_stride_h", ctypes.c_int64),
+        ("page_ref", vp), ("page_table", vp), ("seq_len", vp),
+    ]
+
+
+class PagedAttn(ctypes.Structure):
+    """dcp_paged_attn_t"""
+    _fields_ = [
+        ("n", ctypes.c_int32), ("hq", ctypes.c_int32), ("layer", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
+        ("window", ctypes.c_int32), ("sink", ctypes.c_int32), ("seqs", vp),
+        ("q", vp), ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
+        ("out", vp), ("o_stride_t", ctypes.c_int64), ("o_stride_h", ctypes.c_int64), ("lse", vp),
+    ]
+
+
 _SIGS = {
     "dcp_build_block_table": (ctypes.c_int, [i32p, ctypes.c_int32, ctypes.c_int32, i32p, i32p, ctypes.c_int64, i64p]),
     "dcp_count_pairs": (ctypes.c_int, [i32p, ctypes.c_int32, ctypes.c_int32, i32p, ctypes.c_int64, i32p, i64p]),
@@ -78,6 +99,15 @@ _SIGS = {
     "dcp_copy_list_create": (ctypes.c_int, [ctypes.POINTER(vp), i32p, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64]),
     "dcp_copy_list_destroy": (ctypes.c_int, [vp]),
     "dcp_blockwise_copy": (ctypes.c_int, [vp, vp, ctypes.c_int64, vp, ctypes.c_int64, ctypes.c_int64, vp]),
+    "dcp_cache_reserve": (ctypes.c_int, [ctypes.POINTER(Cache), vp, vp, ctypes.c_int32, vp, vp]),
+    "dcp_cache_append": (ctypes.c_int, [ctypes.POINTER(Cache), ctypes.c_int32, vp, vp, ctypes.c_int32, vp, vp, ctypes.c_int64, ctypes.c_int64,
+                                        vp, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, vp]),
+    "dcp_cache_fork": (ctypes.c_int, [ctypes.POINTER(Cache), vp, vp, ctypes.c_int32, vp, vp]),
+    "dcp_cache_free": (ctypes.c_int, [ctypes.POINTER(Cache), vp, ctypes.c_int32, vp]),
+    "dcp_cache_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Cache)]),
+    "dcp_cache_compact": (ctypes.c_int, [ctypes.POINTER(Cache), vp, vp, ctypes.c_size_t, vp]),
+    "dcp_paged_attn_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Cache), ctypes.c_int32, ctypes.c_int32]),
+    "dcp_paged_attn_fwd": (ctypes.c_int, [ctypes.POINTER(Cache), ctypes.POINTER(PagedAttn), vp, ctypes.c_size_t, vp]),
     "dcp_profile_enable": (ctypes.c_int, [ctypes.c_int32]),
     "dcp_profile_read": (ctypes.c_int, [ctypes.c_int32, ctypes.POINTER(ctypes.c_double), i64p]),
     "dcp_last_error": (ctypes.c_char_p, []),

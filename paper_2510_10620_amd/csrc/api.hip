@@ -13,7 +13,7 @@ using namespace dcp;
 namespace dcp {
 struct ProfRec { hipEvent_t a, b; };
 static bool g_prof_on = false;
-static std::vector<ProfRec> g_prof[7];
+static std::vector<ProfRec> g_prof[9];
 ProfScope::ProfScope(int id_, hipStream_t s_, bool enabled) : id(id_), s(s_) {
   if (!g_prof_on || !enabled) return;
   hipEvent_t a = nullptr;
@@ -38,7 +38,7 @@ extern "C" dcp_status_t dcp_profile_enable(int32_t enable) {
 }
 
 extern "C" dcp_status_t dcp_profile_read(int32_t kernel_id, double* total_ms, int64_t* launches) {
-  if (kernel_id < 0 || kernel_id > 6 || !total_ms || !launches) return fail(DCP_ERR_INVALID_ARG, "bad kernel id or NULL output");
+  if (kernel_id < 0 || kernel_id > 8 || !total_ms || !launches) return fail(DCP_ERR_INVALID_ARG, "bad kernel id or NULL output");
   double tot = 0;
   for (auto& r : g_prof[kernel_id]) {
     DCP_HIP_TRY(hipEventSynchronize(r.b));

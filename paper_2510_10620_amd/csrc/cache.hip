@@ -1,0 +1,489 @@
+// The calls that change a paged key-value cache: pages are taken, shared, given back and moved to the front, and new
+// tokens are written into them.  Everything is decided on the device from page_ref, page_table and seq_len, so that a
+// decoding step never waits for the host.
+#include <algorithm>
+
+#include "cache_internal.h"
+
+using namespace dcp;
+
+namespace dcp {
+
+static constexpr int kMapThreads = 1024, kMapWaves = kMapThreads / 64;
+static constexpr int kScan = 8;           // page_ref entries a lane has in flight
+static constexpr int kNoOwner = INT_MAX;
+
+// Inclusive sums over the workgroup, cut at `cap` (cutting is associative for numbers >= 0, and no sum passes 2^31).
+__device__ __forceinline__ int block_sum(int x, int cap, int* wave_sum, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x = min(x + y, cap);
+  }
+  __syncthreads();
+  if (lane == 63) wave_sum[wave] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kMapWaves; w++) {
+    const int v = wave_sum[w];
+    if (w < wave) before = min(before + v, cap);
+    all = min(all + v, cap);
+  }
+  *total = all;
+  return min(before + x, cap);
+}
+
+// What a place of dcp_cache_reserve (dcp_cache_fork) asks for: `need` pages for row `seq` of the table from entry `first` on,
+// after which the sequence has `tokens` tokens.  seq -1: padding, or not OK.
+struct Place {
+  int32_t seq, first, need, tokens, code;
+};
+
+// a: seqs (src); b: n_new (dst).  owner[s]: the first place that changes sequence s.
+template <bool FORK>
+__device__ __forceinline__ Place place_at(const KCache& c, const int32_t* a, const int32_t* b, int i, const int32_t* owner) {
+  Place p{-1, 0, 0, 0, DCP_PLACE_OK};
+  const int s = a ? a[i] : i;
+  if (s < 0) return p;
+  p.code = DCP_PLACE_BAD;
+  if (!c.is_seq(s)) return p;
+  if (FORK) {
+    const int d = b[i];
+    if (!c.is_seq(d) || owner[d] != i || owner[s] != kNoOwner || c.len[d] != 0) return p;
+    p.tokens = c.length(s);
+    p.seq = d;
+    p.first = c.page.quot(p.tokens);
+    p.need = c.page.rem(p.tokens, p.first) != 0;
+  } else {
+    const int more = b ? b[i] : 1, len = c.length(s);
+    if (owner[s] != i || more < 0 || more > c.max_len - len) return p;
+    p.tokens = len + more;
+    p.seq = s;
+    p.first = c.pages_of(len);
+    p.need = c.pages_of(p.tokens) - p.first;
+  }
+  p.code = DCP_PLACE_OK;
+  return p;
+}
+
+// One workgroup: the places' needs are summed up in their order, page_ref is walked once, and the k-th free page goes to the place
+// whose sums k falls between.  That a place finds too few pages is known at the end: the one that got some gives them back.
+// Bound by latency: three dependent trips to memory, then 4 bytes a page.
+template <bool FORK>
+__global__ __launch_bounds__(kMapThreads) void take_kernel(KCache c, const int32_t* __restrict__ a, const int32_t* __restrict__ b,
+                                                           int32_t n, int32_t* __restrict__ status) {
+  __shared__ int32_t owner[DCP_CACHE_MAX_SEQS], sums[DCP_CACHE_MAX_SEQS], wave_sum[kMapWaves], short_place;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int cap = c.n_pages + 1;
+  for (int s = tid; s < c.n_seqs; s += kMapThreads) owner[s] = kNoOwner;
+  if (tid == 0) short_place = -1;
+  __syncthreads();
+  for (int i = tid; i < n; i += kMapThreads) {
+    const int s = a ? a[i] : i;
+    if (!c.is_seq(s)) continue;
+    const int t = FORK ? b[i] : s;
+    if (c.is_seq(t)) atomicMin(&owner[t], i);
+  }
+  __syncthreads();
+  int total = 0;
+  for (int base = 0; base < n; base += kMapThreads) {
+    const int i = base + tid;
+    int all;
+    const int x = block_sum(i < n ? min(place_at<FORK>(c, a, b, i, owner).need, cap) : 0, cap, wave_sum, &all);
+    if (i < n) sums[i] = min(total + x, cap);
+    total = min(total + all, cap);
+  }
+  __syncthreads();
+  int found = 0;
+  for (int64_t base = 0; base < c.n_pages && found < total; base += kMapThreads * kScan) {
+    const int64_t first = base + wave * (64 * kScan) + lane;
+    int32_t held[kScan];
+#pragma unroll
+    for (int u = 0; u < kScan; u++) held[u] = first + u * 64 < c.n_pages ? c.ref[first + u * 64] : 1;
+    uint64_t mask[kScan];
+    int mine = 0;
+#pragma unroll
+    for (int u = 0; u < kScan; u++) {
+      mask[u] = __ballot(held[u] <= 0);
+      mine += __popcll(mask[u]);
+    }
+    int all;
+    // the wave's count enters the sum once
+    int k = found + block_sum(lane == 63 ? mine : 0, INT_MAX / 2, wave_sum, &all) - (lane == 63 ? mine : 0);
+    k = __shfl(k, 63);
+#pragma unroll
+    for (int u = 0; u < kScan; u++) {
+      const int rank = k + __popcll(mask[u] & ((uint64_t(1) << lane) - 1));
+      if (held[u] <= 0 && rank < total) {
+        int lo = 0, hi = n - 1;   // the first place whose sum is above rank
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (sums[mid] > rank) hi = mid;
+          else lo = mid + 1;
+        }
+        const Place p = place_at<FORK>(c, a, b, lo, owner);
+        const int32_t page = (int32_t)(first + u * 64);
+        c.row(p.seq)[p.first + rank - (lo ? sums[lo - 1] : 0)] = page;
+        c.ref[page] = 1;
+      }
+      k += __popcll(mask[u]);
+    }
+    found += all;
+  }
+  __syncthreads();
+  // Lengths change here only.  A place reads the length of its own sequence, and of a source that nobody changes.
+  for (int i = tid; i < n; i += kMapThreads) {
+    Place p = place_at<FORK>(c, a, b, i, owner);
+    if (p.seq >= 0 && p.need > 0 && sums[i] > found) {
+      p.code = DCP_PLACE_FULL;
+      if ((i ? sums[i - 1] : 0) < found) short_place = i;
+    } else if (p.seq >= 0) {
+      c.len[p.seq] = p.tokens;
+    }
+    status[i] = p.code;
+  }
+  __syncthreads();
+  if (short_place >= 0) {
+    const Place p = place_at<FORK>(c, a, b, short_place, owner);
+    const int got = found - (short_place ? sums[short_place - 1] : 0);
+    for (int k = tid; k < got; k += kMapThreads) {
+      int32_t* entry = c.row(p.seq) + p.first + k;
+      c.ref[*entry] = 0;
+      *entry = -1;
+    }
+  }
+}
+
+// 16 bytes past the caches: pages are read and written once here.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x4 load16(const char* p) { return __builtin_nontemporal_load((const u32x4*)p); }
+__device__ __forceinline__ void store16(char* p, u32x4 v) { __builtin_nontemporal_store(v, (u32x4*)p); }
+
+// Tokens [t0, t1) of page `from` to page `to` of one layer of k or v, by one workgroup of 256.
+__device__ __forceinline__ void copy_tokens(const KCache& c, char* base, int64_t st_p, int64_t st_t, int64_t st_h, int from, int to, int t0, int t1) {
+  const char* src = base + from * st_p;
+  char* dst = base + to * st_p;
+  const int per_token = c.hkv * c.head_chunks, n = (t1 - t0) * per_token;
+  for (int x = threadIdx.x; x < n; x += 256) {
+    const int row = x / c.head_chunks, off = x - row * c.head_chunks;   // row: (token, head)
+    const int t = c.heads.quot(row), h = c.heads.rem(row, t);
+    const int64_t at = (t0 + t) * st_t + h * st_h + off * 16;
+    store16(dst + at, load16(src + at));
+  }
+}
+
+// After take_kernel: workgroup (i, 0) shares the whole pages of place i, (i, 1 + 2 layer + (0: k, 1: v)) copies the page being filled.
+__global__ __launch_bounds__(256) void fork_kernel(KCache c, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+                                                   const int32_t* __restrict__ status) {
+  const int i = blockIdx.x;
+  const int a = src[i];
+  if (a < 0 || status[i] != DCP_PLACE_OK) return;
+  const int b = dst[i], len = c.length(a), whole = c.page.quot(len);
+  const int32_t* from = c.row(a);
+  int32_t* to = c.row(b);
+  if (blockIdx.y == 0) {
+    for (int p = threadIdx.x; p < whole; p += 256) {
+      const int32_t page = from[p];
+      to[p] = page;
+      if (c.is_page(page)) atomicAdd(&c.ref[page], 1);
+    }
+    return;
+  }
+  const int filled = c.page.rem(len, whole);
+  if (!filled) return;
+  const int32_t page = from[whole], mine = to[whole];
+  if (!c.is_page(page) || !c.is_page(mine)) return;
+  const int layer = (blockIdx.y - 1) >> 1;
+  if (blockIdx.y & 1) copy_tokens(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, page, mine, 0, filled);
+  else copy_tokens(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, page, mine, 0, filled);
+}
+
+// One workgroup a place.  The length is taken by an exchange, so that a sequence that is named twice is freed once.
+__global__ __launch_bounds__(256) void free_kernel(KCache c, const int32_t* __restrict__ seqs) {
+  __shared__ int32_t taken;
+  const int s = seqs ? seqs[blockIdx.x] : (int)blockIdx.x;
+  if (!c.is_seq(s)) return;
+  if (threadIdx.x == 0) taken = atomicExch(&c.len[s], 0);
+  __syncthreads();
+  const int held = c.pages_of(max(0, min(taken, c.max_len)));
+  int32_t* row = c.row(s);
+  for (int p = threadIdx.x; p < held; p += 256) {
+    const int32_t page = row[p];
+    row[p] = -1;
+    if (c.is_page(page)) atomicSub(&c.ref[page], 1);
+  }
+}
+
+// What the two launches of dcp_cache_compact share: the pages that move, and where every page goes.
+struct Moves {
+  int32_t *count, *from, *to, *where;   // [1], [n_pages / 2 + 1], [n_pages / 2 + 1], [n_pages]: of the pages behind those in use, -1: free
+};
+
+// One workgroup: counts the pages in use (u), then lists the free ones before u and the used ones behind it, which are as many.
+__global__ __launch_bounds__(kMapThreads) void list_moves_kernel(KCache c, Moves m, int32_t* __restrict__ counts) {
+  __shared__ int32_t wave_sum[kMapWaves];
+  const int tid = threadIdx.x;
+  int used = 0;
+  for (int64_t p = tid; p < c.n_pages; p += kMapThreads) used += c.ref[p] > 0;
+  int total;
+  block_sum(used, INT_MAX / 2, wave_sum, &total);
+  const int n_used = total;
+  int holes = 0, high = 0;
+  for (int64_t base = 0; base < c.n_pages; base += kMapThreads) {
+    const int64_t p = base + tid;
+    const bool held = p < c.n_pages && c.ref[p] > 0;
+    const bool front = p < n_used, listed = p < c.n_pages && (front ? !held : held);
+    int all_h, all_u;
+    const int h = block_sum(listed && front, INT_MAX / 2, wave_sum, &all_h);
+    const int u = block_sum(listed && !front, INT_MAX / 2, wave_sum, &all_u);
+    if (listed && front) m.to[holes + h - 1] = (int32_t)p;
+    if (listed && !front) m.from[high + u - 1] = (int32_t)p;
+    if (p < c.n_pages && !front && !held) m.where[p] = -1;
+    holes += all_h;
+    high += all_u;
+  }
+  __syncthreads();
+  for (int k = tid; k < high; k += kMapThreads) m.where[m.from[k]] = m.to[k];
+  if (tid == 0) {
+    *m.count = high;
+    counts[0] = n_used;
+    counts[1] = high;
+  }
+}
+
+// The first n_seqs workgroups renumber a row of the table each; the others share (page, layer, k or v) among themselves.  No page, and no
+// count, is both read and written: those that move lie at or behind u, where they go before it.
+__global__ __launch_bounds__(256) void move_kernel(KCache c, Moves m, const int32_t* __restrict__ counts) {
+  if ((int)blockIdx.x < c.n_seqs) {
+    const int s = blockIdx.x, held = c.pages_of(c.length(s)), n_used = counts[0];
+    int32_t* row = c.row(s);
+    for (int p = threadIdx.x; p < held; p += 256) {
+      const int32_t page = row[p];
+      if (c.is_page(page) && page >= n_used) {
+        const int32_t to = m.where[page];
+        if (to >= 0) row[p] = to;
+      }
+    }
+    return;
+  }
+  const int64_t units = (int64_t)*m.count * c.n_layers * 2;
+  for (int64_t x = blockIdx.x - c.n_seqs; x < units; x += gridDim.x - c.n_seqs) {
+    const int64_t l = x >> 1, layer = l % c.n_layers;
+    const int from = m.from[l / c.n_layers], to = m.to[l / c.n_layers];
+    if (x % (2 * c.n_layers) == 0 && threadIdx.x == 0) {
+      c.ref[to] = c.ref[from];
+      c.ref[from] = 0;
+    }
+    if (x & 1) copy_tokens(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, from, to, 0, c.page.d);
+    else copy_tokens(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, from, to, 0, c.page.d);
+  }
+}
+
+struct NewTokens {
+  const char *k, *v;
+  int64_t k_st, k_sh, v_st, v_sh;   // bytes
+  int64_t n;
+};
+
+// A workgroup writes kAppendTokens tokens: their rows are found by a thread each, then all threads copy.
+static constexpr int kAppendTokens = 8;
+__global__ __launch_bounds__(256) void append_kernel(KCache c, int32_t layer, const int32_t* __restrict__ seqs, const int32_t* __restrict__ cu,
+                                                     int32_t n, const int32_t* __restrict__ status, NewTokens x) {
+  __shared__ int32_t page_of[kAppendTokens], slot_of[kAppendTokens];
+  const int64_t t0 = (int64_t)blockIdx.x * kAppendTokens;
+  if (threadIdx.x < kAppendTokens) {
+    const int64_t t = t0 + threadIdx.x;
+    int page = -1, slot = 0;
+    int i = -1, behind = 0;   // the token's place, and the tokens of it from this one on
+    if (t < x.n) {
+      if (!cu) {
+        if (t < n) { i = (int)t; behind = 1; }
+      } else if (t >= cu[0] && t < cu[n]) {
+        int lo = 0, hi = n - 1;   // the last place that begins at or before t
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (cu[mid] <= t) lo = mid;
+          else hi = mid - 1;
+        }
+        i = lo;
+        behind = (int)min((int64_t)INT_MAX, cu[lo + 1] - t);
+      }
+    }
+    if (i >= 0 && (!status || status[i] == DCP_PLACE_OK)) {
+      const int s = seqs ? seqs[i] : i;
+      if (c.is_seq(s)) {
+        const int pos = c.length(s) - behind;
+        if (pos >= 0 && behind > 0) {
+          const int p = c.page.quot(pos), entry = c.row(s)[p];
+          if (c.is_page(entry)) { page = entry; slot = c.page.rem(pos, p); }
+        }
+      }
+    }
+    page_of[threadIdx.x] = page;
+    slot_of[threadIdx.x] = slot;
+  }
+  __syncthreads();
+  const int per_token = c.hkv * c.head_chunks;
+  for (int y = threadIdx.x; y < 2 * kAppendTokens * per_token; y += 256) {
+    const int row = y / c.head_chunks, off = (y - row * c.head_chunks) * 16;   // row: (k or v, token, head)
+    const int tt = c.heads.quot(row), h = c.heads.rem(row, tt), t = tt & (kAppendTokens - 1);
+    const int page = page_of[t];
+    if (page < 0) continue;
+    const int64_t slot = slot_of[t];
+    if (tt < kAppendTokens)
+      store16(c.k + layer * c.k_sl + page * c.k_sp + slot * c.k_st + h * c.k_sh + off, load16(x.k + (t0 + t) * x.k_st + h * x.k_sh + off));
+    else
+      store16(c.v + layer * c.v_sl + page * c.v_sp + slot * c.v_st + h * c.v_sh + off, load16(x.v + (t0 + t) * x.v_st + h * x.v_sh + off));
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+static bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+dcp_status_t check_rows(const char* name, const void* p, int64_t stride_t, int64_t stride_h, int32_t d) {
+  if (!p) return fail(DCP_ERR_INVALID_ARG, std::string(name) + " is NULL");
+  if (!aligned(p, 16)) return fail(DCP_ERR_INVALID_ARG, std::string(name) + " must be 16-byte aligned");
+  if (stride_h < d || stride_t < d || stride_h % 8 || stride_t % 8)
+    return fail(DCP_ERR_INVALID_ARG, std::string(name) + ": strides must be >= d and multiples of 8 elements");
+  return DCP_OK;
+}
+
+dcp_status_t pack_cache(const dcp_cache_t* cache, KCache* out) {
+  if (!cache) return fail(DCP_ERR_INVALID_ARG, "cache is NULL");
+  const dcp_cache_t& c = *cache;
+  if (c.n_layers <= 0 || c.n_pages <= 0 || c.page_size <= 0 || c.hkv <= 0 || c.d <= 0 || c.n_seqs <= 0 || c.max_pages <= 0)
+    return fail(DCP_ERR_INVALID_ARG, "n_layers, n_pages, page_size, hkv, d, n_seqs, max_pages must be positive");
+  if (c.dtype != DCP_BF16 && c.dtype != DCP_F32) return fail(DCP_ERR_UNSUPPORTED, "dtype must be DCP_BF16 or DCP_F32");
+  if (c.d != 32 && c.d != 64 && c.d != 128) return fail(DCP_ERR_UNSUPPORTED, "head_dim of a cache must be 32, 64 or 128");
+  if (c.n_seqs > DCP_CACHE_MAX_SEQS) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most " + std::to_string(DCP_CACHE_MAX_SEQS) + " sequences");
+  if (c.n_pages > (1 << 30)) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most 2^30 pages");
+  if ((int64_t)c.max_pages * c.page_size > INT32_MAX) return fail(DCP_ERR_UNSUPPORTED, "max_pages * page_size must be below 2^31");
+  const int32_t e = c.dtype == DCP_BF16 ? 2 : 4;
+  if ((int64_t)c.page_size * c.hkv * (c.d * e / 16) > (1 << 26)) return fail(DCP_ERR_UNSUPPORTED, "a page holds at most 1 GiB of keys");
+  struct { const char* name; const void* p; int64_t l, page, t, h; } kv[2] = {{"k", c.k, c.k_stride_l, c.k_stride_p, c.k_stride_t, c.k_stride_h},
+                                                                              {"v", c.v, c.v_stride_l, c.v_stride_p, c.v_stride_t, c.v_stride_h}};
+  for (auto& x : kv) {
+    if (!x.p || !aligned(x.p, 16)) return fail(DCP_ERR_INVALID_ARG, std::string(x.name) + " of the cache is NULL or not 16-byte aligned");
+    if (x.l < c.d || x.page < c.d || x.t < c.d || x.h < c.d || x.l % 8 || x.page % 8 || x.t % 8 || x.h % 8)
+      return fail(DCP_ERR_INVALID_ARG, std::string(x.name) + " of the cache: strides must be >= d and multiples of 8 elements");
+  }
+  if (!c.page_ref || !c.page_table || !c.seq_len || !aligned(c.page_ref, 4) || !aligned(c.page_table, 4) || !aligned(c.seq_len, 4))
+    return fail(DCP_ERR_INVALID_ARG, "page_ref, page_table or seq_len is NULL or misaligned");
+  KCache k{};
+  k.k = (char*)c.k; k.v = (char*)c.v;
+  k.k_sl = c.k_stride_l * e; k.k_sp = c.k_stride_p * e; k.k_st = c.k_stride_t * e; k.k_sh = c.k_stride_h * e;
+  k.v_sl = c.v_stride_l * e; k.v_sp = c.v_stride_p * e; k.v_st = c.v_stride_t * e; k.v_sh = c.v_stride_h * e;
+  k.ref = c.page_ref; k.table = c.page_table; k.len = c.seq_len;
+  k.n_layers = c.n_layers; k.n_pages = c.n_pages; k.hkv = c.hkv; k.n_seqs = c.n_seqs; k.max_pages = c.max_pages;
+  k.max_len = c.max_pages * c.page_size;
+  k.head_chunks = c.d * e / 16;
+  k.page = fast_div((uint32_t)c.page_size);
+  k.heads = fast_div((uint32_t)c.hkv);
+  *out = k;
+  return DCP_OK;
+}
+
+dcp_status_t check_places(const KCache& c, const int32_t* seqs, int32_t n) {
+  if (n < 0) return fail(DCP_ERR_INVALID_ARG, "n must not be negative");
+  if (n > DCP_CACHE_MAX_SEQS) return fail(DCP_ERR_UNSUPPORTED, "a call has at most " + std::to_string(DCP_CACHE_MAX_SEQS) + " places");
+  if (!seqs && n > c.n_seqs) return fail(DCP_ERR_INVALID_ARG, "seqs is NULL and n is more than the cache's sequences");
+  if (!aligned(seqs, 4)) return fail(DCP_ERR_INVALID_ARG, "seqs is misaligned");
+  return DCP_OK;
+}
+
+static size_t moves_bytes(int32_t n_pages) { return 4 * (64 + 2 * (size_t)n_pages + 2); }   // count, from and to (n_pages / 2 + 1 each), where
+
+}  // namespace dcp
+
+extern "C" dcp_status_t dcp_cache_reserve(const dcp_cache_t* cache, const int32_t* seqs, const int32_t* n_new, int32_t n,
+                                          int32_t* status, void* stream) {
+  KCache c;
+  dcp_status_t st = pack_cache(cache, &c);
+  if (st != DCP_OK) return st;
+  if ((st = check_places(c, seqs, n)) != DCP_OK) return st;
+  if (n == 0) return DCP_OK;
+  if (!status || !aligned(status, 4) || !aligned(n_new, 4)) return fail(DCP_ERR_INVALID_ARG, "status is NULL, or status or n_new misaligned");
+  ProfScope ps(DCP_K_CACHE, (hipStream_t)stream);
+  hipLaunchKernelGGL(take_kernel<false>, dim3(1), dim3(kMapThreads), 0, (hipStream_t)stream, c, seqs, n_new, n, status);
+  DCP_HIP_TRY(hipGetLastError());
+  return DCP_OK;
+}
+
+extern "C" dcp_status_t dcp_cache_append(const dcp_cache_t* cache, int32_t layer, const int32_t* seqs, const int32_t* cu_new, int32_t n,
+                                         const int32_t* status, const void* k_new, int64_t k_st, int64_t k_sh, const void* v_new,
+                                         int64_t v_st, int64_t v_sh, int64_t n_tokens, void* stream) {
+  KCache c;
+  dcp_status_t st = pack_cache(cache, &c);
+  if (st != DCP_OK) return st;
+  if ((st = check_places(c, seqs, n)) != DCP_OK) return st;
+  if (layer < 0 || layer >= c.n_layers) return fail(DCP_ERR_INVALID_ARG, "layer out of range");
+  if (n_tokens < 0) return fail(DCP_ERR_INVALID_ARG, "n_tokens must not be negative");
+  if (n_tokens > (1 << 26)) return fail(DCP_ERR_UNSUPPORTED, "dcp_cache_append covers at most 2^26 tokens");
+  if (!aligned(cu_new, 4) || !aligned(status, 4)) return fail(DCP_ERR_INVALID_ARG, "cu_new or status is misaligned");
+  if (n == 0 || n_tokens == 0) return DCP_OK;
+  if ((st = check_rows("k_new", k_new, k_st, k_sh, cache->d)) != DCP_OK) return st;
+  if ((st = check_rows("v_new", v_new, v_st, v_sh, cache->d)) != DCP_OK) return st;
+  const int64_t e = cache->dtype == DCP_BF16 ? 2 : 4;
+  const NewTokens x{(const char*)k_new, (const char*)v_new, k_st * e, k_sh * e, v_st * e, v_sh * e, n_tokens};
+  const int64_t wgs = (n_tokens + kAppendTokens - 1) / kAppendTokens;
+  ProfScope ps(DCP_K_CACHE, (hipStream_t)stream);
+  hipLaunchKernelGGL(append_kernel, dim3((unsigned)wgs), dim3(256), 0, (hipStream_t)stream, c, layer, seqs, cu_new, n, status, x);
+  DCP_HIP_TRY(hipGetLastError());
+  return DCP_OK;
+}
+
+extern "C" dcp_status_t dcp_cache_fork(const dcp_cache_t* cache, const int32_t* src, const int32_t* dst, int32_t n, int32_t* status,
+                                       void* stream) {
+  KCache c;
+  dcp_status_t st = pack_cache(cache, &c);
+  if (st != DCP_OK) return st;
+  if ((st = check_places(c, src, n)) != DCP_OK) return st;
+  if (n == 0) return DCP_OK;
+  if (!src || !dst || !status || !aligned(dst, 4) || !aligned(status, 4)) return fail(DCP_ERR_INVALID_ARG, "src, dst or status is NULL or misaligned");
+  if (c.n_layers > 32767) return fail(DCP_ERR_UNSUPPORTED, "dcp_cache_fork covers at most 32 767 layers");
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope ps(DCP_K_CACHE, s);
+  hipLaunchKernelGGL(take_kernel<true>, dim3(1), dim3(kMapThreads), 0, s, c, src, dst, n, status);
+  DCP_HIP_TRY(hipGetLastError());
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)n, 1 + 2 * (unsigned)c.n_layers), dim3(256), 0, s, c, src, dst, status);
+  DCP_HIP_TRY(hipGetLastError());
+  return DCP_OK;
+}
+
+extern "C" dcp_status_t dcp_cache_free(const dcp_cache_t* cache, const int32_t* seqs, int32_t n, void* stream) {
+  KCache c;
+  dcp_status_t st = pack_cache(cache, &c);
+  if (st != DCP_OK) return st;
+  if ((st = check_places(c, seqs, n)) != DCP_OK) return st;
+  if (n == 0) return DCP_OK;
+  ProfScope ps(DCP_K_CACHE, (hipStream_t)stream);
+  hipLaunchKernelGGL(free_kernel, dim3((unsigned)n), dim3(256), 0, (hipStream_t)stream, c, seqs);
+  DCP_HIP_TRY(hipGetLastError());
+  return DCP_OK;
+}
+
+extern "C" size_t dcp_cache_workspace_bytes(const dcp_cache_t* cache) {
+  return cache && cache->n_pages > 0 ? moves_bytes(cache->n_pages) : 0;
+}
+
+extern "C" dcp_status_t dcp_cache_compact(const dcp_cache_t* cache, int32_t* counts, void* workspace, size_t workspace_bytes, void* stream) {
+  KCache c;
+  dcp_status_t st = pack_cache(cache, &c);
+  if (st != DCP_OK) return st;
+  if (!counts || !aligned(counts, 4)) return fail(DCP_ERR_INVALID_ARG, "counts is NULL or misaligned");
+  if (!workspace || workspace_bytes < moves_bytes(c.n_pages)) return fail(DCP_ERR_WORKSPACE, "workspace is NULL or smaller than dcp_cache_workspace_bytes");
+  if (!aligned(workspace, 256)) return fail(DCP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  int32_t* w = (int32_t*)workspace;
+  const int32_t half = c.n_pages / 2 + 1;
+  const Moves m{w, w + 64, w + 64 + half, w + 64 + 2 * half};
+  hipStream_t s = (hipStream_t)stream;
+  ProfScope ps(DCP_K_CACHE, s);
+  hipLaunchKernelGGL(list_moves_kernel, dim3(1), dim3(kMapThreads), 0, s, c, m, counts);
+  DCP_HIP_TRY(hipGetLastError());
+  const int64_t most = (int64_t)(c.n_pages / 2 + 1) * c.n_layers * 2;
+  hipLaunchKernelGGL(move_kernel, dim3((unsigned)(c.n_seqs + std::min<int64_t>(most, 4096))), dim3(256), 0, s, c, m, counts);
+  DCP_HIP_TRY(hipGetLastError());
+  return DCP_OK;
+}

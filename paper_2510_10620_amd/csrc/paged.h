@@ -1,0 +1,45 @@
+// The paged key-value cache as its kernels see it, and the index arithmetic that they share with the host.
+#pragma once
+#include <cstdint>
+
+#include "dcp.h"
+
+#if defined(__HIPCC__)
+#define DCP_HD __host__ __device__ __forceinline__
+#else
+#define DCP_HD inline
+#endif
+
+namespace dcp {
+
+// n / d for 0 <= n < 2^31 by a multiplication: with 2^s >= d > 2^(s-1) and m = floor(2^32 (2^s - d) / d) + 1,
+// (floor(m n / 2^32) + n) >> s; the sum stays below 2^32.
+struct FastDiv {
+  uint32_t m, s, d;
+  DCP_HD int32_t quot(int32_t n) const { return (int32_t)(((uint32_t)(((uint64_t)m * (uint32_t)n) >> 32) + (uint32_t)n) >> s); }
+  DCP_HD int32_t rem(int32_t n, int32_t q) const { return n - q * (int32_t)d; }
+};
+inline FastDiv fast_div(uint32_t d) {
+  uint32_t s = 0;
+  while ((uint64_t(1) << s) < d) s++;
+  return FastDiv{(uint32_t)(((uint64_t(1) << 32) * ((uint64_t(1) << s) - d)) / d + 1), s, d};
+}
+
+// dcp_cache_t by value, strides in bytes.
+struct KCache {
+  char *k, *v;
+  int64_t k_sl, k_sp, k_st, k_sh, v_sl, v_sp, v_st, v_sh;
+  int32_t *ref, *table, *len;
+  int32_t n_layers, n_pages, hkv, n_seqs, max_pages, max_len;   // max_len: tokens that a row of the table has room for
+  int32_t head_chunks;   // 16-byte chunks of one token's head
+  FastDiv page, heads;
+
+  DCP_HD const int32_t* row(int32_t seq) const { return table + (int64_t)seq * max_pages; }
+  DCP_HD int32_t* row(int32_t seq) { return table + (int64_t)seq * max_pages; }
+  DCP_HD bool is_seq(int32_t seq) const { return (uint32_t)seq < (uint32_t)n_seqs; }
+  DCP_HD bool is_page(int32_t p) const { return (uint32_t)p < (uint32_t)n_pages; }
+  DCP_HD int32_t length(int32_t seq) const { const int32_t n = len[seq]; return n < 0 ? 0 : n > max_len ? max_len : n; }
+  DCP_HD int32_t pages_of(int32_t tokens) const { const int32_t q = page.quot(tokens); return q + (q * (int32_t)page.d < tokens); }
+};
+
+}  // namespace dcp
