@@ -409,7 +409,7 @@ dcp_status_t dcp_comm_volume(const int32_t* cu_seqlens_host, int32_t n_seq, int3
  * gets DCP_PLACE_BAD where the call has a status array and is padding elsewhere.  Page numbers outside [0, n_pages) and lengths outside
  * [0, max_pages * page_size] are never followed: such a page holds nothing, such a length is cut.
  * `status` (int32 [n], device) receives DCP_PLACE_*; a place that is not OK leaves its sequence and every page as they were.
- * At most DCP_CACHE_MAX_SEQS sequences in a cache and places in a call; n == 0 is legal.  Calls that change one cache, and
+ * At most DCP_CACHE_MAX_SEQS sequences in a cache and places in a call, 2^30 tokens in a row of the table; n == 0 is legal.  Calls that change one cache, and
  * those that read it meanwhile, must be ordered (one stream, or events).  Errors of the host's checks as elsewhere. */
 #define DCP_CACHE_MAX_SEQS 16384
 typedef enum {

@@ -359,7 +359,7 @@ dcp_status_t pack_cache(const dcp_cache_t* cache, KCache* out) {
   if (c.d != 32 && c.d != 64 && c.d != 128) return fail(DCP_ERR_UNSUPPORTED, "head_dim of a cache must be 32, 64 or 128");
   if (c.n_seqs > DCP_CACHE_MAX_SEQS) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most " + std::to_string(DCP_CACHE_MAX_SEQS) + " sequences");
   if (c.n_pages > (1 << 30)) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most 2^30 pages");
-  if ((int64_t)c.max_pages * c.page_size > INT32_MAX) return fail(DCP_ERR_UNSUPPORTED, "max_pages * page_size must be below 2^31");
+  if ((int64_t)c.max_pages * c.page_size > (1 << 30)) return fail(DCP_ERR_UNSUPPORTED, "max_pages * page_size must be at most 2^30");
   const int32_t e = c.dtype == DCP_BF16 ? 2 : 4;
   if ((int64_t)c.page_size * c.hkv * (c.d * e / 16) > (1 << 26)) return fail(DCP_ERR_UNSUPPORTED, "a page holds at most 1 GiB of keys");
   struct { const char* name; const void* p; int64_t l, page, t, h; } kv[2] = {{"k", c.k, c.k_stride_l, c.k_stride_p, c.k_stride_t, c.k_stride_h},

@@ -42,4 +42,34 @@ struct KCache {
   DCP_HD int32_t pages_of(int32_t tokens) const { const int32_t q = page.quot(tokens); return q + (q * (int32_t)page.d < tokens); }
 };
 
+// The keys that a place of a batch sees, as tiles of `tile` tokens that start at multiples of it: those that hold tokens before `head`
+// (the sink), then those that hold tokens from `lo` on; no tile twice.
+struct KeyTiles {
+  int32_t len, lo, head, n_head, first, count;   // first: number of the tile that follows the n_head ones
+  DCP_HD KeyTiles(int32_t length, int32_t window, int32_t sink, int32_t tile) {
+    len = length;
+    lo = window > 0 && length > window ? length - window : 0;
+    head = sink < lo ? sink : lo;
+    n_head = (int32_t)(((uint32_t)head + tile - 1) / tile);
+    first = lo / tile;
+    if (first < n_head) first = n_head;
+    count = n_head + (int32_t)(((uint32_t)length + tile - 1) / tile) - first;
+    if (count < 1) count = 1;   // of an empty sequence: a tile without a key
+  }
+  DCP_HD int32_t tile_at(int32_t x) const { return x < n_head ? x : x - n_head + first; }
+  DCP_HD bool sees(int32_t j) const { return (j < len) & ((j >= lo) | (j < head)); }
+};
+
+// The tiles of a batch, one after the other, dealt to workers in contiguous shares that differ by at most one.
+struct Shares {
+  int64_t total;
+  int32_t workers;
+  DCP_HD int64_t start(int32_t w) const { return total * w / workers; }
+  DCP_HD int32_t worker_of(int64_t t) const { return (int32_t)(((t + 1) * workers - 1) / total); }
+};
+DCP_HD Shares make_shares(int64_t total, int32_t most_workers, int32_t least_tiles) {
+  const int64_t w = (total + least_tiles - 1) / least_tiles;
+  return Shares{total, (int32_t)(w < most_workers ? w : most_workers)};
+}
+
 }  // namespace dcp

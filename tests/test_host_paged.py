@@ -1,6 +1,9 @@
 """Refusals of the calls on a paged cache: every one is the host's, before any launch, so that they run without a GPU
 (the addresses are never followed)."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import pytest
 
@@ -105,3 +108,16 @@ def test_attention_refuses():
     assert lib.dcp_paged_attn_fwd(_ref(c), ctypes.byref(_attn()), None, need, None) == -5
     assert lib.dcp_paged_attn_fwd(_ref(c), ctypes.byref(_attn()), A, need - 1, None) == -5
     assert lib.dcp_paged_attn_fwd(_ref(c), ctypes.byref(_attn()), A + 128, need, None) == -5
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_index_arithmetic_of_the_kernels(tmp_path):
+    """csrc/paged.h on the CPU, under the undefined-behaviour sanitizer: tests/host_paged/driver.cpp."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "host_paged")
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-I" + os.path.join(root, "include"),
+                        "-I" + os.path.join(root, "paper_2510_10620_amd", "csrc"), os.path.join(root, "tests", "host_paged", "driver.cpp"), "-o", exe],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "host-paged ok" in r.stdout, r.stdout[-2000:] + r.stderr[-3000:]
