@@ -60,16 +60,26 @@ struct KeyTiles {
   DCP_HD bool sees(int32_t j) const { return (j < len) & ((j >= lo) | (j < head)); }
 };
 
-// The tiles of a batch, one after the other, dealt to workers in contiguous shares that differ by at most one.
+// n / d by a 32-bit division where that is enough (a 64-bit one takes a few hundred instructions).
+DCP_HD int64_t quot64(int64_t n, int64_t d) { return ((uint64_t)(n | d) >> 32) == 0 ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d; }
+
+// The tiles of a batch, one after the other, dealt to workers in contiguous shares: `each` tiles, and one more for the first `more`.
 struct Shares {
-  int64_t total;
-  int32_t workers;
-  DCP_HD int64_t start(int32_t w) const { return total * w / workers; }
-  DCP_HD int32_t worker_of(int64_t t) const { return (int32_t)(((t + 1) * workers - 1) / total); }
+  int64_t each;
+  int32_t more, workers;
+  DCP_HD int64_t start(int32_t w) const { return each * w + (w < more ? w : more); }
+  DCP_HD int32_t worker_of(int64_t t) const {
+    const int64_t longer = (each + 1) * more;
+    return t < longer ? (int32_t)quot64(t, each + 1) : more + (int32_t)quot64(t - longer, each);
+  }
 };
 DCP_HD Shares make_shares(int64_t total, int32_t most_workers, int32_t least_tiles) {
   const int64_t w = (total + least_tiles - 1) / least_tiles;
-  return Shares{total, (int32_t)(w < most_workers ? w : most_workers)};
+  Shares s;
+  s.workers = (int32_t)(w < most_workers ? w : most_workers);
+  s.each = quot64(total, s.workers);
+  s.more = (int32_t)(total - s.each * s.workers);
+  return s;
 }
 
 }  // namespace dcp

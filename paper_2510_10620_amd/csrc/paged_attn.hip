@@ -16,23 +16,32 @@ struct PagedArgs {
   const int32_t* seqs;
   int64_t q_st, q_sh, o_st, o_sh;   // bytes
   int32_t n, hq, group, layer, window, sink;
-  int32_t head_sets;   // items of a place: KV heads x sets of up to 16 query heads that share one
+  // Query heads that share a KV head are taken in sets of up to 16 (or 8, see Tile::weigh); a workgroup's waves take `abreast` (1, 2 or 4) sets
+  // that lie side by side, and where there are fewer than four, the waves of a set take its tiles in turn.
+  int32_t per_kv, set_heads, abreast, log_abreast, groups;   // sets of a KV head, heads of a set at most, ..., sets / abreast
   float scale_log2e;
 };
 
-// Partial results of items (place, head set) that several workers share, unnormalised, in units of log2.  A worker's share of the tiles
+// Partial results of items (place, group of sets) that several workers share, unnormalised, in units of log2.  A worker's share of the tiles
 // begins in the middle of at most one item and ends in the middle of at most one: slot 2 w holds the first, 2 w + 1 the second.
 struct PagedParts {
-  int4* joins;    // [kWorkers] of the item whose first tile worker w has, where others have its last: (place, head set, last worker), place -1: none
-  float2* ml;     // [2 kWorkers][heads of a set] running maximum, sum
-  float* o;       // [2 kWorkers][heads of a set][D]
+  int4* joins;     // [kWorkers] (place, group, first worker, last worker), place -1: nothing to join.  By item where there are no more
+                   // items than workers, else by the worker that has the item's first tile
+  float2* ml;      // [2 kWorkers][abreast][set_heads] running maximum, sum
+  float* o;        // [2 kWorkers][abreast][set_heads][D]
+  int32_t by_item;
 };
 
-static constexpr int kWorkers = 768;     // workgroups, three on a CU
+// Two workgroups on a CU, all resident.  The four waves read neighbouring heads of the same keys: where each workgroup walks one head, a
+// quarter of what the memory reads lies in pages that others open again (8 KV heads of 256 bytes, a plain read of all keys
+// and values 5.8 TB/s against 6.9; linear 7.0).
+static constexpr int kWorkers = 512;
 static constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
 static constexpr int kSetHeads = 16;     // query heads of a matrix tile
-static constexpr int kLeastTiles = kPagedWaves;   // of a worker
+static constexpr int kLeastTiles = 4;    // of a worker
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -44,23 +53,29 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // the maximum over a tile's keys.
 template <typename T, int D> struct Tile;
 
+// Keys and values are read once, so they go past the caches (ONCE), unless several sets of heads read them.
+template <bool ONCE, typename V> __device__ __forceinline__ V load_kv(const char* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load((const V*)p);
+  else return *(const V*)p;
+}
+
 template <int D> struct Tile<bf16_t, D> {
   static constexpr int kGroup = 8, kKeys = 32, kRowTiles = 2, kAcc = D / 16;
   static constexpr int kWords = D / 32;   // 4-byte words of a lane's columns of V
   struct V { uint32_t w[kWords]; };
-  uint4 k[kRowTiles][D / 32];
+  u32x4 k[kRowTiles][D / 32];
   V v[kGroup];
 
   static __device__ __forceinline__ int k_off(int g) { return g * 16; }
   static __device__ __forceinline__ int v_off(int i) { return i * (D / 8); }
-  __device__ __forceinline__ void load_k(int s, const char* p) {
+  template <bool ONCE> __device__ __forceinline__ void load_k(int s, const char* p) {
 #pragma unroll
-    for (int x = 0; x < D / 32; x++) k[s][x] = *(const uint4*)(p + 64 * x);
+    for (int x = 0; x < D / 32; x++) k[s][x] = load_kv<ONCE, u32x4>(p + 64 * x);
   }
-  __device__ __forceinline__ void load_v(int j, const char* p) {
-    if constexpr (kWords == 4) { const uint4 u = *(const uint4*)p; v[j].w[0] = u.x; v[j].w[1] = u.y; v[j].w[2] = u.z; v[j].w[3] = u.w; }
-    else if constexpr (kWords == 2) { const uint2 u = *(const uint2*)p; v[j].w[0] = u.x; v[j].w[1] = u.y; }
-    else v[j].w[0] = *(const uint32_t*)p;
+  template <bool ONCE> __device__ __forceinline__ void load_v(int j, const char* p) {
+    if constexpr (kWords == 4) { const u32x4 u = load_kv<ONCE, u32x4>(p); v[j].w[0] = u[0]; v[j].w[1] = u[1]; v[j].w[2] = u[2]; v[j].w[3] = u[3]; }
+    else if constexpr (kWords == 2) { const u32x2 u = load_kv<ONCE, u32x2>(p); v[j].w[0] = u[0]; v[j].w[1] = u[1]; }
+    else v[j].w[0] = load_kv<ONCE, uint32_t>(p);
   }
   __device__ __forceinline__ void keep_v(int j, bool keep) {
 #pragma unroll
@@ -113,8 +128,9 @@ template <int D> struct Tile<bf16_t, D> {
         acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b2), acc[e], 0, 0, 0);
     }
   }
-  // column of acc[e][r] in lane (., g)
-  static __device__ __forceinline__ int column(int e, int r, int g) { return (4 * g + r) * kAcc + e; }
+  // Lane (., g) holds columns first(r, x, g) .. + kRun - 1 of the result in acc[x * kRun ..][r].
+  static constexpr int kRun = kAcc, kRuns = 1;
+  static __device__ __forceinline__ int first(int r, int, int g) { return (4 * g + r) * kAcc; }
 };
 
 template <int D> struct Tile<float, D> {
@@ -125,15 +141,15 @@ template <int D> struct Tile<float, D> {
 
   static __device__ __forceinline__ int k_off(int g) { return g * 16; }
   static __device__ __forceinline__ int v_off(int i) { return i * kVec * 4; }
-  __device__ __forceinline__ void load_k(int, const char* p) {
+  template <bool ONCE> __device__ __forceinline__ void load_k(int, const char* p) {
 #pragma unroll
-    for (int x = 0; x < D / 16; x++) k[x] = *(const f32x4*)(p + 64 * x);
+    for (int x = 0; x < D / 16; x++) k[x] = load_kv<ONCE, f32x4>(p + 64 * x);
   }
-  __device__ __forceinline__ void load_v(int j, const char* p) {
+  template <bool ONCE> __device__ __forceinline__ void load_v(int j, const char* p) {
     typedef float Vec __attribute__((ext_vector_type(kVec)));
 #pragma unroll
     for (int x = 0; x < kParts; x++) {
-      const Vec u = *(const Vec*)(p + 64 * kVec * x);
+      const Vec u = load_kv<ONCE, Vec>(p + 64 * kVec * x);
 #pragma unroll
       for (int y = 0; y < kVec; y++) v[j][x][y] = u[y];
     }
@@ -167,8 +183,29 @@ template <int D> struct Tile<float, D> {
 #pragma unroll
         for (int y = 0; y < kVec; y++) acc[x * kVec + y] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][x][y], p[j], acc[x * kVec + y], 0, 0, 0);
   }
-  static __device__ __forceinline__ int column(int e, int r, int g) { return (e / kVec) * 16 * kVec + (4 * g + r) * kVec + e % kVec; }
+  static constexpr int kRun = kVec, kRuns = kParts;
+  static __device__ __forceinline__ int first(int r, int x, int g) { return x * 16 * kVec + (4 * g + r) * kVec; }
 };
+
+// N values in a row: 2, 4 or 8 of them.
+template <typename T, int N> __device__ __forceinline__ void store_run(char* p, const float* o) {
+  if constexpr (sizeof(T) == 4) {
+    typedef float Vec __attribute__((ext_vector_type(N < 4 ? N : 4)));
+#pragma unroll
+    for (int x = 0; x < N; x += 4) {
+      Vec v;
+#pragma unroll
+      for (int y = 0; y < (N < 4 ? N : 4); y++) v[y] = o[x + y];
+      *(Vec*)(p + 4 * x) = v;
+    }
+  } else if constexpr (N == 2) {
+    *(uint32_t*)p = pack_bf16x2(o[0], o[1]);
+  } else if constexpr (N == 4) {
+    *(uint2*)p = make_uint2(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]));
+  } else {
+    *(uint4*)p = make_uint4(pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3]), pack_bf16x2(o[4], o[5]), pack_bf16x2(o[6], o[7]));
+  }
+}
 
 // Where the keys of a tile lie.  GROUPED: page_size is a multiple of the lanes' groups of 8 (fp32: 4) keys, so that a group shares a page
 // and one entry of the table serves it; else every key has its own.
@@ -195,26 +232,26 @@ template <typename TT, bool GROUPED> struct Where {
       slot[x] = page[x] < 0 ? 0 : slot[x];
     }
   }
-  __device__ __forceinline__ void load_k(const KCache& c, TT& t, const char* kb, int i) const {
+  template <bool ONCE> __device__ __forceinline__ void load_k(const KCache& c, TT& t, const char* kb, int i) const {
     if constexpr (GROUPED) {
       const int from = (i >> 2) << 4;
       const int32_t p = __shfl(max(page[0], 0), from), at = __shfl(slot[0], from) + (i & 3);
       const char* k = kb + p * c.k_sp + at * c.k_st;
 #pragma unroll
-      for (int x = 0; x < TT::kRowTiles; x++) t.load_k(x, k + 4 * x * c.k_st);
+      for (int x = 0; x < TT::kRowTiles; x++) t.template load_k<ONCE>(x, k + 4 * x * c.k_st);
     } else {
 #pragma unroll
-      for (int x = 0; x < kK; x++) t.load_k(x, kb + max(page[kV + x], 0) * c.k_sp + slot[kV + x] * c.k_st);
+      for (int x = 0; x < kK; x++) t.template load_k<ONCE>(x, kb + max(page[kV + x], 0) * c.k_sp + slot[kV + x] * c.k_st);
     }
   }
-  __device__ __forceinline__ void load_v(const KCache& c, TT& t, const char* vb) const {
+  template <bool ONCE> __device__ __forceinline__ void load_v(const KCache& c, TT& t, const char* vb) const {
     if constexpr (GROUPED) {
       const char* v = vb + max(page[0], 0) * c.v_sp + slot[0] * c.v_st;
 #pragma unroll
-      for (int x = 0; x < TT::kGroup; x++) t.load_v(x, v + x * c.v_st);
+      for (int x = 0; x < TT::kGroup; x++) t.template load_v<ONCE>(x, v + x * c.v_st);
     } else {
 #pragma unroll
-      for (int x = 0; x < kV; x++) t.load_v(x, vb + max(page[x], 0) * c.v_sp + slot[x] * c.v_st);
+      for (int x = 0; x < kV; x++) t.template load_v<ONCE>(x, vb + max(page[x], 0) * c.v_sp + slot[x] * c.v_st);
     }
   }
   __device__ __forceinline__ bool there(int x) const { return page[GROUPED ? 0 : x] >= 0; }
@@ -226,69 +263,68 @@ template <typename TT, bool GROUPED> struct Where {
   }
 };
 
-__device__ __forceinline__ int32_t place_tiles(const KCache& c, const PagedArgs& a, int i, int tile) {
-  const int s = a.seqs ? a.seqs[i] : i;
-  return c.is_seq(s) ? KeyTiles(c.length(s), a.window, a.sink, tile).count : 0;
-}
+__device__ __forceinline__ int32_t seq_at(const PagedArgs& a, int i) { return a.seqs ? a.seqs[i] : i; }
 
-template <typename T, int D, int COLS, bool GROUPED>
-__global__ __launch_bounds__(kPagedThreads) void paged_attn_kernel(KCache c, PagedArgs a, PagedParts parts) {
+template <typename T, int D, int COLS, bool GROUPED, bool ONCE>
+__global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, PagedArgs a, PagedParts parts) {
   typedef Tile<T, D> TT;
-  constexpr int kSet = COLS;   // heads of a set at most
-  __shared__ int64_t s_sums[kPagedThreads + 1];
-  __shared__ float s_m[kPagedWaves][kSet], s_l[kPagedWaves][kSet], s_o[kPagedWaves][kSet][D + 4];
+  __shared__ int64_t s_wave[kPagedWaves], s_before;
+  __shared__ int32_t s_place, s_seq[kPagedThreads], s_len[kPagedThreads];
+  __shared__ float s_acc[kPagedWaves - 1][TT::kAcc * 4 + 2][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4, w = blockIdx.x;
 
-  // all places' tiles, summed up by every workgroup for itself
+  // Every workgroup sums up all places' tiles for itself: thread t those of places [t per, (t + 1) per).
   const int per = (a.n + kPagedThreads - 1) / kPagedThreads;
-  {
-    int64_t mine = 0;
-    for (int x = tid * per; x < min(a.n, (tid + 1) * per); x++) mine += place_tiles(c, a, x, TT::kKeys);
-    int64_t x = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t y = __shfl_up(x, o);
-      if (lane >= o) x += y;
-    }
-    if (lane == 63) s_sums[wave] = x;
-    __syncthreads();
-    int64_t before = 0;
-    for (int y = 0; y < wave; y++) before += s_sums[y];
-    __syncthreads();
-    s_sums[tid + 1] = before + x;
-    if (tid == 0) s_sums[0] = 0;
-    __syncthreads();
+  int64_t mine = 0;
+  for (int x = tid * per; x < min(a.n, (tid + 1) * per); x++) {
+    const int seq = seq_at(a, x), len = c.is_seq(seq) ? c.length(seq) : 0;
+    if (c.is_seq(seq)) mine += KeyTiles(len, a.window, a.sink, TT::kKeys).count;
+    s_seq[tid] = seq;   // of use where a thread has one place
+    s_len[tid] = len;
   }
-  const int sets = a.head_sets, per_kv = sets / c.hkv;
-  const int64_t all = s_sums[kPagedThreads] * sets;
-  if (tid == 0) parts.joins[w] = make_int4(-1, 0, 0, 0);
+  int64_t upto = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(upto, o);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 63) s_wave[wave] = upto;
+  __syncthreads();
+  int64_t all = 0, earlier = 0;
+#pragma unroll
+  for (int y = 0; y < kPagedWaves; y++) {
+    if (y < wave) earlier += s_wave[y];
+    all += s_wave[y];
+  }
+  // nothing to join, unless the worker that begins an item says so
+  if (tid == 0 && (!parts.by_item || w >= a.n * a.groups || !c.is_seq(seq_at(a, w / a.groups)))) parts.joins[w] = make_int4(-1, 0, 0, 0);
   if (all == 0) return;
-  const Shares sh = make_shares(all, kWorkers, kLeastTiles);
+  const Shares sh = make_shares(all * a.groups, kWorkers, kLeastTiles);
   if (w >= sh.workers) return;
   int64_t at = sh.start(w);
   const int64_t end = sh.start(w + 1);
-  // the place of tile `at`, and the tiles before that place
-  int place;
-  int64_t before;
   {
-    int lo = 0, hi = kPagedThreads - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_sums[mid] * sets <= at) lo = mid;
-      else hi = mid - 1;
+    const int64_t b = (earlier + upto - mine) * a.groups;
+    if (b <= at && at < b + mine * a.groups) {
+      s_place = tid * per;
+      s_before = earlier + upto - mine;
     }
-    place = lo * per;
-    before = s_sums[lo];
   }
+  __syncthreads();
+  int place = s_place;
+  int64_t before = s_before;   // tiles of the places before it
+  const int abreast = a.abreast, turns = kPagedWaves >> a.log_abreast, turn = wave >> a.log_abreast;
   while (at < end && place < a.n) {
-    const int seq = a.seqs ? a.seqs[place] : place;
+    const int seq = per == 1 ? s_seq[place] : seq_at(a, place);
     if (!c.is_seq(seq)) { place++; continue; }
-    const KeyTiles keys(c.length(seq), a.window, a.sink, TT::kKeys);
-    if ((before + keys.count) * sets <= at) { before += keys.count; place++; continue; }
+    const KeyTiles keys(per == 1 ? s_len[place] : c.length(seq), a.window, a.sink, TT::kKeys);
+    const int64_t rel = at - before * a.groups;
+    if (rel >= (int64_t)keys.count * a.groups) { before += keys.count; place++; continue; }
     const int32_t* row = c.row(seq);
-    const int set = (int)((at - before * sets) / keys.count), t0 = (int)(at - before * sets - (int64_t)set * keys.count);
+    const int grp = (int)quot64(rel, keys.count), t0 = (int)(rel - (int64_t)grp * keys.count);
     const int t1 = (int)min((int64_t)keys.count, t0 + (end - at));
-    const int hk = set / per_kv, h0 = hk * a.group + (set - hk * per_kv) * kSetHeads, n_heads = min(kSetHeads, (hk + 1) * a.group - h0);
+    const int set = grp * abreast + (wave & (abreast - 1)), hk = a.per_kv == 1 ? set : set / a.per_kv;
+    const int h0 = hk * a.group + (set - hk * a.per_kv) * kSetHeads, n_heads = min(kSetHeads, (hk + 1) * a.group - h0);
     const int col = COLS == 8 ? i & 7 : i;
 
     typename TT::Q q;
@@ -301,21 +337,21 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attn_kernel(KCache c, Pag
     float m = -INFINITY, l = 0;
     TT t;
     Where<TT, GROUPED> now, next;
-    int x = t0 + wave;
+    int x = t0 + turn;
     int32_t base = keys.tile_at(x) * TT::kKeys, base_next = 0;
     if (x < t1) {
       now.look(c, row, base, keys.len, i, g);
+      base_next = keys.tile_at(min(x + turns, keys.count)) * TT::kKeys;
+      next.look(c, row, base_next, x + turns < t1 ? keys.len : 0, i, g);
       now.settle(c);
-      now.load_k(c, t, kb, i);
-      now.load_v(c, t, vb);
-      base_next = keys.tile_at(min(x + kPagedWaves, keys.count)) * TT::kKeys;
-      next.look(c, row, base_next, x + kPagedWaves < t1 ? keys.len : 0, i, g);
+      now.template load_k<ONCE>(c, t, kb, i);
+      now.template load_v<ONCE>(c, t, vb);
     }
-    for (; x < t1; x += kPagedWaves) {
+    for (; x < t1; x += turns) {
       float s[TT::kGroup];
       t.scores(q, s);
       next.settle(c);
-      next.load_k(c, t, kb, i);
+      next.template load_k<ONCE>(c, t, kb, i);
       const bool whole = (base + TT::kKeys <= keys.len) & ((base >= keys.lo) | (base + TT::kKeys <= keys.head));
 #pragma unroll
       for (int j = 0; j < TT::kGroup; j++) s[j] *= a.scale_log2e;
@@ -346,76 +382,102 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attn_kernel(KCache c, Pag
       }
       m = m2;
       t.template weigh<COLS>(p, i >= 8, acc);
-      next.load_v(c, t, vb);
+      next.template load_v<ONCE>(c, t, vb);
       now = next;
       base = base_next;
-      base_next = keys.tile_at(min(x + 2 * kPagedWaves, keys.count)) * TT::kKeys;
-      next.look(c, row, base_next, x + 2 * kPagedWaves < t1 ? keys.len : 0, i, g);
+      base_next = keys.tile_at(min(x + 2 * turns, keys.count)) * TT::kKeys;
+      next.look(c, row, base_next, x + 2 * turns < t1 ? keys.len : 0, i, g);
     }
 
-    // the waves meet
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if constexpr (COLS == 8 && sizeof(T) == 2) {
+    if (turns > 1) {   // the waves of a set meet, lane by lane
+      if (turn > 0 && t0 + turn < t1) {
+        float (*to)[64] = s_acc[wave - abreast];
 #pragma unroll
-      for (int e = 0; e < TT::kAcc; e++)
+        for (int e = 0; e < TT::kAcc; e++)
 #pragma unroll
-        for (int r = 0; r < 4; r++) acc[e][r] += __shfl_xor(acc[e][r], 8);
-    }
-    if (i < n_heads) {
-      if (g == 0) { s_m[wave][i] = m; s_l[wave][i] = l; }
-#pragma unroll
-      for (int e = 0; e < TT::kAcc; e++)
-#pragma unroll
-        for (int r = 0; r < 4; r++) s_o[wave][i][TT::column(e, r, g)] = acc[e][r];
-    }
-    __syncthreads();
-    const bool complete = t0 == 0 && t1 == keys.count;
-    const int slot = 2 * w + (t0 == 0);
-    for (int y = tid; y < n_heads * (D / 4); y += kPagedThreads) {
-      const int h = y / (D / 4), d = (y - h * (D / 4)) * 4;
-      float top = s_m[0][h], sum = 0;
-#pragma unroll
-      for (int v = 1; v < kPagedWaves; v++) top = fmaxf(top, s_m[v][h]);
-      const float zero = top == -INFINITY ? 0.f : top;
-      f32x4 o = {0, 0, 0, 0};
-#pragma unroll
-      for (int v = 0; v < kPagedWaves; v++) {
-        if (t0 + v >= t1) continue;   // a wave without a tile
-        const float f = __builtin_amdgcn_exp2f(s_m[v][h] - zero);
-        sum += f * s_l[v][h];
-        o += f * *(const f32x4*)&s_o[v][h][d];
+          for (int r = 0; r < 4; r++) to[4 * e + r][lane] = acc[e][r];
+        to[4 * TT::kAcc][lane] = m;
+        to[4 * TT::kAcc + 1][lane] = l;
       }
-      if (complete) {
-        const f32x4 r = sum == 0.f ? f32x4{0, 0, 0, 0} : o / sum;
-        char* p = a.out + place * a.o_st + (h0 + h) * a.o_sh + d * sizeof(T);
-        if constexpr (sizeof(T) == 2) *(uint2*)p = make_uint2(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]));
-        else *(f32x4*)p = r;
-        if (d == 0) a.lse[(int64_t)(h0 + h) * a.n + place] = sum == 0.f ? -INFINITY : zero * 0.6931471805599453f + logf(sum);
+      __syncthreads();
+      if (turn == 0) {
+        for (int v = 1; v < turns && t0 + v < t1; v++) {
+          const float (*from)[64] = s_acc[(v - 1) * abreast + wave];
+          const float mv = from[4 * TT::kAcc][lane], m2 = fmaxf(m, mv), zero = m2 == -INFINITY ? 0.f : m2;
+          const float f = __builtin_amdgcn_exp2f(m - zero), fv = __builtin_amdgcn_exp2f(mv - zero);
+          l = l * f + from[4 * TT::kAcc + 1][lane] * fv;
+#pragma unroll
+          for (int e = 0; e < TT::kAcc; e++)
+#pragma unroll
+            for (int r = 0; r < 4; r++) acc[e][r] = acc[e][r] * f + from[4 * e + r][lane] * fv;
+          m = m2;
+        }
+      }
+      __syncthreads();
+    }
+    if (turn == 0) {
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      if constexpr (COLS == 8) {
+#pragma unroll
+        for (int e = 0; e < TT::kAcc; e++)
+#pragma unroll
+          for (int r = 0; r < 4; r++) acc[e][r] += __shfl_xor(acc[e][r], 8);
+      }
+      if (t0 == 0 && t1 == keys.count) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        if (i < n_heads) {
+          char* out = a.out + place * a.o_st + (h0 + i) * a.o_sh;
+#pragma unroll
+          for (int r = 0; r < 4; r++)
+#pragma unroll
+            for (int y = 0; y < TT::kRuns; y++) {
+              float o[TT::kRun];
+#pragma unroll
+              for (int z = 0; z < TT::kRun; z++) o[z] = l == 0.f ? 0.f : acc[y * TT::kRun + z][r] * inv;
+              store_run<T, TT::kRun>(out + TT::first(r, y, g) * sizeof(T), o);
+            }
+          if (g == 0) a.lse[(int64_t)(h0 + i) * a.n + place] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.6931471805599453f + logf(l);
+        }
       } else {
-        *(f32x4*)&parts.o[((int64_t)slot * kSet + h) * D + d] = o;
-        if (d == 0) parts.ml[slot * kSet + h] = make_float2(top, sum);
+        const int slot = (2 * w + (t0 == 0)) * abreast + (wave & (abreast - 1));
+        if (i < n_heads) {
+          float* out = parts.o + ((int64_t)slot * a.set_heads + i) * D;
+#pragma unroll
+          for (int r = 0; r < 4; r++)
+#pragma unroll
+            for (int y = 0; y < TT::kRuns; y++) {
+              float o[TT::kRun];
+#pragma unroll
+              for (int z = 0; z < TT::kRun; z++) o[z] = acc[y * TT::kRun + z][r];
+              store_run<float, TT::kRun>((char*)(out + TT::first(r, y, g)), o);
+            }
+          if (g == 0) parts.ml[slot * a.set_heads + i] = make_float2(m, l);
+        }
       }
     }
-    if (!complete && t0 == 0 && tid == 0)
-      parts.joins[w] = make_int4(place, set, sh.worker_of(before * sets + (int64_t)(set + 1) * keys.count - 1), 0);
-    __syncthreads();
+    if (t0 == 0 && tid == 0) {
+      const int last = t1 == keys.count ? w : sh.worker_of(before * a.groups + (int64_t)(grp + 1) * keys.count - 1);
+      if (parts.by_item) parts.joins[place * a.groups + grp] = make_int4(last == w ? -1 : place, grp, w, last);
+      else if (last != w) parts.joins[w] = make_int4(place, grp, w, last);
+    }
     at += t1 - t0;
   }
 }
 
-// Joins the parts of an item: workgroup (w, h) takes head h of the item that worker w began and another ended.
-template <typename T, int D, int COLS>
+// Joins the parts of an item: workgroup (x, y) takes query head y of entry x of the list.
+template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(KCache c, PagedArgs a, PagedParts parts) {
-  constexpr int kSet = COLS, kLanes = D / 4, kRows = kPagedThreads / kLanes;
+  constexpr int kLanes = D / 4, kRows = kPagedThreads / kLanes;
   __shared__ float s_top[kPagedWaves], s_sum[kRows], s_o[kRows][D + 4];
-  const int tid = threadIdx.x, w = blockIdx.x, h = blockIdx.y;
-  const int4 job = parts.joins[w];
+  const int tid = threadIdx.x;
+  const int4 job = parts.joins[blockIdx.x];
   if (job.x < 0) return;
-  const int per_kv = a.head_sets / c.hkv, hk = job.y / per_kv, h0 = hk * a.group + (job.y - hk * per_kv) * kSetHeads;
+  const int beside = blockIdx.y / a.set_heads, h = blockIdx.y - beside * a.set_heads, set = job.y * a.abreast + beside;
+  const int hk = set / a.per_kv, h0 = hk * a.group + (set - hk * a.per_kv) * kSetHeads;
   if (h0 + h >= (hk + 1) * a.group) return;
-  const int n = job.z - w + 1;   // parts: slot 2 w + 1, then 2 v of the later workers v
-  auto slot = [&](int p) { return (p == 0 ? 2 * w + 1 : 2 * (w + p)) * kSet + h; };
+  const int w = job.z, n = job.w - w + 1;   // parts: slot 2 w + 1, then 2 v of the later workers v
+  auto slot = [&](int p) { return ((p == 0 ? 2 * w + 1 : 2 * (w + p)) * a.abreast + beside) * a.set_heads + h; };
   float top = -INFINITY;
   for (int p = tid; p < n; p += kPagedThreads) top = fmaxf(top, parts.ml[slot(p)].x);
 #pragma unroll
@@ -428,6 +490,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(KCache c, Pag
   const int r = tid / kLanes, d = (tid - r * kLanes) * 4;
   f32x4 o = {0, 0, 0, 0};
   float sum = 0;
+#pragma unroll 4
   for (int p = r; p < n; p += kRows) {
     const float2 ml = parts.ml[slot(p)];
     const float f = __builtin_amdgcn_exp2f(ml.x - zero);
@@ -443,18 +506,24 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(KCache c, Pag
     sum += s_sum[x];
     o += *(const f32x4*)&s_o[x][d];
   }
-  const f32x4 res = sum == 0.f ? f32x4{0, 0, 0, 0} : o / sum;
-  char* out = a.out + job.x * a.o_st + (h0 + h) * a.o_sh + d * sizeof(T);
-  if constexpr (sizeof(T) == 2) *(uint2*)out = make_uint2(pack_bf16x2(res[0], res[1]), pack_bf16x2(res[2], res[3]));
-  else *(f32x4*)out = res;
+  float res[4];
+#pragma unroll
+  for (int x = 0; x < 4; x++) res[x] = sum == 0.f ? 0.f : o[x] / sum;
+  store_run<T, 4>(a.out + job.x * a.o_st + (h0 + h) * a.o_sh + d * sizeof(T), res);
   if (d == 0) a.lse[(int64_t)(h0 + h) * a.n + job.x] = sum == 0.f ? -INFINITY : zero * 0.6931471805599453f + logf(sum);
 }
 
+template <typename T, int D, int COLS, bool ONCE>
+static void launch_once(const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
+  if (c.page.d % Tile<T, D>::kGroup == 0) hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, true, ONCE>), dim3(kWorkers), dim3(kPagedThreads), 0, s, c, a, parts);
+  else hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, false, ONCE>), dim3(kWorkers), dim3(kPagedThreads), 0, s, c, a, parts);
+}
 template <typename T, int D, int COLS>
 static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
-  if (c.page.d % Tile<T, D>::kGroup == 0) hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, true>), dim3(kWorkers), dim3(kPagedThreads), 0, s, c, a, parts);
-  else hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, false>), dim3(kWorkers), dim3(kPagedThreads), 0, s, c, a, parts);
-  hipLaunchKernelGGL((paged_join_kernel<T, D, COLS>), dim3(kWorkers, (unsigned)std::min(a.group, COLS)), dim3(kPagedThreads), 0, s, c, a, parts);
+  if (a.per_kv == 1) launch_once<T, D, COLS, true>(c, a, parts, s);
+  else if constexpr (COLS == kSetHeads) launch_once<T, D, COLS, false>(c, a, parts, s);   // more sets than one are full ones
+  const int entries = parts.by_item ? a.n * a.groups : kWorkers;
+  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)entries, (unsigned)(a.abreast * a.set_heads)), dim3(kPagedThreads), 0, s, c, a, parts);
 }
 template <typename T, int COLS>
 static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts, int d, hipStream_t s) {
@@ -463,15 +532,30 @@ static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts,
   else launch<T, 32, COLS>(c, a, parts, s);
 }
 
-// The largest set of heads of a launch: 8 columns where a weight's two parts lie side by side.
-static int set_columns(int32_t dtype, int group) { return dtype == DCP_BF16 && group <= 8 ? 8 : kSetHeads; }
-static size_t parts_bytes(int columns, int d) { return kWorkers * (sizeof(int4) + 2 * (size_t)columns * (sizeof(float2) + d * sizeof(float))); }
+// How the query heads are taken: see PagedArgs.
+struct Sets {
+  int32_t per_kv, heads, abreast, log_abreast;
+  int64_t groups;
+  size_t bytes;   // of the workspace
+};
+static Sets sets_of(int32_t hkv, int32_t hq, int32_t d) {
+  const int32_t group = hq / hkv;
+  Sets s;
+  s.per_kv = (group + kSetHeads - 1) / kSetHeads;
+  s.heads = std::min(group, kSetHeads);
+  const int64_t sets = (int64_t)hkv * s.per_kv;
+  s.log_abreast = sets % 4 == 0 ? 2 : sets % 2 == 0 ? 1 : 0;
+  s.abreast = 1 << s.log_abreast;
+  s.groups = sets / s.abreast;
+  s.bytes = kWorkers * (sizeof(int4) + 2 * (size_t)s.abreast * s.heads * (sizeof(float2) + d * sizeof(float)));
+  return s;
+}
 
 }  // namespace dcp
 
 extern "C" size_t dcp_paged_attn_workspace_bytes(const dcp_cache_t* cache, int32_t n, int32_t hq) {
   if (!cache || n <= 0 || hq <= 0 || cache->hkv <= 0 || cache->d <= 0) return 0;
-  return parts_bytes(set_columns(cache->dtype, hq / cache->hkv), cache->d);
+  return hq % cache->hkv ? 0 : sets_of(cache->hkv, hq, cache->d).bytes;
 }
 
 extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t* args, void* workspace, size_t workspace_bytes,
@@ -501,20 +585,20 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
     const char* o1 = o0 + ((t.n - 1) * t.o_stride_t + (t.hq - 1) * t.o_stride_h + cache->d) * e;
     if (q0 < o1 && o0 < q1) return fail(DCP_ERR_INVALID_ARG, "out overlaps q");
   }
-  const int group = t.hq / c.hkv, columns = set_columns(cache->dtype, group);
-  const int64_t sets = (int64_t)c.hkv * ((group + kSetHeads - 1) / kSetHeads);
-  if (sets > (1 << 12)) return fail(DCP_ERR_UNSUPPORTED, "dcp_paged_attn_fwd covers at most 4 096 sets of 16 query heads on one KV head");
+  const Sets sets = sets_of(c.hkv, t.hq, cache->d);
+  if (sets.groups * sets.abreast > (1 << 12)) return fail(DCP_ERR_UNSUPPORTED, "dcp_paged_attn_fwd covers at most 4 096 sets of 16 query heads on one KV head");
   const PagedArgs a{(const char*)t.q, (char*)t.out, t.lse, t.seqs, t.q_stride_t * e, t.q_stride_h * e, t.o_stride_t * e, t.o_stride_h * e,
-                    t.n, t.hq, group, t.layer, t.window, t.sink, (int32_t)sets, t.softmax_scale * 1.44269504088896340736f};
-  char* w = (char*)workspace;
+                    t.n, t.hq, t.hq / c.hkv, t.layer, t.window, t.sink, sets.per_kv, sets.heads, sets.abreast, sets.log_abreast, (int32_t)sets.groups,
+                    t.softmax_scale * 1.44269504088896340736f};
   PagedParts parts;
-  parts.joins = (int4*)w;
-  parts.o = (float*)(w + kWorkers * sizeof(int4));
-  parts.ml = (float2*)(parts.o + 2 * (size_t)kWorkers * columns * cache->d);
+  parts.joins = (int4*)workspace;
+  parts.o = (float*)(parts.joins + kWorkers);
+  parts.ml = (float2*)(parts.o + 2 * (size_t)kWorkers * sets.abreast * sets.heads * cache->d);
+  parts.by_item = t.n * sets.groups <= kWorkers;
   hipStream_t s = (hipStream_t)stream;
   ProfScope ps(DCP_K_PAGED_ATTN, s);
   if (cache->dtype == DCP_F32) launch<float, 16>(c, a, parts, cache->d, s);
-  else if (columns == 8) launch<bf16_t, 8>(c, a, parts, cache->d, s);
+  else if (a.group <= 8) launch<bf16_t, 8>(c, a, parts, cache->d, s);
   else launch<bf16_t, 16>(c, a, parts, cache->d, s);
   DCP_HIP_TRY(hipGetLastError());
   return DCP_OK;
