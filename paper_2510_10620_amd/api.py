@@ -460,24 +460,32 @@ class Program:
 # paged key-value cache
 class Cache:
     """dcp_cache_t over the caller's tensors, which it keeps alive: k, v [layers, pages, page_size, hkv, d] (any strides with d
-    contiguous), page_ref int32 [pages], page_table int32 [seqs, max_pages], seq_len int32 [seqs], all on one device."""
+    contiguous), page_ref int32 [pages], page_table int32 [seqs, max_pages], seq_len int32 [seqs], all on one device, which has to be
+    the current one when a call is made."""
 
     def __init__(self, k, v, page_ref, page_table, seq_len):
+        import torch
         if k.dim() != 5 or v.shape != k.shape or v.dtype != k.dtype:
             raise ValueError("k and v: [layers, pages, page_size, hkv, d] of one shape and dtype")
         if page_ref.dim() != 1 or page_ref.shape[0] != k.shape[1] or page_table.dim() != 2 or seq_len.dim() != 1 or seq_len.shape[0] != page_table.shape[0]:
             raise ValueError("page_ref [pages], page_table [seqs, max_pages], seq_len [seqs]")
-        self.k, self.v, self.page_ref, self.page_table, self.seq_len, self.device = k, v, page_ref, page_table, seq_len, k.device
+        if not k.is_cuda:
+            raise ValueError("k: device tensor required")
+        self.k, self.v, self.page_ref, self.page_table, self.seq_len = k, v, page_ref, page_table, seq_len
+        self.device, self._index, self._dtype, self._heads, self._i32, self._f32 = k.device, k.device.index, k.dtype, k.shape[3:], torch.int32, torch.float32
+        # the current stream as a number; torch.cuda.current_stream builds an object, which takes longer than a launch
+        self._raw_stream, self._raw_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        self._lib = _lib.load()
         d = self.descr = _lib.Cache()
         d.n_layers, d.n_pages, d.page_size, d.hkv, d.d = k.shape
         d.dtype, d.n_seqs, d.max_pages = _dtype_code(k), page_table.shape[0], page_table.shape[1]
         for name, t in (("k", k), ("v", v)):
-            self._rows(name, t)
-            setattr(d, name, t.data_ptr())
+            setattr(d, name, self._rows(name, t))
             for axis, letter in enumerate("lpth"):
                 # a dimension of one element has no stride of its own
                 setattr(d, f"{name}_stride_{letter}", t.stride(axis) if t.shape[axis] > 1 else max(8, t.shape[4]))
-        d.page_ref, d.page_table, d.seq_len = self._ints("page_ref", page_ref), self._ints("page_table", page_table), self._ints("seq_len", seq_len)
+        d.page_ref, d.seq_len = self._ints("page_ref", page_ref, page_ref.shape[0]), self._ints("seq_len", seq_len, seq_len.shape[0])
+        d.page_table = self._ints("page_table", page_table, page_table.numel())
         self.ref = ctypes.byref(d)
 
     @classmethod
@@ -489,16 +497,15 @@ class Cache:
         return cls(*kv, zeros[0], torch.full((seqs, max_pages), -1, dtype=torch.int32, device=device), zeros[1])
 
     def _rows(self, name, t):
-        if not t.is_cuda or t.device != self.device or t.stride(-1) != 1:
-            raise ValueError(f"{name}: tensor with contiguous last dim on the cache's device required")
+        if t.dtype != self._dtype or t.stride(-1) != 1 or t.device != self.device:
+            raise ValueError(f"{name}: tensor of the cache's dtype with contiguous last dim on its device required")
         return t.data_ptr()
 
-    def _ints(self, name, t, shape=None):
-        import torch
+    def _ints(self, name, t, n):
         if t is None:
             return None
-        if t.dtype != torch.int32 or not t.is_contiguous() or t.device != self.device or (shape is not None and tuple(t.shape) != shape):
-            raise ValueError(f"{name}: contiguous int32 tensor on the cache's device required" + (f", of shape {shape}" if shape is not None else ""))
+        if t.dtype != self._i32 or t.numel() != n or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"{name}: contiguous int32 tensor of {n} elements on the cache's device required")
         return t.data_ptr()
 
     def _space(self, workspace):
@@ -507,75 +514,72 @@ class Cache:
         return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
     def _stream(self):
-        import torch
-        if torch.cuda.current_device() != self.device.index:
+        if self._raw_device() != self._index:
             raise ValueError(f"the cache lies on {self.device}, which is not the current device")
-        return _stream()
+        return self._raw_stream(self._index)
+
+    def _token_rows(self, name, t):
+        """[tokens, heads, d]: (address, token stride, head stride); a dimension of one element has no stride of its own."""
+        n, h, d = t.shape
+        st, sh, _ = t.stride()
+        return self._rows(name, t), st if n > 1 else max(8, d), sh if h > 1 else max(8, d)
 
 
 def dcp_cache_reserve(cache, seqs, status, n_new=None):
     """Room for n_new (int32 [n]; None: one) more tokens of each place; seqs int32 [n] or None; status int32 [n] receives DCP_PLACE_*."""
     n = status.numel()
-    _check(_lib.load().dcp_cache_reserve(cache.ref, cache._ints("seqs", seqs, (n,)), cache._ints("n_new", n_new, (n,)), n,
-                                         cache._ints("status", status, (n,)), cache._stream()))
+    _check(cache._lib.dcp_cache_reserve(cache.ref, cache._ints("seqs", seqs, n), cache._ints("n_new", n_new, n), n,
+                                        cache._ints("status", status, n), cache._stream()))
 
 
 def dcp_cache_append(cache, k_new, v_new, seqs=None, cu_new=None, status=None, layer=0):
     """k_new, v_new [tokens, hkv, d] go to the last places of the sequences: place i has rows [cu_new[i], cu_new[i + 1]), or row i."""
-    n = cu_new.numel() - 1 if cu_new is not None else k_new.shape[0] if seqs is None else seqs.numel()
-    if k_new.dim() != 3 or k_new.shape != v_new.shape or tuple(k_new.shape[1:]) != tuple(cache.k.shape[3:]) or k_new.dtype != cache.k.dtype or v_new.dtype != cache.k.dtype:
-        raise ValueError("k_new, v_new: [tokens, hkv, d] of the cache's dtype, hkv and d")
-    if cu_new is None and k_new.shape[0] != n:
+    tokens = k_new.shape[0]
+    n = cu_new.numel() - 1 if cu_new is not None else tokens if seqs is None else seqs.numel()
+    if k_new.dim() != 3 or k_new.shape != v_new.shape or k_new.shape[1:] != cache._heads:
+        raise ValueError("k_new, v_new: [tokens, hkv, d] with the cache's hkv and d")
+    if cu_new is None and tokens != n:
         raise ValueError("without cu_new there is one token per place")
-    (k_st, k_sh), (v_st, v_sh) = _row_strides(k_new), _row_strides(v_new)
-    _check(_lib.load().dcp_cache_append(cache.ref, int(layer), cache._ints("seqs", seqs, (n,)), cache._ints("cu_new", cu_new, (n + 1,)), n,
-                                        cache._ints("status", status, (n,)), cache._rows("k_new", k_new), k_st, k_sh,
-                                        cache._rows("v_new", v_new), v_st, v_sh, k_new.shape[0], cache._stream()))
+    _check(cache._lib.dcp_cache_append(cache.ref, layer, cache._ints("seqs", seqs, n), cache._ints("cu_new", cu_new, n + 1), n,
+                                       cache._ints("status", status, n), *cache._token_rows("k_new", k_new), *cache._token_rows("v_new", v_new),
+                                       tokens, cache._stream()))
 
 
 def dcp_cache_fork(cache, src, dst, status):
     """Empty sequences dst[i] become copies of src[i]."""
     n = status.numel()
-    _check(_lib.load().dcp_cache_fork(cache.ref, cache._ints("src", src, (n,)), cache._ints("dst", dst, (n,)), n,
-                                      cache._ints("status", status, (n,)), cache._stream()))
+    _check(cache._lib.dcp_cache_fork(cache.ref, cache._ints("src", src, n), cache._ints("dst", dst, n), n, cache._ints("status", status, n),
+                                     cache._stream()))
 
 
 def dcp_cache_free(cache, seqs):
-    _check(_lib.load().dcp_cache_free(cache.ref, cache._ints("seqs", seqs, (seqs.numel(),)), seqs.numel(), cache._stream()))
+    n = seqs.numel()
+    _check(cache._lib.dcp_cache_free(cache.ref, cache._ints("seqs", seqs, n), n, cache._stream()))
 
 
 def dcp_cache_workspace_bytes(cache):
-    return int(_lib.load().dcp_cache_workspace_bytes(cache.ref))
+    return int(cache._lib.dcp_cache_workspace_bytes(cache.ref))
 
 
 def dcp_cache_compact(cache, counts, workspace):
     """Pages in use move to the front; counts int32 [2]: pages in use, pages moved."""
-    _check(_lib.load().dcp_cache_compact(cache.ref, cache._ints("counts", counts, (2,)), *cache._space(workspace), cache._stream()))
-
-
-def _row_strides(t):
-    """Token and head strides; a dimension of one element has none of its own."""
-    d = max(8, t.shape[2])
-    return (t.stride(0) if t.shape[0] > 1 else d), (t.stride(1) if t.shape[1] > 1 else d)
+    _check(cache._lib.dcp_cache_compact(cache.ref, cache._ints("counts", counts, 2), *cache._space(workspace), cache._stream()))
 
 
 def dcp_paged_attn_workspace_bytes(cache, n, hq):
-    return int(_lib.load().dcp_paged_attn_workspace_bytes(cache.ref, int(n), int(hq)))
+    return int(cache._lib.dcp_paged_attn_workspace_bytes(cache.ref, int(n), int(hq)))
 
 
 def dcp_paged_attn_fwd(cache, q, out, lse, softmax_scale, workspace, seqs=None, window=0, sink=0, layer=0):
     """q, out [n, hq, d], lse float [hq, n]: one new token of each place over its sequence."""
-    import torch
     n, hq, d = q.shape
-    if out.shape != q.shape or q.dtype != cache.k.dtype or out.dtype != q.dtype or d != cache.k.shape[4]:
-        raise ValueError("q, out: [n, hq, d] of the cache's dtype and d")
-    if lse.dtype != torch.float32 or tuple(lse.shape) != (hq, n) or not lse.is_contiguous() or lse.device != cache.device:
+    if out.shape != q.shape or d != cache._heads[1]:
+        raise ValueError("q, out: [n, hq, d] with the cache's d")
+    if lse.dtype != cache._f32 or lse.shape != (hq, n) or not lse.is_contiguous() or lse.device != cache.device:
         raise ValueError("lse: contiguous float32 tensor [hq, n] on the cache's device")
-    a = _lib.PagedAttn()
-    a.n, a.hq, a.layer, a.softmax_scale, a.window, a.sink = n, hq, int(layer), softmax_scale, int(window), int(sink)
-    a.seqs, a.q, a.out, a.lse = cache._ints("seqs", seqs, (n,)), cache._rows("q", q), cache._rows("out", out), lse.data_ptr()
-    (a.q_stride_t, a.q_stride_h), (a.o_stride_t, a.o_stride_h) = _row_strides(q), _row_strides(out)
-    _check(_lib.load().dcp_paged_attn_fwd(cache.ref, ctypes.byref(a), *cache._space(workspace), cache._stream()))
+    args = _lib.PagedAttn(n, hq, layer, softmax_scale, window, sink, cache._ints("seqs", seqs, n), *cache._token_rows("q", q),
+                          *cache._token_rows("out", out), lse.data_ptr())
+    _check(cache._lib.dcp_paged_attn_fwd(cache.ref, ctypes.byref(args), *cache._space(workspace), cache._stream()))
 
 
 KERNEL_IDS = dict(fwd=0, merge=1, delta=2, dq=3, dkv=4, sum=5, copy=6, paged_attn=7, cache=8)

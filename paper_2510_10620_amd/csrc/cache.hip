@@ -70,13 +70,21 @@ __device__ __forceinline__ Place place_at(const KCache& c, const int32_t* a, con
 
 // One workgroup: the places' needs are summed up in their order, page_ref is walked once, and the k-th free page goes to the place
 // whose sums k falls between.  That a place finds too few pages is known at the end: the one that got some gives them back.
-// Bound by latency: three dependent trips to memory, then 4 bytes a page.
+// Bound by latency: two dependent trips to memory (the places, their lengths; the first 8 192 entries of page_ref come meanwhile), and one
+// for each further 8 192 pages until enough are found.  Up to kMapThreads places stay in registers and LDS, more are worked out anew.
 template <bool FORK>
 __global__ __launch_bounds__(kMapThreads) void take_kernel(KCache c, const int32_t* __restrict__ a, const int32_t* __restrict__ b,
                                                            int32_t n, int32_t* __restrict__ status) {
-  __shared__ int32_t owner[DCP_CACHE_MAX_SEQS], sums[DCP_CACHE_MAX_SEQS], wave_sum[kMapWaves], short_place;
+  __shared__ int32_t owner[DCP_CACHE_MAX_SEQS], sums[DCP_CACHE_MAX_SEQS], seqs[kMapThreads], firsts[kMapThreads], wave_sum[kMapWaves], short_place;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int cap = c.n_pages + 1;
+  const bool few = n <= kMapThreads;
+  int32_t held[kScan];
+  auto scan = [&](int64_t first) {
+#pragma unroll
+    for (int u = 0; u < kScan; u++) held[u] = first + u * 64 < c.n_pages ? c.ref[first + u * 64] : 1;
+  };
+  scan(wave * (64 * kScan) + lane);
   for (int s = tid; s < c.n_seqs; s += kMapThreads) owner[s] = kNoOwner;
   if (tid == 0) short_place = -1;
   __syncthreads();
@@ -87,32 +95,38 @@ __global__ __launch_bounds__(kMapThreads) void take_kernel(KCache c, const int32
     if (c.is_seq(t)) atomicMin(&owner[t], i);
   }
   __syncthreads();
+  Place mine{-1, 0, 0, 0, DCP_PLACE_OK};
   int total = 0;
   for (int base = 0; base < n; base += kMapThreads) {
     const int i = base + tid;
+    if (i < n) mine = place_at<FORK>(c, a, b, i, owner);
     int all;
-    const int x = block_sum(i < n ? min(place_at<FORK>(c, a, b, i, owner).need, cap) : 0, cap, wave_sum, &all);
+    const int x = block_sum(i < n ? min(mine.need, cap) : 0, cap, wave_sum, &all);
     if (i < n) sums[i] = min(total + x, cap);
     total = min(total + all, cap);
   }
+  if (few) { seqs[tid] = mine.seq; firsts[tid] = mine.first; }
   __syncthreads();
   int found = 0;
   for (int64_t base = 0; base < c.n_pages && found < total; base += kMapThreads * kScan) {
     const int64_t first = base + wave * (64 * kScan) + lane;
-    int32_t held[kScan];
-#pragma unroll
-    for (int u = 0; u < kScan; u++) held[u] = first + u * 64 < c.n_pages ? c.ref[first + u * 64] : 1;
+    if (base) scan(first);
     uint64_t mask[kScan];
-    int mine = 0;
+    int free_here = 0;
 #pragma unroll
     for (int u = 0; u < kScan; u++) {
       mask[u] = __ballot(held[u] <= 0);
-      mine += __popcll(mask[u]);
+      free_here += __popcll(mask[u]);
     }
-    int all;
-    // the wave's count enters the sum once
-    int k = found + block_sum(lane == 63 ? mine : 0, INT_MAX / 2, wave_sum, &all) - (lane == 63 ? mine : 0);
-    k = __shfl(k, 63);
+    __syncthreads();
+    if (lane == 0) wave_sum[wave] = free_here;
+    __syncthreads();
+    int k = found, all = 0;   // k: free pages before the wave's
+#pragma unroll
+    for (int w = 0; w < kMapWaves; w++) {
+      if (w < wave) k += wave_sum[w];
+      all += wave_sum[w];
+    }
 #pragma unroll
     for (int u = 0; u < kScan; u++) {
       const int rank = k + __popcll(mask[u] & ((uint64_t(1) << lane) - 1));
@@ -123,9 +137,11 @@ __global__ __launch_bounds__(kMapThreads) void take_kernel(KCache c, const int32
           if (sums[mid] > rank) hi = mid;
           else lo = mid + 1;
         }
-        const Place p = place_at<FORK>(c, a, b, lo, owner);
+        int seq, entry;
+        if (few) { seq = seqs[lo]; entry = firsts[lo]; }
+        else { const Place p = place_at<FORK>(c, a, b, lo, owner); seq = p.seq; entry = p.first; }
         const int32_t page = (int32_t)(first + u * 64);
-        c.row(p.seq)[p.first + rank - (lo ? sums[lo - 1] : 0)] = page;
+        c.row(seq)[entry + rank - (lo ? sums[lo - 1] : 0)] = page;
         c.ref[page] = 1;
       }
       k += __popcll(mask[u]);
@@ -135,7 +151,7 @@ __global__ __launch_bounds__(kMapThreads) void take_kernel(KCache c, const int32
   __syncthreads();
   // Lengths change here only.  A place reads the length of its own sequence, and of a source that nobody changes.
   for (int i = tid; i < n; i += kMapThreads) {
-    Place p = place_at<FORK>(c, a, b, i, owner);
+    Place p = few ? mine : place_at<FORK>(c, a, b, i, owner);
     if (p.seq >= 0 && p.need > 0 && sums[i] > found) {
       p.code = DCP_PLACE_FULL;
       if ((i ? sums[i - 1] : 0) < found) short_place = i;
@@ -161,43 +177,68 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ u32x4 load16(const char* p) { return __builtin_nontemporal_load((const u32x4*)p); }
 __device__ __forceinline__ void store16(char* p, u32x4 v) { __builtin_nontemporal_store(v, (u32x4*)p); }
 
-// Tokens [t0, t1) of page `from` to page `to` of one layer of k or v, by one workgroup of 256.
-__device__ __forceinline__ void copy_tokens(const KCache& c, char* base, int64_t st_p, int64_t st_t, int64_t st_h, int from, int to, int t0, int t1) {
+// 16-byte chunks [first, last) of page `from` to page `to`, of one layer of k or v, by one workgroup of 256: chunk x is chunk x % head_chunks of
+// (token, head) x / head_chunks.  Four in flight a lane.
+__device__ __forceinline__ void copy_chunks(const KCache& c, char* base, int64_t st_p, int64_t st_t, int64_t st_h, int from, int to, int first, int last) {
   const char* src = base + from * st_p;
   char* dst = base + to * st_p;
-  const int per_token = c.hkv * c.head_chunks, n = (t1 - t0) * per_token;
-  for (int x = threadIdx.x; x < n; x += 256) {
-    const int row = x / c.head_chunks, off = x - row * c.head_chunks;   // row: (token, head)
-    const int t = c.heads.quot(row), h = c.heads.rem(row, t);
-    const int64_t at = (t0 + t) * st_t + h * st_h + off * 16;
+  auto offset = [&](int x) {
+    const int row = x >> c.log_head_chunks, t = c.heads.quot(row);
+    return t * st_t + c.heads.rem(row, t) * st_h + (x & ((1 << c.log_head_chunks) - 1)) * 16;
+  };
+  int x = first + threadIdx.x;
+  for (; x + 768 < last; x += 1024) {
+    int64_t at[4];
+    u32x4 v[4];
+#pragma unroll
+    for (int y = 0; y < 4; y++) { at[y] = offset(x + 256 * y); v[y] = load16(src + at[y]); }
+#pragma unroll
+    for (int y = 0; y < 4; y++) store16(dst + at[y], v[y]);
+  }
+  for (; x < last; x += 256) {
+    const int64_t at = offset(x);
     store16(dst + at, load16(src + at));
   }
 }
 
-// After take_kernel: workgroup (i, 0) shares the whole pages of place i, (i, 1 + 2 layer + (0: k, 1: v)) copies the page being filled.
-__global__ __launch_bounds__(256) void fork_kernel(KCache c, const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
-                                                   const int32_t* __restrict__ status) {
-  const int i = blockIdx.x;
-  const int a = src[i];
-  if (a < 0 || status[i] != DCP_PLACE_OK) return;
-  const int b = dst[i], len = c.length(a), whole = c.page.quot(len);
-  const int32_t* from = c.row(a);
-  int32_t* to = c.row(b);
-  if (blockIdx.y == 0) {
-    for (int p = threadIdx.x; p < whole; p += 256) {
-      const int32_t page = from[p];
-      to[p] = page;
-      if (c.is_page(page)) atomicAdd(&c.ref[page], 1);
+// What a workgroup copies at a time: kPieceChunks chunks (16 KiB) of a page, so that pages that are filled unevenly, or few, still fill the chip
+// (64 sequences forked, 4 layers, pages of 512 KiB: 93 us with a workgroup a page, 47 so).
+static constexpr int kPieceChunks = 1024;
+// Workgroups that share such pieces, each taking every kCopyWorkers-th: half of 9 712 pages of 4 layers moved, 5.1 GB read and written, in 995
+// us with 4 096, 980 with 16 384 and 64 KiB at a time, 842 to 960 (by where the pages lie) so: 5.3 to 6.0 TB/s.
+static constexpr int kCopyWorkers = 32768;
+inline int pieces_of(const KCache& c) { return (int)(((int64_t)c.page.d * c.hkv * c.head_chunks() + kPieceChunks - 1) / kPieceChunks); }
+
+// After take_kernel.  Of place i's units the first shares its whole pages, unit 1 + x copies a piece of the page being filled, x = 2 (layer pieces
+// + piece) + (0: k, 1: v).
+__global__ __launch_bounds__(256) void fork_kernel(KCache c, const int32_t* __restrict__ src, const int32_t* __restrict__ dst, int32_t n,
+                                                   const int32_t* __restrict__ status, int32_t pieces) {
+  const int64_t per_place = 1 + 2 * (int64_t)c.n_layers * pieces, units = n * per_place;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int i = (int)quot64(unit, per_place);
+    const int64_t y = unit - i * per_place;
+    const int a = src[i], b = dst[i];
+    if (a < 0 || status[i] != DCP_PLACE_OK) continue;
+    const int len = c.length(a), whole = c.page.quot(len);
+    const int32_t* from = c.row(a);
+    int32_t* to = c.row(b);
+    if (y == 0) {
+      for (int p = threadIdx.x; p < whole; p += 256) {
+        const int32_t page = from[p];
+        to[p] = page;
+        if (c.is_page(page)) atomicAdd(&c.ref[page], 1);
+      }
+      continue;
     }
-    return;
+    const int64_t x = (y - 1) >> 1, layer = quot64(x, pieces);
+    const int first = (int)(x - layer * pieces) * kPieceChunks;
+    const int last = min(first + kPieceChunks, c.page.rem(len, whole) * c.hkv << c.log_head_chunks);
+    if (first >= last) continue;
+    const int32_t page = from[whole], mine = to[whole];
+    if (!c.is_page(page) || !c.is_page(mine)) continue;
+    if (y & 1) copy_chunks(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, page, mine, first, last);
+    else copy_chunks(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, page, mine, first, last);
   }
-  const int filled = c.page.rem(len, whole);
-  if (!filled) return;
-  const int32_t page = from[whole], mine = to[whole];
-  if (!c.is_page(page) || !c.is_page(mine)) return;
-  const int layer = (blockIdx.y - 1) >> 1;
-  if (blockIdx.y & 1) copy_tokens(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, page, mine, 0, filled);
-  else copy_tokens(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, page, mine, 0, filled);
 }
 
 // One workgroup a place.  The length is taken by an exchange, so that a sequence that is named twice is freed once.
@@ -221,31 +262,78 @@ struct Moves {
   int32_t *count, *from, *to, *where;   // [1], [n_pages / 2 + 1], [n_pages / 2 + 1], [n_pages]: of the pages behind those in use, -1: free
 };
 
-// One workgroup: counts the pages in use (u), then lists the free ones before u and the used ones behind it, which are as many.
+// One workgroup: counts the pages in use (u), then lists the free ones before u and the used ones behind it, which are as many.  page_ref is
+// read twice, 8 192 pages at a time (the second time from the cache).
 __global__ __launch_bounds__(kMapThreads) void list_moves_kernel(KCache c, Moves m, int32_t* __restrict__ counts) {
-  __shared__ int32_t wave_sum[kMapWaves];
-  const int tid = threadIdx.x;
+  __shared__ int32_t wave_sum[kMapWaves], wave_high[kMapWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int32_t held[kScan];
+  auto scan = [&](int64_t first) {
+#pragma unroll
+    for (int u = 0; u < kScan; u++) held[u] = first + u * 64 < c.n_pages ? c.ref[first + u * 64] : 0;
+  };
   int used = 0;
-  for (int64_t p = tid; p < c.n_pages; p += kMapThreads) used += c.ref[p] > 0;
-  int total;
-  block_sum(used, INT_MAX / 2, wave_sum, &total);
-  const int n_used = total;
+  for (int64_t base = 0; base < c.n_pages; base += kMapThreads * kScan) {
+    scan(base + wave * (64 * kScan) + lane);
+#pragma unroll
+    for (int u = 0; u < kScan; u++) used += __popcll(__ballot(held[u] > 0));
+  }
+  if (lane == 0) wave_sum[wave] = used;
+  __syncthreads();
+  int n_used = 0;
+#pragma unroll
+  for (int w = 0; w < kMapWaves; w++) n_used += wave_sum[w];
   int holes = 0, high = 0;
-  for (int64_t base = 0; base < c.n_pages; base += kMapThreads) {
-    const int64_t p = base + tid;
-    const bool held = p < c.n_pages && c.ref[p] > 0;
-    const bool front = p < n_used, listed = p < c.n_pages && (front ? !held : held);
-    int all_h, all_u;
-    const int h = block_sum(listed && front, INT_MAX / 2, wave_sum, &all_h);
-    const int u = block_sum(listed && !front, INT_MAX / 2, wave_sum, &all_u);
-    if (listed && front) m.to[holes + h - 1] = (int32_t)p;
-    if (listed && !front) m.from[high + u - 1] = (int32_t)p;
-    if (p < c.n_pages && !front && !held) m.where[p] = -1;
-    holes += all_h;
-    high += all_u;
+  for (int64_t base = 0; base < c.n_pages; base += kMapThreads * kScan) {
+    const int64_t first = base + wave * (64 * kScan) + lane;
+    scan(first);
+    uint64_t hole[kScan], up[kScan];
+    int h = 0, p = 0;
+#pragma unroll
+    for (int u = 0; u < kScan; u++) {
+      const int64_t page = first + u * 64;
+      hole[u] = __ballot(page < n_used && held[u] <= 0);
+      up[u] = __ballot(page >= n_used && held[u] > 0);
+      h += __popcll(hole[u]);
+      p += __popcll(up[u]);
+    }
+    __syncthreads();
+    if (lane == 0) { wave_sum[wave] = h; wave_high[wave] = p; }
+    __syncthreads();
+    int kh = holes, kp = high;   // of the waves before
+#pragma unroll
+    for (int w = 0; w < kMapWaves; w++) {
+      if (w < wave) { kh += wave_sum[w]; kp += wave_high[w]; }
+      holes += wave_sum[w];
+      high += wave_high[w];
+    }
+    const uint64_t below = (uint64_t(1) << lane) - 1;
+#pragma unroll
+    for (int u = 0; u < kScan; u++) {
+      const int64_t page = first + u * 64;
+      if (page < c.n_pages) {
+        if (page < n_used) {
+          if (held[u] <= 0) m.to[kh + __popcll(hole[u] & below)] = (int32_t)page;
+        } else if (held[u] > 0) {
+          m.from[kp + __popcll(up[u] & below)] = (int32_t)page;
+        } else {
+          m.where[page] = -1;
+        }
+      }
+      kh += __popcll(hole[u]);
+      kp += __popcll(up[u]);
+    }
   }
   __syncthreads();
-  for (int k = tid; k < high; k += kMapThreads) m.where[m.from[k]] = m.to[k];
+  for (int k = tid; k < high; k += 4 * kMapThreads) {
+    int32_t from[4], to[4];
+#pragma unroll
+    for (int x = 0; x < 4; x++)
+      if (k + x * kMapThreads < high) { from[x] = m.from[k + x * kMapThreads]; to[x] = m.to[k + x * kMapThreads]; }
+#pragma unroll
+    for (int x = 0; x < 4; x++)
+      if (k + x * kMapThreads < high) m.where[from[x]] = to[x];
+  }
   if (tid == 0) {
     *m.count = high;
     counts[0] = n_used;
@@ -253,9 +341,9 @@ __global__ __launch_bounds__(kMapThreads) void list_moves_kernel(KCache c, Moves
   }
 }
 
-// The first n_seqs workgroups renumber a row of the table each; the others share (page, layer, k or v) among themselves.  No page, and no
-// count, is both read and written: those that move lie at or behind u, where they go before it.
-__global__ __launch_bounds__(256) void move_kernel(KCache c, Moves m, const int32_t* __restrict__ counts) {
+// The first n_seqs workgroups renumber a row of the table each; the others share (page, layer, piece, k or v) among themselves.  No page, and
+// no count, is both read and written: those that move lie at or behind u, where they go before it.  Bound by HBM.
+__global__ __launch_bounds__(256) void move_kernel(KCache c, Moves m, const int32_t* __restrict__ counts, int32_t pieces) {
   if ((int)blockIdx.x < c.n_seqs) {
     const int s = blockIdx.x, held = c.pages_of(c.length(s)), n_used = counts[0];
     int32_t* row = c.row(s);
@@ -268,16 +356,18 @@ __global__ __launch_bounds__(256) void move_kernel(KCache c, Moves m, const int3
     }
     return;
   }
-  const int64_t units = (int64_t)*m.count * c.n_layers * 2;
+  const int64_t per_page = 2 * (int64_t)c.n_layers * pieces, units = *m.count * per_page;
+  const int all = c.page.d * c.hkv << c.log_head_chunks;
   for (int64_t x = blockIdx.x - c.n_seqs; x < units; x += gridDim.x - c.n_seqs) {
-    const int64_t l = x >> 1, layer = l % c.n_layers;
-    const int from = m.from[l / c.n_layers], to = m.to[l / c.n_layers];
-    if (x % (2 * c.n_layers) == 0 && threadIdx.x == 0) {
+    const int64_t k = quot64(x, per_page), y = x - k * per_page, layer = quot64(y >> 1, pieces);
+    const int first = (int)((y >> 1) - layer * pieces) * kPieceChunks, last = min(first + kPieceChunks, all);
+    const int from = m.from[k], to = m.to[k];
+    if (y == 0 && threadIdx.x == 0) {
       c.ref[to] = c.ref[from];
       c.ref[from] = 0;
     }
-    if (x & 1) copy_tokens(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, from, to, 0, c.page.d);
-    else copy_tokens(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, from, to, 0, c.page.d);
+    if (y & 1) copy_chunks(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, from, to, first, last);
+    else copy_chunks(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, from, to, first, last);
   }
 }
 
@@ -287,33 +377,44 @@ struct NewTokens {
   int64_t n;
 };
 
-// A workgroup writes kAppendTokens tokens: their rows are found by a thread each, then all threads copy.
-static constexpr int kAppendTokens = 8;
+// A workgroup writes TOKENS tokens: their places in the cache are found by a thread each, then all threads copy, four chunks in flight.  HBM-bound
+// where there are many (83 396 tokens of 4 KiB 117 us, 5.8 TB/s read and written); few take a workgroup each and are bound by the trips
+// to memory: cu_new, seqs, seq_len, page_table, the tokens.
+static constexpr int kCuInLds = 1024;   // entries of cu_new that are searched in LDS
+template <int TOKENS>
 __global__ __launch_bounds__(256) void append_kernel(KCache c, int32_t layer, const int32_t* __restrict__ seqs, const int32_t* __restrict__ cu,
                                                      int32_t n, const int32_t* __restrict__ status, NewTokens x) {
-  __shared__ int32_t page_of[kAppendTokens], slot_of[kAppendTokens];
-  const int64_t t0 = (int64_t)blockIdx.x * kAppendTokens;
-  if (threadIdx.x < kAppendTokens) {
+  __shared__ int32_t page_of[TOKENS], slot_of[TOKENS], s_cu[kCuInLds];
+  const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
+  const bool in_lds = cu && n < kCuInLds;
+  if (in_lds) {
+    for (int y = threadIdx.x; y <= n; y += 256) s_cu[y] = cu[y];
+    __syncthreads();
+  }
+  if (threadIdx.x < TOKENS) {
     const int64_t t = t0 + threadIdx.x;
     int page = -1, slot = 0;
     int i = -1, behind = 0;   // the token's place, and the tokens of it from this one on
     if (t < x.n) {
       if (!cu) {
         if (t < n) { i = (int)t; behind = 1; }
-      } else if (t >= cu[0] && t < cu[n]) {
-        int lo = 0, hi = n - 1;   // the last place that begins at or before t
-        while (lo < hi) {
-          const int mid = (lo + hi + 1) >> 1;
-          if (cu[mid] <= t) lo = mid;
-          else hi = mid - 1;
+      } else {
+        auto at = [&](int y) { return in_lds ? s_cu[y] : cu[y]; };
+        if (t >= at(0) && t < at(n)) {
+          int lo = 0, hi = n - 1;   // the last place that begins at or before t
+          while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (at(mid) <= t) lo = mid;
+            else hi = mid - 1;
+          }
+          i = lo;
+          behind = (int)(at(lo + 1) - t);
         }
-        i = lo;
-        behind = (int)min((int64_t)INT_MAX, cu[lo + 1] - t);
       }
     }
-    if (i >= 0 && (!status || status[i] == DCP_PLACE_OK)) {
-      const int s = seqs ? seqs[i] : i;
-      if (c.is_seq(s)) {
+    if (i >= 0) {
+      const int s = seqs ? seqs[i] : i, st = status ? status[i] : DCP_PLACE_OK;
+      if (c.is_seq(s) && st == DCP_PLACE_OK) {
         const int pos = c.length(s) - behind;
         if (pos >= 0 && behind > 0) {
           const int p = c.page.quot(pos), entry = c.row(s)[p];
@@ -325,17 +426,30 @@ __global__ __launch_bounds__(256) void append_kernel(KCache c, int32_t layer, co
     slot_of[threadIdx.x] = slot;
   }
   __syncthreads();
-  const int per_token = c.hkv * c.head_chunks;
-  for (int y = threadIdx.x; y < 2 * kAppendTokens * per_token; y += 256) {
-    const int row = y / c.head_chunks, off = (y - row * c.head_chunks) * 16;   // row: (k or v, token, head)
-    const int tt = c.heads.quot(row), h = c.heads.rem(row, tt), t = tt & (kAppendTokens - 1);
-    const int page = page_of[t];
-    if (page < 0) continue;
-    const int64_t slot = slot_of[t];
-    if (tt < kAppendTokens)
-      store16(c.k + layer * c.k_sl + page * c.k_sp + slot * c.k_st + h * c.k_sh + off, load16(x.k + (t0 + t) * x.k_st + h * x.k_sh + off));
-    else
-      store16(c.v + layer * c.v_sl + page * c.v_sp + slot * c.v_st + h * c.v_sh + off, load16(x.v + (t0 + t) * x.v_st + h * x.v_sh + off));
+  const int all = TOKENS * c.hkv << c.log_head_chunks;   // chunks of k; as many of v
+  for (int y0 = threadIdx.x; y0 < all; y0 += 512) {
+    u32x4 kv[2][2];
+    char* to[2][2];
+#pragma unroll
+    for (int z = 0; z < 2; z++) {
+      const int y = y0 + 256 * z;
+      const int row = y >> c.log_head_chunks, off = (y & ((1 << c.log_head_chunks) - 1)) * 16;   // row: (token, head)
+      const int t = c.heads.quot(row), h = c.heads.rem(row, t);
+      to[z][0] = nullptr;
+      if (y < all && page_of[t] >= 0) {
+        const int64_t page = page_of[t], slot = slot_of[t];
+        to[z][0] = c.k + layer * c.k_sl + page * c.k_sp + slot * c.k_st + h * c.k_sh + off;
+        to[z][1] = c.v + layer * c.v_sl + page * c.v_sp + slot * c.v_st + h * c.v_sh + off;
+        kv[z][0] = load16(x.k + (t0 + t) * x.k_st + h * x.k_sh + off);
+        kv[z][1] = load16(x.v + (t0 + t) * x.v_st + h * x.v_sh + off);
+      }
+    }
+#pragma unroll
+    for (int z = 0; z < 2; z++)
+      if (to[z][0]) {
+        store16(to[z][0], kv[z][0]);
+        store16(to[z][1], kv[z][1]);
+      }
   }
 }
 
@@ -378,7 +492,7 @@ dcp_status_t pack_cache(const dcp_cache_t* cache, KCache* out) {
   k.ref = c.page_ref; k.table = c.page_table; k.len = c.seq_len;
   k.n_layers = c.n_layers; k.n_pages = c.n_pages; k.hkv = c.hkv; k.n_seqs = c.n_seqs; k.max_pages = c.max_pages;
   k.max_len = c.max_pages * c.page_size;
-  k.head_chunks = c.d * e / 16;
+  for (k.log_head_chunks = 2; (16 << k.log_head_chunks) < c.d * e; k.log_head_chunks++) {}
   k.page = fast_div((uint32_t)c.page_size);
   k.heads = fast_div((uint32_t)c.hkv);
   *out = k;
@@ -427,9 +541,10 @@ extern "C" dcp_status_t dcp_cache_append(const dcp_cache_t* cache, int32_t layer
   if ((st = check_rows("v_new", v_new, v_st, v_sh, cache->d)) != DCP_OK) return st;
   const int64_t e = cache->dtype == DCP_BF16 ? 2 : 4;
   const NewTokens x{(const char*)k_new, (const char*)v_new, k_st * e, k_sh * e, v_st * e, v_sh * e, n_tokens};
-  const int64_t wgs = (n_tokens + kAppendTokens - 1) / kAppendTokens;
   ProfScope ps(DCP_K_CACHE, (hipStream_t)stream);
-  hipLaunchKernelGGL(append_kernel, dim3((unsigned)wgs), dim3(256), 0, (hipStream_t)stream, c, layer, seqs, cu_new, n, status, x);
+  // up to four tokens a CU a workgroup each (64 tokens 6.4 -> 4.3 us), else eight in one
+  if (n_tokens <= 1024) hipLaunchKernelGGL(append_kernel<1>, dim3((unsigned)n_tokens), dim3(256), 0, (hipStream_t)stream, c, layer, seqs, cu_new, n, status, x);
+  else hipLaunchKernelGGL(append_kernel<8>, dim3((unsigned)((n_tokens + 7) / 8)), dim3(256), 0, (hipStream_t)stream, c, layer, seqs, cu_new, n, status, x);
   DCP_HIP_TRY(hipGetLastError());
   return DCP_OK;
 }
@@ -442,12 +557,13 @@ extern "C" dcp_status_t dcp_cache_fork(const dcp_cache_t* cache, const int32_t* 
   if ((st = check_places(c, src, n)) != DCP_OK) return st;
   if (n == 0) return DCP_OK;
   if (!src || !dst || !status || !aligned(dst, 4) || !aligned(status, 4)) return fail(DCP_ERR_INVALID_ARG, "src, dst or status is NULL or misaligned");
-  if (c.n_layers > 32767) return fail(DCP_ERR_UNSUPPORTED, "dcp_cache_fork covers at most 32 767 layers");
+  const int pieces = pieces_of(c);
   hipStream_t s = (hipStream_t)stream;
   ProfScope ps(DCP_K_CACHE, s);
   hipLaunchKernelGGL(take_kernel<true>, dim3(1), dim3(kMapThreads), 0, s, c, src, dst, n, status);
   DCP_HIP_TRY(hipGetLastError());
-  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)n, 1 + 2 * (unsigned)c.n_layers), dim3(256), 0, s, c, src, dst, status);
+  const int64_t units = n * (1 + 2 * (int64_t)c.n_layers * pieces);
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)std::min<int64_t>(units, kCopyWorkers)), dim3(256), 0, s, c, src, dst, n, status, pieces);
   DCP_HIP_TRY(hipGetLastError());
   return DCP_OK;
 }
@@ -482,8 +598,9 @@ extern "C" dcp_status_t dcp_cache_compact(const dcp_cache_t* cache, int32_t* cou
   ProfScope ps(DCP_K_CACHE, s);
   hipLaunchKernelGGL(list_moves_kernel, dim3(1), dim3(kMapThreads), 0, s, c, m, counts);
   DCP_HIP_TRY(hipGetLastError());
-  const int64_t most = (int64_t)(c.n_pages / 2 + 1) * c.n_layers * 2;
-  hipLaunchKernelGGL(move_kernel, dim3((unsigned)(c.n_seqs + std::min<int64_t>(most, 4096))), dim3(256), 0, s, c, m, counts);
+  const int pieces = pieces_of(c);
+  const int64_t most = std::min<int64_t>((c.n_pages / 2 + 1) * (2 * (int64_t)c.n_layers * pieces), kCopyWorkers);
+  hipLaunchKernelGGL(move_kernel, dim3((unsigned)(c.n_seqs + most)), dim3(256), 0, s, c, m, counts, pieces);
   DCP_HIP_TRY(hipGetLastError());
   return DCP_OK;
 }

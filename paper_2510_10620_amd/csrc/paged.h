@@ -31,9 +31,10 @@ struct KCache {
   int64_t k_sl, k_sp, k_st, k_sh, v_sl, v_sp, v_st, v_sh;
   int32_t *ref, *table, *len;
   int32_t n_layers, n_pages, hkv, n_seqs, max_pages, max_len;   // max_len: tokens that a row of the table has room for
-  int32_t head_chunks;   // 16-byte chunks of one token's head
+  int32_t log_head_chunks;   // log2 of the 16-byte chunks of one token's head
   FastDiv page, heads;
 
+  DCP_HD int32_t head_chunks() const { return 1 << log_head_chunks; }
   DCP_HD const int32_t* row(int32_t seq) const { return table + (int64_t)seq * max_pages; }
   DCP_HD int32_t* row(int32_t seq) { return table + (int64_t)seq * max_pages; }
   DCP_HD bool is_seq(int32_t seq) const { return (uint32_t)seq < (uint32_t)n_seqs; }

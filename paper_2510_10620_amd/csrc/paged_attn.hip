@@ -38,7 +38,10 @@ struct PagedParts {
 static constexpr int kWorkers = 512;
 static constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
 static constexpr int kSetHeads = 16;     // query heads of a matrix tile
-static constexpr int kLeastTiles = 4;    // of a worker
+static constexpr int kLeastTiles = 2;    // of a worker: one sequence of 4 096 tokens, 8 KV heads, 16.5 / 17.1 / 19.8 / 26.3 us with 1 / 2 / 4 / 8
+// Entries of the list up to which a join takes 1 024 threads a head: so few items may be in hundreds of parts (one sequence of 131 067
+// tokens 116 -> 101 us; one of 300 tokens 10.8 -> 11.5).
+static constexpr unsigned kWideJoins = 16;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -465,46 +468,61 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, 
   }
 }
 
-// Joins the parts of an item: workgroup (x, y) takes query head y of entry x of the list.
-template <typename T, int D>
-__global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(KCache c, PagedArgs a, PagedParts parts) {
-  constexpr int kLanes = D / 4, kRows = kPagedThreads / kLanes;
-  __shared__ float s_top[kPagedWaves], s_sum[kRows], s_o[kRows][D + 4];
+// Joins the parts of an item: workgroup (x, y) takes HEADS query heads of entry x of the list.  D / 4 lanes walk every kRows-th part of a
+// head, with a maximum of their own, and meet in LDS.  Bound by latency: three dependent trips to memory where an item has few parts.
+template <typename T, int D, int THREADS, int HEADS>
+__global__ __launch_bounds__(THREADS) void paged_join_kernel(KCache c, PagedArgs a, PagedParts parts) {
+  constexpr int kLanes = D / 4, kRows = THREADS / kLanes / HEADS;
+  __shared__ float s_m[HEADS][kRows], s_l[HEADS][kRows], s_o[HEADS][kRows][D];
   const int tid = threadIdx.x;
   const int4 job = parts.joins[blockIdx.x];
   if (job.x < 0) return;
-  const int beside = blockIdx.y / a.set_heads, h = blockIdx.y - beside * a.set_heads, set = job.y * a.abreast + beside;
+  const int hw = tid / (kLanes * kRows), r = tid / kLanes % kRows, d = tid % kLanes * 4;
+  const int y = blockIdx.y * HEADS + hw, beside = y / a.set_heads, h = y - beside * a.set_heads, set = job.y * a.abreast + beside;
   const int hk = set / a.per_kv, h0 = hk * a.group + (set - hk * a.per_kv) * kSetHeads;
-  if (h0 + h >= (hk + 1) * a.group) return;
-  const int w = job.z, n = job.w - w + 1;   // parts: slot 2 w + 1, then 2 v of the later workers v
-  auto slot = [&](int p) { return ((p == 0 ? 2 * w + 1 : 2 * (w + p)) * a.abreast + beside) * a.set_heads + h; };
-  float top = -INFINITY;
-  for (int p = tid; p < n; p += kPagedThreads) top = fmaxf(top, parts.ml[slot(p)].x);
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-  if ((tid & 63) == 0) s_top[tid >> 6] = top;
-  __syncthreads();
-#pragma unroll
-  for (int v = 0; v < kPagedWaves; v++) top = fmaxf(top, s_top[v]);
-  const float zero = top == -INFINITY ? 0.f : top;
-  const int r = tid / kLanes, d = (tid - r * kLanes) * 4;
+  const bool real = beside < a.abreast && h0 + h < (hk + 1) * a.group;
+  const int w = job.z, n = real ? job.w - w + 1 : 0;   // parts: slot 2 w + 1, then 2 v of the later workers v
+  float m = -INFINITY, l = 0;
   f32x4 o = {0, 0, 0, 0};
-  float sum = 0;
-#pragma unroll 4
-  for (int p = r; p < n; p += kRows) {
-    const float2 ml = parts.ml[slot(p)];
-    const float f = __builtin_amdgcn_exp2f(ml.x - zero);
-    sum += f * ml.y;
-    o += f * *(const f32x4*)&parts.o[(int64_t)slot(p) * D + d];
-  }
-  if (d == 0) s_sum[r] = sum;
-  *(f32x4*)&s_o[r][d] = o;
-  __syncthreads();
-  if (r) return;
+  constexpr int kAhead = 4;   // parts of a lane in flight
+  for (int p0 = r; p0 < n; p0 += kAhead * kRows) {
+    float2 ml[kAhead];
+    f32x4 part[kAhead];
 #pragma unroll
-  for (int x = 1; x < kRows; x++) {
-    sum += s_sum[x];
-    o += *(const f32x4*)&s_o[x][d];
+    for (int x = 0; x < kAhead; x++) {
+      const int p = p0 + x * kRows;
+      const int64_t slot = ((int64_t)(p == 0 ? 2 * w + 1 : 2 * (w + p)) * a.abreast + beside) * a.set_heads + h;
+      ml[x] = make_float2(-INFINITY, 0.f);
+      part[x] = f32x4{0, 0, 0, 0};
+      if (p < n) {
+        ml[x] = parts.ml[slot];
+        part[x] = *(const f32x4*)&parts.o[slot * D + d];
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < kAhead; x++) {
+      const float m2 = fmaxf(m, ml[x].x), zero = m2 == -INFINITY ? 0.f : m2;
+      const float f = __builtin_amdgcn_exp2f(m - zero), fx = __builtin_amdgcn_exp2f(ml[x].x - zero);
+      l = l * f + ml[x].y * fx;
+      o = o * f + part[x] * fx;
+      m = m2;
+    }
+  }
+  if (d == 0) { s_m[hw][r] = m; s_l[hw][r] = l; }
+  *(f32x4*)&s_o[hw][r][d] = o;
+  __syncthreads();
+  if (r || !real) return;
+  float top = m, sum = 0;
+#pragma unroll
+  for (int x = 1; x < kRows; x++) top = fmaxf(top, s_m[hw][x]);
+  const float zero = top == -INFINITY ? 0.f : top;
+  o = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int x = 0; x < kRows; x++) {
+    if (x >= n) continue;
+    const float f = __builtin_amdgcn_exp2f(s_m[hw][x] - zero);
+    sum += s_l[hw][x] * f;
+    o += f * *(const f32x4*)&s_o[hw][x][d];
   }
   float res[4];
 #pragma unroll
@@ -522,8 +540,9 @@ template <typename T, int D, int COLS>
 static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
   if (a.per_kv == 1) launch_once<T, D, COLS, true>(c, a, parts, s);
   else if constexpr (COLS == kSetHeads) launch_once<T, D, COLS, false>(c, a, parts, s);   // more sets than one are full ones
-  const int entries = parts.by_item ? a.n * a.groups : kWorkers;
-  hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3((unsigned)entries, (unsigned)(a.abreast * a.set_heads)), dim3(kPagedThreads), 0, s, c, a, parts);
+  const unsigned entries = parts.by_item ? a.n * a.groups : kWorkers, heads = a.abreast * a.set_heads;
+  if (entries <= kWideJoins) hipLaunchKernelGGL((paged_join_kernel<T, D, 1024, 1>), dim3(entries, heads), dim3(1024), 0, s, c, a, parts);
+  else hipLaunchKernelGGL((paged_join_kernel<T, D, 256, 4>), dim3(entries, (heads + 3) / 4), dim3(256), 0, s, c, a, parts);
 }
 template <typename T, int COLS>
 static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts, int d, hipStream_t s) {
