@@ -39,9 +39,9 @@ static constexpr int kWorkers = 512;
 static constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
 static constexpr int kSetHeads = 16;     // query heads of a matrix tile
 static constexpr int kLeastTiles = 2;    // of a worker: one sequence of 4 096 tokens, 8 KV heads, 16.5 / 17.1 / 19.8 / 26.3 us with 1 / 2 / 4 / 8
-// Entries of the list up to which a join takes 1 024 threads a head: so few items may be in hundreds of parts (one sequence of 131 067
-// tokens 116 -> 101 us; one of 300 tokens 10.8 -> 11.5).
-static constexpr unsigned kWideJoins = 16;
+// Of few items each is in many parts, which a join takes with more threads a head: up to kWideJoins entries of the list 1 024, up to
+// kMiddleJoins 256, else 64 (one sequence of 131 067 tokens, 2 entries, 101 / - / 116 us; 16 of 1 to 4 096, 16 entries, 22.6 / - / 22.0).
+static constexpr unsigned kWideJoins = 7, kMiddleJoins = 31;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -542,6 +542,7 @@ static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts,
   else if constexpr (COLS == kSetHeads) launch_once<T, D, COLS, false>(c, a, parts, s);   // more sets than one are full ones
   const unsigned entries = parts.by_item ? a.n * a.groups : kWorkers, heads = a.abreast * a.set_heads;
   if (entries <= kWideJoins) hipLaunchKernelGGL((paged_join_kernel<T, D, 1024, 1>), dim3(entries, heads), dim3(1024), 0, s, c, a, parts);
+  else if (entries <= kMiddleJoins) hipLaunchKernelGGL((paged_join_kernel<T, D, 256, 1>), dim3(entries, heads), dim3(256), 0, s, c, a, parts);
   else hipLaunchKernelGGL((paged_join_kernel<T, D, 256, 4>), dim3(entries, (heads + 3) / 4), dim3(256), 0, s, c, a, parts);
 }
 template <typename T, int COLS>
