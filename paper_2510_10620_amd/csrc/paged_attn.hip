@@ -56,7 +56,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // the maximum over a tile's keys.
 template <typename T, int D> struct Tile;
 
-// Keys and values are read once, so they go past the caches (ONCE), unless several sets of heads read them.
+// Keys and values are read once, so they go past the caches (ONCE: 32 places of 512 to 8 192 tokens 78 -> 73 us), unless several sets of heads
+// read them, or a head's row is half a line of the caches whose other half the wave beside reads (bf16 with D = 32: 53 -> 50).
 template <bool ONCE, typename V> __device__ __forceinline__ V load_kv(const char* p) {
   if constexpr (ONCE) return __builtin_nontemporal_load((const V*)p);
   else return *(const V*)p;
@@ -538,7 +539,8 @@ static void launch_once(const KCache& c, const PagedArgs& a, const PagedParts& p
 }
 template <typename T, int D, int COLS>
 static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
-  if (a.per_kv == 1) launch_once<T, D, COLS, true>(c, a, parts, s);
+  if constexpr (D * sizeof(T) < 128) launch_once<T, D, COLS, false>(c, a, parts, s);
+  else if (a.per_kv == 1) launch_once<T, D, COLS, true>(c, a, parts, s);
   else if constexpr (COLS == kSetHeads) launch_once<T, D, COLS, false>(c, a, parts, s);   // more sets than one are full ones
   const unsigned entries = parts.by_item ? a.n * a.groups : kWorkers, heads = a.abreast * a.set_heads;
   if (entries <= kWideJoins) hipLaunchKernelGGL((paged_join_kernel<T, D, 1024, 1>), dim3(entries, heads), dim3(1024), 0, s, c, a, parts);
