@@ -74,10 +74,9 @@ struct Shares {
     return t < longer ? (int32_t)quot64(t, each + 1) : more + (int32_t)quot64(t - longer, each);
   }
 };
-DCP_HD Shares make_shares(int64_t total, int32_t most_workers, int32_t least_tiles) {
-  const int64_t w = (total + least_tiles - 1) / least_tiles;
+DCP_HD Shares make_shares(int64_t total, int32_t most_workers) {
   Shares s;
-  s.workers = (int32_t)(w < most_workers ? w : most_workers);
+  s.workers = (int32_t)(total < most_workers ? total : most_workers);
   s.each = quot64(total, s.workers);
   s.more = (int32_t)(total - s.each * s.workers);
   return s;

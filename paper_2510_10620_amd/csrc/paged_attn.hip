@@ -19,6 +19,7 @@ struct PagedArgs {
   // Query heads that share a KV head are taken in sets of up to 16 (or 8, see Tile::weigh); a workgroup's waves take `abreast` (1, 2 or 4) sets
   // that lie side by side, and where there are fewer than four, the waves of a set take its tiles in turn.
   int32_t per_kv, set_heads, abreast, log_abreast, groups;   // sets of a KV head, heads of a set at most, ..., sets / abreast
+  int32_t whole;   // items are not cut: nothing to join
   float scale_log2e;
 };
 
@@ -38,7 +39,12 @@ struct PagedParts {
 static constexpr int kWorkers = 512;
 static constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
 static constexpr int kSetHeads = 16;     // query heads of a matrix tile
-static constexpr int kLeastTiles = 2;    // of a worker: one sequence of 4 096 tokens, 8 KV heads, 16.5 / 17.1 / 19.8 / 26.3 us with 1 / 2 / 4 / 8
+// Items are taken whole, so that nothing is to be joined, where a workgroup each is enough and none can have more than that many tiles a wave:
+// short sequences (or windows) in a table that has no room for more.  Whole and cut, us: one sequence of 30 tokens, 8 KV heads 7.5 and 13.6, of
+// 300 tokens 12.6 and 12.8; 64 of 90 13.6 and 20.1, of 380 27.5 and 29.0; 16 of 380, 2 KV heads 15.4 and 13.4; with one more
+// round 16 of 500 18.9 and 16.7.
+static constexpr int kWholeRounds = 3;
+
 // Of few items each is in many parts, which a join takes with more threads a head: up to kWideJoins entries of the list 1 024, up to
 // kMiddleJoins 256, else 64 (one sequence of 131 067 tokens, 2 entries, 101 / - / 116 us; 16 of 1 to 4 096, 16 entries, 22.6 / - / 22.0).
 static constexpr unsigned kWideJoins = 7, kMiddleJoins = 31;
@@ -282,7 +288,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, 
   int64_t mine = 0;
   for (int x = tid * per; x < min(a.n, (tid + 1) * per); x++) {
     const int seq = seq_at(a, x), len = c.is_seq(seq) ? c.length(seq) : 0;
-    if (c.is_seq(seq)) mine += KeyTiles(len, a.window, a.sink, TT::kKeys).count;
+    if (c.is_seq(seq)) mine += a.whole ? 1 : KeyTiles(len, a.window, a.sink, TT::kKeys).count;
     s_seq[tid] = seq;   // of use where a thread has one place
     s_len[tid] = len;
   }
@@ -301,9 +307,9 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, 
     all += s_wave[y];
   }
   // nothing to join, unless the worker that begins an item says so
-  if (tid == 0 && (!parts.by_item || w >= a.n * a.groups || !c.is_seq(seq_at(a, w / a.groups)))) parts.joins[w] = make_int4(-1, 0, 0, 0);
+  if (tid == 0 && !a.whole && (!parts.by_item || w >= a.n * a.groups || !c.is_seq(seq_at(a, w / a.groups)))) parts.joins[w] = make_int4(-1, 0, 0, 0);
   if (all == 0) return;
-  const Shares sh = make_shares(all * a.groups, kWorkers, kLeastTiles);
+  const Shares sh = make_shares(all * a.groups, kWorkers);
   if (w >= sh.workers) return;
   int64_t at = sh.start(w);
   const int64_t end = sh.start(w + 1);
@@ -322,11 +328,12 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, 
     const int seq = per == 1 ? s_seq[place] : seq_at(a, place);
     if (!c.is_seq(seq)) { place++; continue; }
     const KeyTiles keys(per == 1 ? s_len[place] : c.length(seq), a.window, a.sink, TT::kKeys);
+    const int units = a.whole ? 1 : keys.count;   // of an item
     const int64_t rel = at - before * a.groups;
-    if (rel >= (int64_t)keys.count * a.groups) { before += keys.count; place++; continue; }
+    if (rel >= (int64_t)units * a.groups) { before += units; place++; continue; }
     const int32_t* row = c.row(seq);
-    const int grp = (int)quot64(rel, keys.count), t0 = (int)(rel - (int64_t)grp * keys.count);
-    const int t1 = (int)min((int64_t)keys.count, t0 + (end - at));
+    const int grp = (int)quot64(rel, units), t0 = (int)(rel - (int64_t)grp * units);
+    const int t1 = a.whole ? keys.count : (int)min((int64_t)keys.count, t0 + (end - at));
     const int set = grp * abreast + (wave & (abreast - 1)), hk = a.per_kv == 1 ? set : set / a.per_kv;
     const int h0 = hk * a.group + (set - hk * a.per_kv) * kSetHeads, n_heads = min(kSetHeads, (hk + 1) * a.group - h0);
     const int col = COLS == 8 ? i & 7 : i;
@@ -460,12 +467,12 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, 
         }
       }
     }
-    if (t0 == 0 && tid == 0) {
+    if (t0 == 0 && tid == 0 && !a.whole) {
       const int last = t1 == keys.count ? w : sh.worker_of(before * a.groups + (int64_t)(grp + 1) * keys.count - 1);
       if (parts.by_item) parts.joins[place * a.groups + grp] = make_int4(last == w ? -1 : place, grp, w, last);
       else if (last != w) parts.joins[w] = make_int4(place, grp, w, last);
     }
-    at += t1 - t0;
+    at += a.whole ? 1 : t1 - t0;
   }
 }
 
@@ -542,6 +549,7 @@ static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts,
   if constexpr (D * sizeof(T) < 128) launch_once<T, D, COLS, false>(c, a, parts, s);
   else if (a.per_kv == 1) launch_once<T, D, COLS, true>(c, a, parts, s);
   else if constexpr (COLS == kSetHeads) launch_once<T, D, COLS, false>(c, a, parts, s);   // more sets than one are full ones
+  if (a.whole) return;
   const unsigned entries = parts.by_item ? a.n * a.groups : kWorkers, heads = a.abreast * a.set_heads;
   if (entries <= kWideJoins) hipLaunchKernelGGL((paged_join_kernel<T, D, 1024, 1>), dim3(entries, heads), dim3(1024), 0, s, c, a, parts);
   else if (entries <= kMiddleJoins) hipLaunchKernelGGL((paged_join_kernel<T, D, 256, 1>), dim3(entries, heads), dim3(256), 0, s, c, a, parts);
@@ -560,13 +568,14 @@ struct Sets {
   int64_t groups;
   size_t bytes;   // of the workspace
 };
-static Sets sets_of(int32_t hkv, int32_t hq, int32_t d) {
+static Sets sets_of(int32_t hkv, int32_t hq, int32_t d, int most_abreast) {
   const int32_t group = hq / hkv;
   Sets s;
   s.per_kv = (group + kSetHeads - 1) / kSetHeads;
   s.heads = std::min(group, kSetHeads);
   const int64_t sets = (int64_t)hkv * s.per_kv;
-  s.log_abreast = sets % 4 == 0 ? 2 : sets % 2 == 0 ? 1 : 0;
+  s.log_abreast = 0;
+  while (2 << s.log_abreast <= most_abreast && sets % (2 << s.log_abreast) == 0) s.log_abreast++;
   s.abreast = 1 << s.log_abreast;
   s.groups = sets / s.abreast;
   s.bytes = kWorkers * (sizeof(int4) + 2 * (size_t)s.abreast * s.heads * (sizeof(float2) + d * sizeof(float)));
@@ -577,7 +586,7 @@ static Sets sets_of(int32_t hkv, int32_t hq, int32_t d) {
 
 extern "C" size_t dcp_paged_attn_workspace_bytes(const dcp_cache_t* cache, int32_t n, int32_t hq) {
   if (!cache || n <= 0 || hq <= 0 || cache->hkv <= 0 || cache->d <= 0) return 0;
-  return hq % cache->hkv ? 0 : sets_of(cache->hkv, hq, cache->d).bytes;
+  return hq % cache->hkv ? 0 : sets_of(cache->hkv, hq, cache->d, kPagedWaves).bytes;
 }
 
 extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t* args, void* workspace, size_t workspace_bytes,
@@ -607,10 +616,19 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
     const char* o1 = o0 + ((t.n - 1) * t.o_stride_t + (t.hq - 1) * t.o_stride_h + cache->d) * e;
     if (q0 < o1 && o0 < q1) return fail(DCP_ERR_INVALID_ARG, "out overlaps q");
   }
-  const Sets sets = sets_of(c.hkv, t.hq, cache->d);
+  // Whole items: the most tiles that one can have, as far as the host knows, over the waves that take them in turn
+  const int tile = cache->dtype == DCP_F32 ? 16 : 32;
+  const int64_t most = ((t.window > 0 ? std::min<int64_t>(c.max_len, (int64_t)t.window + t.sink + 2 * tile) : c.max_len) + tile - 1) / tile;
+  Sets sets = sets_of(c.hkv, t.hq, cache->d, kPagedWaves);
+  bool whole = false;
+  for (int abreast = 1; abreast <= sets.abreast && !whole; abreast *= 2) {
+    const Sets x = sets_of(c.hkv, t.hq, cache->d, abreast);
+    whole = t.n * x.groups <= kWorkers && most <= kWholeRounds * (kPagedWaves / x.abreast);
+    if (whole) sets = x;
+  }
   if (sets.groups * sets.abreast > (1 << 12)) return fail(DCP_ERR_UNSUPPORTED, "dcp_paged_attn_fwd covers at most 4 096 sets of 16 query heads on one KV head");
   const PagedArgs a{(const char*)t.q, (char*)t.out, t.lse, t.seqs, t.q_stride_t * e, t.q_stride_h * e, t.o_stride_t * e, t.o_stride_h * e,
-                    t.n, t.hq, t.hq / c.hkv, t.layer, t.window, t.sink, sets.per_kv, sets.heads, sets.abreast, sets.log_abreast, (int32_t)sets.groups,
+                    t.n, t.hq, t.hq / c.hkv, t.layer, t.window, t.sink, sets.per_kv, sets.heads, sets.abreast, sets.log_abreast, (int32_t)sets.groups, whole,
                     t.softmax_scale * 1.44269504088896340736f};
   PagedParts parts;
   parts.joins = (int4*)workspace;

@@ -64,7 +64,7 @@ int main() {
     int64_t total = 0;
     for (int64_t x : items) total += x;
     const int most = (int)uni(1, 700);
-    const Shares s = make_shares(total, most, (int)uni(1, 8));
+    const Shares s = make_shares(total, most);
     CHECK(s.workers >= 1 && s.workers <= most && s.start(0) == 0 && s.start(s.workers) == total);
     std::map<int, int> slots;   // slot -> item
     int64_t begin = 0;
@@ -83,7 +83,7 @@ int main() {
     for (int w = 0; w < s.workers; w++) CHECK(s.start(w + 1) - s.start(w) >= 1 && s.start(w + 1) - s.start(w) <= total / s.workers + 1);
   }
   // the largest batch: 16 384 places of 2^30 tokens (2^26 tiles), 4 096 sets
-  const Shares s = make_shares(int64_t(1) << (14 + 26 + 12), 1000, 4);
+  const Shares s = make_shares(int64_t(1) << (14 + 26 + 12), 1000);
   CHECK(s.start(s.workers) == int64_t(1) << 52 && s.worker_of((int64_t(1) << 52) - 1) == s.workers - 1);
   std::printf("host-paged ok\n");
 }

@@ -136,8 +136,10 @@ def test_lengths_and_pages(dtype, d, page):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 3), (2, 1), (4, 1), (6, 2), (7, 1), (8, 1), (9, 1), (16, 1), (17, 1), (40, 1), (64, 2), (48, 16)])
-def test_heads(dtype, hq, hkv):
-    cache, names = make_cache([5, 300, 64], 16, hkv, 64, dtype, seed=hq)
+@pytest.mark.parametrize("width", [None, 500])
+def test_heads(dtype, hq, hkv, width):
+    """width 500: a table with room for long sequences, whose items may be cut."""
+    cache, names = make_cache([5, 300, 64], 16, hkv, 64, dtype, seed=hq, width=width)
     q = randn((3, hq, 64), dtype, 2)
     out, lse = attend(cache, q, 0.125, ints(names))
     check(cache, q, out, lse, 0.125, [int(s) for s in names])
@@ -248,6 +250,23 @@ def test_inf_and_nan_reach_who_sees_them(dtype, d):
     q2[3, 2:, 0] = 1.0
     out, lse = attend(cache, q2, 0.1, ints(names))
     assert (out[3, 2:] == 0).all() and (lse[2:, 3] == -float("inf")).all()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 32), ("f32", 64)])
+@pytest.mark.parametrize("n", [1, 3, 64, 150, 600])
+def test_short_sequences_taken_whole_or_cut(dtype, d, n):
+    """Up to 90 tokens in a table without room for more (a workgroup an item, or several items one after the other), and in one with."""
+    rng = np.random.default_rng(n)
+    lens = [int(x) for x in rng.integers(0, 91, n)]
+    lens[0] = 90
+    for width in (None, 300):
+        cache, names = make_cache(lens, 16, 4, d, dtype, seed=n, width=width)
+        places = [int(s) for s in names] + [-1]
+        q = randn((len(places), 8, d), dtype, 70)
+        out, lse = attend(cache, q, d ** -0.5, ints(places))
+        check(cache, q, out, lse, d ** -0.5, places)
+        out, lse = attend(cache, q, d ** -0.5, ints(places), 20, 3)
+        check(cache, q, out, lse, d ** -0.5, places, 20, 3)
 
 
 def test_many_places_and_one_long_sequence():
@@ -639,6 +658,38 @@ def test_on_a_stream_of_its_own_and_two_at_once():
     torch.cuda.synchronize()
     for i in range(2):
         check(cache, q[i], outs[i], lses[i], 0.1, [int(s) for s in names])
+
+
+def test_two_graphs_share_a_workspace():
+    """Calls of other sizes captured into two graphs over one workspace, replayed in turn with eager calls between them."""
+    import torch
+    cases = []
+    ws = None
+    for lens, hq in (([3000, 100, 17], 8), ([50, 700], 4)):
+        cache, names = make_cache(lens, 16, 2, 64, seed=hq, width=300)
+        q = randn((len(lens), hq, 64), "bf16", 71)
+        out, lse = attend(cache, q, 0.1, ints(names))
+        need = P.dcp_paged_attn_workspace_bytes(cache, len(lens), hq)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda").random_() if ws is None or ws.numel() < need else ws
+        cases.append([cache, q, torch.full_like(out, NAN), torch.full_like(lse, NAN), ints(names), out, lse])
+    graphs = []
+    for cache, q, out, lse, seqs, _, _ in cases:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            P.dcp_paged_attn_fwd(cache, q, out, lse, 0.1, ws, seqs=seqs)
+        graphs.append(g)
+    for _ in range(3):
+        for g, (cache, q, out, lse, seqs, want, want_l) in zip(graphs, cases):
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want) and torch.equal(lse, want_l)
+            out.fill_(NAN)
+            lse.fill_(NAN)
+            ws.random_()
+            P.dcp_paged_attn_fwd(cache, q, out, lse, 0.1, ws, seqs=seqs)
+            torch.cuda.synchronize()
+            assert torch.equal(out, want) and torch.equal(lse, want_l)
+            out.fill_(NAN)
 
 
 def test_the_same_call_gives_the_same_bits():
