@@ -472,7 +472,8 @@ class Cache:
         if not k.is_cuda:
             raise ValueError("k: device tensor required")
         self.k, self.v, self.page_ref, self.page_table, self.seq_len = k, v, page_ref, page_table, seq_len
-        self.device, self._index, self._dtype, self._heads, self._i32, self._f32 = k.device, k.device.index, k.dtype, k.shape[3:], torch.int32, torch.float32
+        self.device, self._index, self._dtype, self._i32, self._f32 = k.device, k.get_device(), k.dtype, torch.int32, torch.float32
+        self._hkv, self._d = k.shape[3:]
         # the current stream as a number; torch.cuda.current_stream builds an object, which takes longer than a launch
         self._raw_stream, self._raw_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         self._lib = _lib.load()
@@ -480,7 +481,9 @@ class Cache:
         d.n_layers, d.n_pages, d.page_size, d.hkv, d.d = k.shape
         d.dtype, d.n_seqs, d.max_pages = _dtype_code(k), page_table.shape[0], page_table.shape[1]
         for name, t in (("k", k), ("v", v)):
-            setattr(d, name, self._rows(name, t))
+            if t.get_device() != self._index or t.stride(-1) != 1:
+                raise ValueError(f"{name}: tensor with contiguous last dim on one device required")
+            setattr(d, name, t.data_ptr())
             for axis, letter in enumerate("lpth"):
                 # a dimension of one element has no stride of its own
                 setattr(d, f"{name}_stride_{letter}", t.stride(axis) if t.shape[axis] > 1 else max(8, t.shape[4]))
@@ -496,20 +499,24 @@ class Cache:
         zeros = [torch.zeros(n, dtype=torch.int32, device=device) for n in (pages, seqs)]
         return cls(*kv, zeros[0], torch.full((seqs, max_pages), -1, dtype=torch.int32, device=device), zeros[1])
 
-    def _rows(self, name, t):
-        if t.dtype != self._dtype or t.stride(-1) != 1 or t.device != self.device:
-            raise ValueError(f"{name}: tensor of the cache's dtype with contiguous last dim on its device required")
-        return t.data_ptr()
-
+    # The checks below run once per tensor and call: they are written for a call that is shorter than its launch.
     def _ints(self, name, t, n):
         if t is None:
             return None
-        if t.dtype != self._i32 or t.numel() != n or not t.is_contiguous() or t.device != self.device:
-            raise ValueError(f"{name}: contiguous int32 tensor of {n} elements on the cache's device required")
-        return t.data_ptr()
+        if t.dtype is self._i32 and t.numel() == n and t.is_contiguous() and t.get_device() == self._index:
+            return t.data_ptr()
+        raise ValueError(f"{name}: contiguous int32 tensor of {n} elements on the cache's device required")
+
+    def _token_rows(self, name, t):
+        """[tokens, heads, d] of the cache's dtype: (address, token stride, head stride); a dimension of one element has no stride of its own."""
+        n, h, d = t.shape
+        st, sh, one = t.stride()
+        if t.dtype is self._dtype and one == 1 and t.get_device() == self._index:
+            return t.data_ptr(), st if n > 1 else max(8, d), sh if h > 1 else max(8, d)
+        raise ValueError(f"{name}: tensor of the cache's dtype with contiguous last dim on its device required")
 
     def _space(self, workspace):
-        if workspace.device != self.device or not workspace.is_contiguous():
+        if workspace.get_device() != self._index or not workspace.is_contiguous():
             raise ValueError("workspace: contiguous tensor on the cache's device required")
         return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
@@ -517,12 +524,6 @@ class Cache:
         if self._raw_device() != self._index:
             raise ValueError(f"the cache lies on {self.device}, which is not the current device")
         return self._raw_stream(self._index)
-
-    def _token_rows(self, name, t):
-        """[tokens, heads, d]: (address, token stride, head stride); a dimension of one element has no stride of its own."""
-        n, h, d = t.shape
-        st, sh, _ = t.stride()
-        return self._rows(name, t), st if n > 1 else max(8, d), sh if h > 1 else max(8, d)
 
 
 def dcp_cache_reserve(cache, seqs, status, n_new=None):
@@ -534,12 +535,10 @@ def dcp_cache_reserve(cache, seqs, status, n_new=None):
 
 def dcp_cache_append(cache, k_new, v_new, seqs=None, cu_new=None, status=None, layer=0):
     """k_new, v_new [tokens, hkv, d] go to the last places of the sequences: place i has rows [cu_new[i], cu_new[i + 1]), or row i."""
-    tokens = k_new.shape[0]
-    n = cu_new.numel() - 1 if cu_new is not None else tokens if seqs is None else seqs.numel()
-    if k_new.dim() != 3 or k_new.shape != v_new.shape or k_new.shape[1:] != cache._heads:
+    tokens, hkv, d = k_new.shape
+    if hkv != cache._hkv or d != cache._d or v_new.shape != k_new.shape:
         raise ValueError("k_new, v_new: [tokens, hkv, d] with the cache's hkv and d")
-    if cu_new is None and tokens != n:
-        raise ValueError("without cu_new there is one token per place")
+    n = cu_new.numel() - 1 if cu_new is not None else tokens
     _check(cache._lib.dcp_cache_append(cache.ref, layer, cache._ints("seqs", seqs, n), cache._ints("cu_new", cu_new, n + 1), n,
                                        cache._ints("status", status, n), *cache._token_rows("k_new", k_new), *cache._token_rows("v_new", v_new),
                                        tokens, cache._stream()))
@@ -573,9 +572,9 @@ def dcp_paged_attn_workspace_bytes(cache, n, hq):
 def dcp_paged_attn_fwd(cache, q, out, lse, softmax_scale, workspace, seqs=None, window=0, sink=0, layer=0):
     """q, out [n, hq, d], lse float [hq, n]: one new token of each place over its sequence."""
     n, hq, d = q.shape
-    if out.shape != q.shape or d != cache._heads[1]:
+    if out.shape != q.shape or d != cache._d:
         raise ValueError("q, out: [n, hq, d] with the cache's d")
-    if lse.dtype != cache._f32 or lse.shape != (hq, n) or not lse.is_contiguous() or lse.device != cache.device:
+    if lse.dtype is not cache._f32 or lse.shape != (hq, n) or not lse.is_contiguous() or lse.get_device() != cache._index:
         raise ValueError("lse: contiguous float32 tensor [hq, n] on the cache's device")
     args = _lib.PagedAttn(n, hq, layer, softmax_scale, window, sink, cache._ints("seqs", seqs, n), *cache._token_rows("q", q),
                           *cache._token_rows("out", out), lse.data_ptr())

@@ -39,11 +39,12 @@ struct PagedParts {
 static constexpr int kWorkers = 512;
 static constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
 static constexpr int kSetHeads = 16;     // query heads of a matrix tile
-// Items are taken whole, so that nothing is to be joined, where a workgroup each is enough and none can have more than that many tiles a wave:
+// Items are taken whole, so that nothing is to be joined, where a workgroup each is enough and none can have more than so many tiles a wave:
 // short sequences (or windows) in a table that has no room for more.  Whole and cut, us: one sequence of 30 tokens, 8 KV heads 7.5 and 13.6, of
 // 300 tokens 12.6 and 12.8; 64 of 90 13.6 and 20.1, of 380 27.5 and 29.0; 16 of 380, 2 KV heads 15.4 and 13.4; with one more
-// round 16 of 500 18.9 and 16.7.
-static constexpr int kWholeRounds = 3;
+// round 16 of 500 18.9 and 16.7.  Where they nearly fill the chip, cutting gains little and costs the joins and a start in the middle: 200 of 150
+// tokens, 8 KV heads 33 and 42, 256 of 1 to 200 34 and 41, of 200 44 and 46, 64 of 1 to 700 36.5 and 34; with 160 items fewer 40 of 1 to 700 33 and 27.
+static constexpr int kWholeRounds = 3, kWholeRoundsFull = 8, kFullItems = kWorkers * 3 / 4;
 
 // Of few items each is in many parts, which a join takes with more threads a head: up to kWideJoins entries of the list 1 024, up to
 // kMiddleJoins 256, else 64 (one sequence of 131 067 tokens, 2 entries, 101 / - / 116 us; 16 of 1 to 4 096, 16 entries, 22.6 / - / 22.0).
@@ -623,7 +624,7 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
   bool whole = false;
   for (int abreast = 1; abreast <= sets.abreast && !whole; abreast *= 2) {
     const Sets x = sets_of(c.hkv, t.hq, cache->d, abreast);
-    whole = t.n * x.groups <= kWorkers && most <= kWholeRounds * (kPagedWaves / x.abreast);
+    whole = t.n * x.groups <= kWorkers && most <= (t.n * x.groups > kFullItems ? kWholeRoundsFull : kWholeRounds) * (kPagedWaves / x.abreast);
     if (whole) sets = x;
   }
   if (sets.groups * sets.abreast > (1 << 12)) return fail(DCP_ERR_UNSUPPORTED, "dcp_paged_attn_fwd covers at most 4 096 sets of 16 query heads on one KV head");
