@@ -465,9 +465,11 @@ dcp_status_t dcp_cache_compact(const dcp_cache_t* cache, int32_t* counts, void* 
 /* Attention of one new token per place over its sequence: the query is the token at position seq_len - 1 (appended already) and
  * sees key j iff j < seq_len and, with window > 0, seq_len - 1 - j < window or j < sink (the predicate of WINDOW rows; window 0: no
  * window).  Keys in pages that do not exist are not seen.  Out and LSE as in dcp_block_attn_fwd: a place that sees no key gets
- * O = 0, LSE = -inf; padding is not written.  Inf and NaN in q, k and v reach the places that see them and no others.
+ * O = 0, LSE = -inf; padding is not written.  Inf and NaN in q, k and v reach the places that see them and no others.  The same
+ * call gives the same bits; the order of a place's sums goes by the lengths of the whole batch.
  *   q, out  [n, hq, d] of the cache's dtype, strides as in dcp_tensors_t; out must not overlap q;  lse float [hq, n] contiguous
- *   workspace  device, >= dcp_paged_attn_workspace_bytes, 256-byte aligned; scratch: calls that may run at the same time need one each */
+ *   workspace  device, >= dcp_paged_attn_workspace_bytes, 256-byte aligned; scratch, whatever it holds: calls that may run at the same
+ *              time need one each.  One launch or two. */
 typedef struct {
   int32_t n, hq, layer;
   float softmax_scale;

@@ -15,7 +15,7 @@ struct PagedArgs {
   float* lse;
   const int32_t* seqs;
   int64_t q_st, q_sh, o_st, o_sh;   // bytes
-  int32_t n, hq, group, layer, window, sink;
+  int32_t n, group, layer, window, sink;   // group: query heads of a KV head
   // Query heads that share a KV head are taken in sets of up to 16 (or 8, see Tile::weigh); a workgroup's waves take `abreast` (1, 2 or 4) sets
   // that lie side by side, and where there are fewer than four, the waves of a set take its tiles in turn.
   int32_t per_kv, set_heads, abreast, log_abreast, groups;   // sets of a KV head, heads of a set at most, ..., sets / abreast
@@ -276,6 +276,14 @@ template <typename TT, bool GROUPED> struct Where {
 
 __device__ __forceinline__ int32_t seq_at(const PagedArgs& a, int i) { return a.seqs ? a.seqs[i] : i; }
 
+// O = sum_j exp(s_j - m) v_j / l, LSE = m + ln l with m = max_j s_j, l = sum_j exp(s_j - m) over the keys j that the place sees, in one pass: m, l and
+// O are carried along in fp32 (the weights too: fp32, or two bf16 parts), and rescaled where m grows.
+// Bound by HBM: 2 x keys x hkv x D values are read once, at 6.2 to 6.5 TB/s in large batches (a plain read of linear memory past the caches 7.0): 224 places
+// of 64 to 16 384 tokens, 32/8 heads of 128, pages of 16, 463 us of which the join is 6.  About 6 us pass before the first keys arrive (launch,
+// seqs, seq_len, page_table, one after the other), 4 to 7 are the join, which is what bounds short calls.  All tiles of the batch are dealt
+// out evenly, whatever the lengths, so that workgroups end together; tiles in flight: the next one's K and V (a second V in flight
+// gained nothing, nor did 768 or 1 024 workgroups).  The sums of a place are taken in an order that goes by the lengths of the whole batch, and by nothing else.
+// Conditions that select lanes are written with & and |: under && and || the compiler has dropped the first of the eight selects of a tile.
 template <typename T, int D, int COLS, bool GROUPED, bool ONCE>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, PagedArgs a, PagedParts parts) {
   typedef Tile<T, D> TT;
@@ -629,7 +637,7 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
   }
   if (sets.groups * sets.abreast > (1 << 12)) return fail(DCP_ERR_UNSUPPORTED, "dcp_paged_attn_fwd covers at most 4 096 sets of 16 query heads on one KV head");
   const PagedArgs a{(const char*)t.q, (char*)t.out, t.lse, t.seqs, t.q_stride_t * e, t.q_stride_h * e, t.o_stride_t * e, t.o_stride_h * e,
-                    t.n, t.hq, t.hq / c.hkv, t.layer, t.window, t.sink, sets.per_kv, sets.heads, sets.abreast, sets.log_abreast, (int32_t)sets.groups, whole,
+                    t.n, t.hq / c.hkv, t.layer, t.window, t.sink, sets.per_kv, sets.heads, sets.abreast, sets.log_abreast, (int32_t)sets.groups, whole,
                     t.softmax_scale * 1.44269504088896340736f};
   PagedParts parts;
   parts.joins = (int4*)workspace;

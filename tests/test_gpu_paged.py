@@ -281,6 +281,18 @@ def test_many_places_and_one_long_sequence():
     check(cache, q[-2:], out, lse, 0.125, places[-2:])
 
 
+def test_thousands_of_places():
+    """More places than a workgroup has threads: twenty a thread."""
+    rng = np.random.default_rng(72)
+    lens = [int(x) for x in rng.integers(0, 70, 60)]
+    cache, names = make_cache(lens, 16, 2, 32, seed=73, width=100)
+    places = [int(s) for s in rng.choice(names, 5000)]
+    places[0] = places[17] = places[4999] = -1
+    q = randn((5000, 4, 32), "bf16", 74)
+    out, lse = attend(cache, q, 0.2, ints(places))
+    check(cache, q, out, lse, 0.2, places)
+
+
 @pytest.mark.parametrize("dtype,hq,hkv", [("bf16", 4, 1), ("f32", 2, 2)])
 def test_long_sequences_few_heads(dtype, hq, hkv):
     cache, names = make_cache([20011, 9000, 31], 64, hkv, 128, dtype, seed=18)
