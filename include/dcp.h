@@ -469,7 +469,8 @@ dcp_status_t dcp_cache_compact(const dcp_cache_t* cache, int32_t* counts, void* 
  * call gives the same bits; the order of a place's sums goes by the lengths of the whole batch.
  *   q, out  [n, hq, d] of the cache's dtype, strides as in dcp_tensors_t; out must not overlap q;  lse float [hq, n] contiguous
  *   workspace  device, >= dcp_paged_attn_workspace_bytes, 256-byte aligned; scratch, whatever it holds: calls that may run at the same
- *              time need one each.  One launch or two. */
+ *              time need one each.  One launch or two.
+ * DCP_ERR_UNSUPPORTED: n * hkv * ceil(hq / hkv / 16) * ceil(max_pages * page_size / 32) (fp32: 16) of 2^31 or more. */
 typedef struct {
   int32_t n, hq, layer;
   float softmax_scale;

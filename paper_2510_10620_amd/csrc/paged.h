@@ -64,22 +64,21 @@ struct KeyTiles {
 // n / d by a 32-bit division where that is enough (a 64-bit one takes a few hundred instructions).
 DCP_HD int64_t quot64(int64_t n, int64_t d) { return ((uint64_t)(n | d) >> 32) == 0 ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d; }
 
-// The tiles of a batch, one after the other, dealt to workers in contiguous shares: `each` tiles, and one more for the first `more`.
-struct Shares {
-  int64_t each;
-  int32_t more, workers;
-  DCP_HD int64_t start(int32_t w) const { return each * w + (w < more ? w : more); }
-  DCP_HD int32_t worker_of(int64_t t) const {
-    const int64_t longer = (each + 1) * more;
-    return t < longer ? (int32_t)quot64(t, each + 1) : more + (int32_t)quot64(t - longer, each);
+// The tiles of a batch, one after the other, dealt to up to 2^LOG workers in contiguous shares: `each` tiles, and one more for the first `more`.
+template <int LOG> struct Shares {
+  int32_t each, more, workers;
+  DCP_HD explicit Shares(int32_t total) {
+    const bool all = total >= 1 << LOG;
+    each = all ? total >> LOG : 1;
+    more = all ? total & ((1 << LOG) - 1) : 0;
+    workers = all ? 1 << LOG : total;
+  }
+  DCP_HD int32_t start(int32_t w) const { return each * w + (w < more ? w : more); }
+  DCP_HD int32_t worker_of(int32_t t) const {
+    const int32_t longer = (each + 1) * more;
+    const bool in = t < longer;
+    return (int32_t)((uint32_t)(in ? t : t - longer) / (uint32_t)(each + in)) + (in ? 0 : more);
   }
 };
-DCP_HD Shares make_shares(int64_t total, int32_t most_workers) {
-  Shares s;
-  s.workers = (int32_t)(total < most_workers ? total : most_workers);
-  s.each = quot64(total, s.workers);
-  s.more = (int32_t)(total - s.each * s.workers);
-  return s;
-}
 
 }  // namespace dcp

@@ -15,7 +15,7 @@ struct PagedArgs {
   float* lse;
   const int32_t* seqs;
   int64_t q_st, q_sh, o_st, o_sh;   // bytes
-  int32_t n, group, layer, window, sink;   // group: query heads of a KV head
+  int32_t n, group, window, sink;   // group: query heads of a KV head
   // Query heads that share a KV head are taken in sets of up to 16 (or 8, see Tile::weigh); a workgroup's waves take `abreast` (1, 2 or 4) sets
   // that lie side by side, and where there are fewer than four, the waves of a set take its tiles in turn.
   int32_t per_kv, set_heads, abreast, log_abreast, groups;   // sets of a KV head, heads of a set at most, ..., sets / abreast
@@ -27,7 +27,7 @@ struct PagedArgs {
 // begins in the middle of at most one item and ends in the middle of at most one: slot 2 w holds the first, 2 w + 1 the second.
 struct PagedParts {
   int4* joins;     // [kWorkers] (place, group, first worker, last worker), place -1: nothing to join.  By item where there are no more
-                   // items than workers, else by the worker that has the item's first tile
+                   // items than workers (not written for padding), else by the worker that has the item's first tile
   float2* ml;      // [2 kWorkers][abreast][set_heads] running maximum, sum
   float* o;        // [2 kWorkers][abreast][set_heads][D]
   int32_t by_item;
@@ -36,7 +36,7 @@ struct PagedParts {
 // Two workgroups on a CU, all resident.  The four waves read neighbouring heads of the same keys: where each workgroup walks one head, a
 // quarter of what the memory reads lies in pages that others open again (8 KV heads of 256 bytes, a plain read of all keys
 // and values 5.8 TB/s against 6.9; linear 7.0).
-static constexpr int kWorkers = 512;
+static constexpr int kLogWorkers = 9, kWorkers = 1 << kLogWorkers;
 static constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
 static constexpr int kSetHeads = 16;     // query heads of a matrix tile
 // Items are taken whole, so that nothing is to be joined, where a workgroup each is enough and none can have more than so many tiles a wave:
@@ -287,43 +287,41 @@ __device__ __forceinline__ int32_t seq_at(const PagedArgs& a, int i) { return a.
 template <typename T, int D, int COLS, bool GROUPED, bool ONCE>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, PagedArgs a, PagedParts parts) {
   typedef Tile<T, D> TT;
-  __shared__ int64_t s_wave[kPagedWaves], s_before;
-  __shared__ int32_t s_place, s_seq[kPagedThreads], s_len[kPagedThreads];
+  __shared__ int32_t s_wave[kPagedWaves], s_before, s_place, s_seq[kPagedThreads], s_len[kPagedThreads];
   __shared__ float s_acc[kPagedWaves - 1][TT::kAcc * 4 + 2][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4, w = blockIdx.x;
 
   // Every workgroup sums up all places' tiles for itself: thread t those of places [t per, (t + 1) per).
   const int per = (a.n + kPagedThreads - 1) / kPagedThreads;
-  int64_t mine = 0;
+  int32_t mine = 0;
   for (int x = tid * per; x < min(a.n, (tid + 1) * per); x++) {
     const int seq = seq_at(a, x), len = c.is_seq(seq) ? c.length(seq) : 0;
     if (c.is_seq(seq)) mine += a.whole ? 1 : KeyTiles(len, a.window, a.sink, TT::kKeys).count;
     s_seq[tid] = seq;   // of use where a thread has one place
     s_len[tid] = len;
   }
-  int64_t upto = mine;
+  int32_t upto = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(upto, o);
+    const int32_t y = __shfl_up(upto, o);
     if (lane >= o) upto += y;
   }
   if (lane == 63) s_wave[wave] = upto;
   __syncthreads();
-  int64_t all = 0, earlier = 0;
+  int32_t all = 0, earlier = 0;
 #pragma unroll
   for (int y = 0; y < kPagedWaves; y++) {
     if (y < wave) earlier += s_wave[y];
     all += s_wave[y];
   }
-  // nothing to join, unless the worker that begins an item says so
-  if (tid == 0 && !a.whole && (!parts.by_item || w >= a.n * a.groups || !c.is_seq(seq_at(a, w / a.groups)))) parts.joins[w] = make_int4(-1, 0, 0, 0);
+  if (tid == 0 && !parts.by_item && !a.whole) parts.joins[w] = make_int4(-1, 0, 0, 0);   // unless it begins an item that it does not end
   if (all == 0) return;
-  const Shares sh = make_shares(all * a.groups, kWorkers);
+  const Shares<kLogWorkers> sh(all * a.groups);   // below 2^31: the host has seen to it
   if (w >= sh.workers) return;
-  int64_t at = sh.start(w);
-  const int64_t end = sh.start(w + 1);
+  int32_t at = sh.start(w);
+  const int32_t end = sh.start(w + 1);
   {
-    const int64_t b = (earlier + upto - mine) * a.groups;
+    const int32_t b = (earlier + upto - mine) * a.groups;
     if (b <= at && at < b + mine * a.groups) {
       s_place = tid * per;
       s_before = earlier + upto - mine;
@@ -331,26 +329,26 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, 
   }
   __syncthreads();
   int place = s_place;
-  int64_t before = s_before;   // tiles of the places before it
+  int32_t before = s_before;   // tiles of the places before it
   const int abreast = a.abreast, turns = kPagedWaves >> a.log_abreast, turn = wave >> a.log_abreast;
   while (at < end && place < a.n) {
     const int seq = per == 1 ? s_seq[place] : seq_at(a, place);
     if (!c.is_seq(seq)) { place++; continue; }
     const KeyTiles keys(per == 1 ? s_len[place] : c.length(seq), a.window, a.sink, TT::kKeys);
     const int units = a.whole ? 1 : keys.count;   // of an item
-    const int64_t rel = at - before * a.groups;
-    if (rel >= (int64_t)units * a.groups) { before += units; place++; continue; }
+    const int32_t rel = at - before * a.groups;
+    if (rel >= units * a.groups) { before += units; place++; continue; }
     const int32_t* row = c.row(seq);
-    const int grp = (int)quot64(rel, units), t0 = (int)(rel - (int64_t)grp * units);
-    const int t1 = a.whole ? keys.count : (int)min((int64_t)keys.count, t0 + (end - at));
+    const int grp = (int)((uint32_t)rel / (uint32_t)units), t0 = rel - grp * units;
+    const int t1 = a.whole ? keys.count : min(keys.count, t0 + (end - at));
     const int set = grp * abreast + (wave & (abreast - 1)), hk = a.per_kv == 1 ? set : set / a.per_kv;
     const int h0 = hk * a.group + (set - hk * a.per_kv) * kSetHeads, n_heads = min(kSetHeads, (hk + 1) * a.group - h0);
     const int col = COLS == 8 ? i & 7 : i;
 
     typename TT::Q q;
     TT::load_q(q, a.q + place * a.q_st + (h0 + col) * a.q_sh, g, col < n_heads);
-    const char* kb = c.k + a.layer * c.k_sl + hk * c.k_sh + TT::k_off(g);
-    const char* vb = c.v + a.layer * c.v_sl + hk * c.v_sh + TT::v_off(i);
+    const char* kb = c.k + hk * c.k_sh + TT::k_off(g);
+    const char* vb = c.v + hk * c.v_sh + TT::v_off(i);
     f32x4 acc[TT::kAcc];
 #pragma unroll
     for (int e = 0; e < TT::kAcc; e++) acc[e] = f32x4{0, 0, 0, 0};
@@ -477,7 +475,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, 
       }
     }
     if (t0 == 0 && tid == 0 && !a.whole) {
-      const int last = t1 == keys.count ? w : sh.worker_of(before * a.groups + (int64_t)(grp + 1) * keys.count - 1);
+      const int last = t1 == keys.count ? w : sh.worker_of(before * a.groups + (grp + 1) * keys.count - 1);
       if (parts.by_item) parts.joins[place * a.groups + grp] = make_int4(last == w ? -1 : place, grp, w, last);
       else if (last != w) parts.joins[w] = make_int4(place, grp, w, last);
     }
@@ -493,6 +491,7 @@ __global__ __launch_bounds__(THREADS) void paged_join_kernel(KCache c, PagedArgs
   __shared__ float s_m[HEADS][kRows], s_l[HEADS][kRows], s_o[HEADS][kRows][D];
   const int tid = threadIdx.x;
   const int4 job = parts.joins[blockIdx.x];
+  if (parts.by_item && !c.is_seq(seq_at(a, blockIdx.x / a.groups))) return;   // nobody has written the entry of padding
   if (job.x < 0) return;
   const int hw = tid / (kLanes * kRows), r = tid / kLanes % kRows, d = tid % kLanes * 4;
   const int y = blockIdx.y * HEADS + hw, beside = y / a.set_heads, h = y - beside * a.set_heads, set = job.y * a.abreast + beside;
@@ -635,9 +634,13 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
     whole = t.n * x.groups <= kWorkers && most <= (t.n * x.groups > kFullItems ? kWholeRoundsFull : kWholeRounds) * (kPagedWaves / x.abreast);
     if (whole) sets = x;
   }
+  if (t.n * (int64_t)((c.max_len + tile - 1) / tile) * sets_of(c.hkv, t.hq, cache->d, 1).groups > INT32_MAX)
+    return fail(DCP_ERR_UNSUPPORTED, "n x hkv x sets of 16 query heads on one KV head x tiles of 32 (fp32: 16) tokens in a row of the table must be below 2^31");
   if (sets.groups * sets.abreast > (1 << 12)) return fail(DCP_ERR_UNSUPPORTED, "dcp_paged_attn_fwd covers at most 4 096 sets of 16 query heads on one KV head");
+  c.k += t.layer * c.k_sl;   // the layer's
+  c.v += t.layer * c.v_sl;
   const PagedArgs a{(const char*)t.q, (char*)t.out, t.lse, t.seqs, t.q_stride_t * e, t.q_stride_h * e, t.o_stride_t * e, t.o_stride_h * e,
-                    t.n, t.hq / c.hkv, t.layer, t.window, t.sink, sets.per_kv, sets.heads, sets.abreast, sets.log_abreast, (int32_t)sets.groups, whole,
+                    t.n, t.hq / c.hkv, t.window, t.sink, sets.per_kv, sets.heads, sets.abreast, sets.log_abreast, (int32_t)sets.groups, whole,
                     t.softmax_scale * 1.44269504088896340736f};
   PagedParts parts;
   parts.joins = (int4*)workspace;

@@ -57,33 +57,38 @@ int main() {
       }
 
   // every tile belongs to one worker, in order; an item that several share leaves its parts in slots of their own
-  for (int k = 0; k < 3000; k++) {
-    std::vector<int64_t> items;
-    const int n = (int)uni(1, 40);
-    for (int i = 0; i < n; i++) items.push_back(k % 5 == 0 ? uni(1, int64_t(1) << 25) : uni(1, 50));
+  for (int k = 0; k < 6000; k++) {
+    std::vector<int32_t> items;
+    const int n = (int)uni(1, 40), most = 1 << (k % 2 ? 9 : 4);
+    for (int i = 0; i < n; i++) items.push_back(k % 5 == 0 ? (int32_t)uni(1, 1 << 25) : (int32_t)uni(1, 50));
     int64_t total = 0;
-    for (int64_t x : items) total += x;
-    const int most = (int)uni(1, 700);
-    const Shares s = make_shares(total, most);
-    CHECK(s.workers >= 1 && s.workers <= most && s.start(0) == 0 && s.start(s.workers) == total);
+    for (int32_t x : items) total += x;
+    CHECK(total <= INT32_MAX);
+    const Shares<9> s9((int32_t)total);
+    const Shares<4> s4((int32_t)total);
+    auto start = [&](int w) { return k % 2 ? s9.start(w) : s4.start(w); };
+    auto worker_of = [&](int t) { return k % 2 ? s9.worker_of(t) : s4.worker_of(t); };
+    const int workers = k % 2 ? s9.workers : s4.workers;
+    CHECK(workers >= 1 && workers <= most && start(0) == 0 && start(workers) == total);
     std::map<int, int> slots;   // slot -> item
-    int64_t begin = 0;
+    int32_t begin = 0;
     for (int i = 0; i < n; begin += items[i], i++) {
-      const int first = s.worker_of(begin), last = s.worker_of(begin + items[i] - 1);
-      CHECK(first >= 0 && first <= last && last < s.workers);
-      CHECK(s.start(first) <= begin && begin < s.start(first + 1));
-      CHECK(s.start(last) < begin + items[i] && begin + items[i] <= s.start(last + 1));
+      const int first = worker_of(begin), last = worker_of(begin + items[i] - 1);
+      CHECK(first >= 0 && first <= last && last < workers);
+      CHECK(start(first) <= begin && begin < start(first + 1));
+      CHECK(start(last) < begin + items[i] && begin + items[i] <= start(last + 1));
       if (first == last) continue;
       for (int w = first; w <= last; w++) {
-        CHECK(s.start(w) < s.start(w + 1));   // nobody between them is without work
+        CHECK(start(w) < start(w + 1));   // nobody between them is without work
         const int slot = w == first ? 2 * w + 1 : 2 * w;
         CHECK(slot < 2 * most && slots.emplace(slot, i).second);
       }
     }
-    for (int w = 0; w < s.workers; w++) CHECK(s.start(w + 1) - s.start(w) >= 1 && s.start(w + 1) - s.start(w) <= total / s.workers + 1);
+    for (int w = 0; w < workers; w++) CHECK(start(w + 1) - start(w) >= 1 && start(w + 1) - start(w) <= total / workers + 1);
   }
-  // the largest batch: 16 384 places of 2^30 tokens (2^26 tiles), 4 096 sets
-  const Shares s = make_shares(int64_t(1) << (14 + 26 + 12), 1000);
-  CHECK(s.start(s.workers) == int64_t(1) << 52 && s.worker_of((int64_t(1) << 52) - 1) == s.workers - 1);
+  for (int32_t total : {INT32_MAX, INT32_MAX - 511, 511, 512, 513, 1}) {
+    const Shares<9> s(total);
+    CHECK(s.start(s.workers) == total && s.worker_of(total - 1) == s.workers - 1 && s.worker_of(0) == 0);
+  }
   std::printf("host-paged ok\n");
 }

@@ -104,6 +104,8 @@ def test_attention_refuses():
                      (dict(sink=-1), -1), (dict(q=0), -1), (dict(q=A + 4), -1), (dict(out=0), -1), (dict(lse=0), -1), (dict(lse=A + 2), -1),
                      (dict(q_stride_t=63), -1), (dict(o_stride_h=60), -1), (dict(out=A + 64), -1)):
         assert lib.dcp_paged_attn_fwd(_ref(c), ctypes.byref(_attn(**kw)), A, max(need, 1 << 30), None) == want, kw
+    full = _cache(max_pages=1 << 26)   # 2^30 tokens a row: 16 384 places of 2^25 tiles
+    assert lib.dcp_paged_attn_fwd(_ref(full), ctypes.byref(_attn(n=16384, out=A << 20)), A, 1 << 30, None) == -4 and "2^31" in P.dcp_last_error()
     assert lib.dcp_paged_attn_fwd(_ref(c), None, A, need, None) == -1
     assert lib.dcp_paged_attn_fwd(_ref(c), ctypes.byref(_attn()), None, need, None) == -5
     assert lib.dcp_paged_attn_fwd(_ref(c), ctypes.byref(_attn()), A, need - 1, None) == -5
