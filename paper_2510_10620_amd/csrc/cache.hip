@@ -178,8 +178,9 @@ __device__ __forceinline__ u32x4 load16(const char* p) { return __builtin_nontem
 __device__ __forceinline__ void store16(char* p, u32x4 v) { __builtin_nontemporal_store(v, (u32x4*)p); }
 
 // 16-byte chunks [first, last) of page `from` to page `to`, of one layer of k or v, by one workgroup of 256: chunk x is chunk x % head_chunks of
-// (token, head) x / head_chunks.  Four in flight a lane; read through the caches, as one page may be copied for many (64 sequences
-// forked from 64 drawn with repeats, over 4 layers: 56 us past them, 50 so).
+// (token, head) x / head_chunks.  Four in flight a lane.  SHARED: one page may be copied for many, and is read through the caches (64
+// sequences forked from 64 drawn with repeats, over 4 layers: 56 us past them, 50 so; half of a large cache moved 956 and 984).
+template <bool SHARED>
 __device__ __forceinline__ void copy_chunks(const KCache& c, char* base, int64_t st_p, int64_t st_t, int64_t st_h, int from, int to, int first, int last) {
   const char* src = base + from * st_p;
   char* dst = base + to * st_p;
@@ -192,13 +193,13 @@ __device__ __forceinline__ void copy_chunks(const KCache& c, char* base, int64_t
     int64_t at[4];
     u32x4 v[4];
 #pragma unroll
-    for (int y = 0; y < 4; y++) { at[y] = offset(x + 256 * y); v[y] = *(const u32x4*)(src + at[y]); }
+    for (int y = 0; y < 4; y++) { at[y] = offset(x + 256 * y); v[y] = SHARED ? *(const u32x4*)(src + at[y]) : load16(src + at[y]); }
 #pragma unroll
     for (int y = 0; y < 4; y++) store16(dst + at[y], v[y]);
   }
   for (; x < last; x += 256) {
     const int64_t at = offset(x);
-    store16(dst + at, *(const u32x4*)(src + at));
+    store16(dst + at, SHARED ? *(const u32x4*)(src + at) : load16(src + at));
   }
 }
 
@@ -237,8 +238,8 @@ __global__ __launch_bounds__(256) void fork_kernel(KCache c, const int32_t* __re
     if (first >= last) continue;
     const int32_t page = from[whole], mine = to[whole];
     if (!c.is_page(page) || !c.is_page(mine)) continue;
-    if (y & 1) copy_chunks(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, page, mine, first, last);
-    else copy_chunks(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, page, mine, first, last);
+    if (y & 1) copy_chunks<true>(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, page, mine, first, last);
+    else copy_chunks<true>(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, page, mine, first, last);
   }
 }
 
@@ -379,8 +380,8 @@ __global__ __launch_bounds__(256) void move_kernel(KCache c, Moves m, const int3
       c.ref[to] = c.ref[from];
       c.ref[from] = 0;
     }
-    if (y & 1) copy_chunks(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, from, to, first, last);
-    else copy_chunks(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, from, to, first, last);
+    if (y & 1) copy_chunks<false>(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, from, to, first, last);
+    else copy_chunks<false>(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, from, to, first, last);
   }
 }
 

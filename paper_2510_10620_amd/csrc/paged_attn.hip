@@ -549,8 +549,9 @@ __global__ __launch_bounds__(THREADS) void paged_join_kernel(KCache c, PagedArgs
 
 template <typename T, int D, int COLS, bool ONCE>
 static void launch_once(const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
-  if (c.page.d % Tile<T, D>::kGroup == 0) hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, true, ONCE>), dim3(kWorkers), dim3(kPagedThreads), 0, s, c, a, parts);
-  else hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, false, ONCE>), dim3(kWorkers), dim3(kPagedThreads), 0, s, c, a, parts);
+  const dim3 grid(a.whole ? a.n * a.groups : kWorkers);
+  if (c.page.d % Tile<T, D>::kGroup == 0) hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, true, ONCE>), grid, dim3(kPagedThreads), 0, s, c, a, parts);
+  else hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, false, ONCE>), grid, dim3(kPagedThreads), 0, s, c, a, parts);
 }
 template <typename T, int D, int COLS>
 static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
