@@ -179,7 +179,7 @@ __device__ __forceinline__ void store16(char* p, u32x4 v) { __builtin_nontempora
 
 // 16-byte chunks [first, last) of page `from` to page `to`, of one layer of k or v, by one workgroup of 256: chunk x is chunk x % head_chunks of
 // (token, head) x / head_chunks.  Four in flight a lane.  SHARED: one page may be copied for many, and is read through the caches (64
-// sequences forked from 64 drawn with repeats, over 4 layers: 56 us past them, 50 so; half of a large cache moved 956 and 984).
+// sequences forked from 64 drawn with repeats, over 4 layers: 56 us past them, 50 so; pages that move, each read once: 956 and 984).
 template <bool SHARED>
 __device__ __forceinline__ void copy_chunks(const KCache& c, char* base, int64_t st_p, int64_t st_t, int64_t st_h, int from, int to, int first, int last) {
   const char* src = base + from * st_p;
@@ -206,8 +206,8 @@ __device__ __forceinline__ void copy_chunks(const KCache& c, char* base, int64_t
 // What a workgroup copies at a time: kPieceChunks chunks (16 KiB) of a page, so that pages that are filled unevenly, or few, still fill the chip
 // (64 sequences forked, 4 layers, pages of 512 KiB: 93 us with a workgroup a page, 47 so).
 static constexpr int kPieceChunks = 1024;
-// Workgroups that share such pieces, each taking every kCopyWorkers-th: half of 9 712 pages of 4 layers moved, 5.1 GB read and written, in 995
-// us with 4 096, 980 with 16 384 and 64 KiB at a time, 842 to 960 (by where the pages lie) so: 5.3 to 6.0 TB/s.
+// Workgroups that share such pieces, each taking every kCopyWorkers-th: 2 430 pages of 512 KiB moved, 5.1 GB read and written, in 995 us with
+// 4 096, 980 with 16 384 and 64 KiB at a time, 842 to 960 (by where the pages lie) so: 5.3 to 6.0 TB/s.
 static constexpr int kCopyWorkers = 32768;
 inline int pieces_of(const KCache& c) { return (int)(((int64_t)c.page.d * c.hkv * c.head_chunks() + kPieceChunks - 1) / kPieceChunks); }
 
