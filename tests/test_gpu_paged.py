@@ -737,3 +737,93 @@ def test_binding_refuses():
             P.Cache(**a)
     with pytest.raises(ValueError):
         P.dcp_cache_append(cache, q[:, :2], q[:, :2], seqs=ints([0]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [128, 32])
+@pytest.mark.parametrize("hq,hkv", [(16, 1), (9, 3), (27, 3), (40, 1), (32, 8)])
+@pytest.mark.parametrize("page", [20, 37, 64])
+def test_wide_groups_in_any_pages(dtype, d, hq, hkv, page):
+    cache, names = make_cache([1, 45, 700, 333], page, hkv, d, dtype, seed=hq + page)
+    q = randn((4, hq, d), dtype, 75)
+    out, lse = attend(cache, q, d ** -0.5, ints(names))
+    check(cache, q, out, lse, d ** -0.5, [int(s) for s in names])
+    out, lse = attend(cache, q, d ** -0.5, ints(names), 50, 10)
+    check(cache, q, out, lse, d ** -0.5, [int(s) for s in names], 50, 10)
+
+
+def test_places_without_seqs():
+    """Reserve, append and attention where place i is sequence i."""
+    import torch
+    cache = P.Cache.empty(1, 20, 8, 2, 64, 5, 6, torch.bfloat16)
+    cache.k.fill_(NAN)
+    cache.v.fill_(NAN)
+    m = mirror(cache)
+    status = ints([7] * 4)
+    new = [9, 0, 1, 30]
+    P.dcp_cache_reserve(cache, None, status, n_new=ints(new))
+    assert status.tolist() == m.reserve(range(4), new)
+    k, v = randn((40, 2, 64), "bf16", 76), randn((40, 2, 64), "bf16", 77)
+    P.dcp_cache_append(cache, k, v, cu_new=ints([0, 9, 9, 10, 40]))
+    m.append(range(4), [0, 9, 9, 10, 40], words(k), words(v), [0] * 4)
+    same_map(cache, m)
+    P.dcp_cache_reserve(cache, None, status)
+    assert status.tolist() == m.reserve(range(4), [1] * 4)
+    P.dcp_cache_append(cache, k[:4], v[:4])
+    m.append(range(4), [0, 1, 2, 3, 4], words(k), words(v), [0] * 4)
+    same_map(cache, m)
+    q = randn((5, 4, 64), "bf16", 78)
+    out, lse = attend(cache, q, 0.125)
+    check(cache, q, out, lse, 0.125, range(5))
+
+
+def test_no_places_and_timing():
+    """Calls without places do nothing; the calls are timed under ids of their own."""
+    import torch
+    cache, names = make_cache([30, 20], 8, 2, 64, seed=79)
+    m = mirror(cache)
+    none = ints([])
+    q = torch.empty((0, 4, 64), dtype=torch.bfloat16, device="cuda")
+    P.dcp_cache_reserve(cache, none, none)
+    P.dcp_cache_append(cache, q[:, :2], q[:, :2], seqs=none)
+    P.dcp_cache_fork(cache, none, none, none)
+    P.dcp_cache_free(cache, none)
+    P.dcp_paged_attn_fwd(cache, q, q.clone(), torch.empty((4, 0), device="cuda"), 0.1, torch.empty(0, dtype=torch.uint8, device="cuda"), seqs=none)
+    same_map(cache, m)
+    P.dcp_profile_enable(True)
+    attend(cache, randn((2, 4, 64), "bf16", 80), 0.1, ints(names))
+    P.dcp_cache_free(cache, ints(names))
+    (ms, n), (ms_c, n_c) = P.dcp_profile_read("paged_attn"), P.dcp_profile_read("cache")
+    P.dcp_profile_enable(False)
+    assert n == n_c == 1 and 0 < ms < 100 and 0 < ms_c < 100
+
+
+def test_a_captured_life_of_a_cache():
+    """Fork, free and compaction recorded once and replayed on the map as it is each time, with eager calls between, against the oracle."""
+    import torch
+    cache, names = make_cache([20, 33, 7], 8, 2, 32, layers=2, spare=20, extra_seqs=5, width=12, seed=81)
+    m = mirror(cache)
+    a, b, c = (int(s) for s in names)
+    empty = [s for s in range(8) if s not in (a, b, c)]
+    src, dst, gone = [a, b, -1], [empty[0], empty[1], empty[2]], [a, 99]
+    args = ints(src), ints(dst), ints([7] * 3), ints(gone), ints([0, 0])
+    ws = torch.empty(P.dcp_cache_workspace_bytes(cache), dtype=torch.uint8, device="cuda").random_()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        P.dcp_cache_fork(cache, args[0], args[1], args[2])
+        P.dcp_cache_free(cache, args[3])
+        P.dcp_cache_compact(cache, args[4], ws)
+    for _ in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+        want = m.fork(src, dst)
+        m.free(gone)
+        assert args[4].tolist() == m.compact() and args[2].tolist() == want
+        same_map(cache, m)
+        ws.random_()
+        # another life between: the copies end, the source fills again
+        P.dcp_cache_free(cache, ints(dst[:2]))
+        m.free(dst[:2])
+        status = reserve(cache, m, [a], [13])
+        append(cache, m, [a], [13], status, 1, 82)
+        same_map(cache, m)
