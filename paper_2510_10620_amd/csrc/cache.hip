@@ -41,31 +41,45 @@ struct Place {
   int32_t seq, first, need, tokens, code;
 };
 
-// a: seqs (src); b: n_new (dst).  owner[s]: the first place that changes sequence s.
+// What is read for a place: s is seqs[i] (src[i]), t n_new[i] (dst[i]); the lengths of s and, for a fork, of t.
+struct Asked {
+  int32_t s, t, len, len_t;
+};
 template <bool FORK>
-__device__ __forceinline__ Place place_at(const KCache& c, const int32_t* a, const int32_t* b, int i, const int32_t* owner) {
+__device__ __forceinline__ Asked asked_at(const KCache& c, const int32_t* a, const int32_t* b, int i) {
+  Asked x{a ? a[i] : i, 1, 0, 0};
+  if (FORK || b) x.t = b[i];
+  if (c.is_seq(x.s)) x.len = c.length(x.s);
+  if (FORK && c.is_seq(x.t)) x.len_t = c.len[x.t];
+  return x;
+}
+
+// owner[s]: the first place that changes sequence s.
+template <bool FORK>
+__device__ __forceinline__ Place place_of(const KCache& c, const Asked& x, int i, const int32_t* owner) {
   Place p{-1, 0, 0, 0, DCP_PLACE_OK};
-  const int s = a ? a[i] : i;
-  if (s < 0) return p;
+  if (x.s < 0) return p;
   p.code = DCP_PLACE_BAD;
-  if (!c.is_seq(s)) return p;
+  if (!c.is_seq(x.s)) return p;
   if (FORK) {
-    const int d = b[i];
-    if (!c.is_seq(d) || owner[d] != i || owner[s] != kNoOwner || c.len[d] != 0) return p;
-    p.tokens = c.length(s);
-    p.seq = d;
+    if (!c.is_seq(x.t) || owner[x.t] != i || owner[x.s] != kNoOwner || x.len_t != 0) return p;
+    p.tokens = x.len;
+    p.seq = x.t;
     p.first = c.page.quot(p.tokens);
     p.need = c.page.rem(p.tokens, p.first) != 0;
   } else {
-    const int more = b ? b[i] : 1, len = c.length(s);
-    if (owner[s] != i || more < 0 || more > c.max_len - len) return p;
-    p.tokens = len + more;
-    p.seq = s;
-    p.first = c.pages_of(len);
+    if (owner[x.s] != i || x.t < 0 || x.t > c.max_len - x.len) return p;
+    p.tokens = x.len + x.t;
+    p.seq = x.s;
+    p.first = c.pages_of(x.len);
     p.need = c.pages_of(p.tokens) - p.first;
   }
   p.code = DCP_PLACE_OK;
   return p;
+}
+template <bool FORK>
+__device__ __forceinline__ Place place_at(const KCache& c, const int32_t* a, const int32_t* b, int i, const int32_t* owner) {
+  return place_of<FORK>(c, asked_at<FORK>(c, a, b, i), i, owner);
 }
 
 // One workgroup: the places' needs are summed up in their order, page_ref is walked once, and the k-th free page goes to the place
@@ -85,13 +99,15 @@ __global__ __launch_bounds__(kMapThreads) void take_kernel(KCache c, const int32
     for (int u = 0; u < kScan; u++) held[u] = first + u * 64 < c.n_pages ? c.ref[first + u * 64] : 1;
   };
   scan(wave * (64 * kScan) + lane);
+  Asked ask{-1, 0, 0, 0};   // of place tid
+  if (tid < n) ask = asked_at<FORK>(c, a, b, tid);
   for (int s = tid; s < c.n_seqs; s += kMapThreads) owner[s] = kNoOwner;
   if (tid == 0) short_place = -1;
   __syncthreads();
   for (int i = tid; i < n; i += kMapThreads) {
-    const int s = a ? a[i] : i;
+    const int s = i == tid ? ask.s : a ? a[i] : i;
     if (!c.is_seq(s)) continue;
-    const int t = FORK ? b[i] : s;
+    const int t = !FORK ? s : i == tid ? ask.t : b[i];
     if (c.is_seq(t)) atomicMin(&owner[t], i);
   }
   __syncthreads();
@@ -99,7 +115,7 @@ __global__ __launch_bounds__(kMapThreads) void take_kernel(KCache c, const int32
   int total = 0;
   for (int base = 0; base < n; base += kMapThreads) {
     const int i = base + tid;
-    if (i < n) mine = place_at<FORK>(c, a, b, i, owner);
+    if (i < n) mine = base ? place_at<FORK>(c, a, b, i, owner) : place_of<FORK>(c, ask, i, owner);
     int all;
     const int x = block_sum(i < n ? min(mine.need, cap) : 0, cap, wave_sum, &all);
     if (i < n) sums[i] = min(total + x, cap);
