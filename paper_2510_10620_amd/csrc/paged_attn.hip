@@ -345,7 +345,12 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, 
     const int h0 = hk * a.group + (set - hk * a.per_kv) * kSetHeads, n_heads = min(kSetHeads, (hk + 1) * a.group - h0);
     const int col = COLS == 8 ? i & 7 : i;
 
-    typename TT::Q q;
+    Where<TT, GROUPED> now, next;
+    int x = t0 + turn;
+    int32_t base = keys.tile_at(x) * TT::kKeys, base_next = keys.tile_at(min(x + turns, keys.count)) * TT::kKeys;
+    now.look(c, row, base, x < t1 ? keys.len : 0, i, g);
+    next.look(c, row, base_next, x + turns < t1 ? keys.len : 0, i, g);
+    typename TT::Q q;   // comes while the entries of the table do
     TT::load_q(q, a.q + place * a.q_st + (h0 + col) * a.q_sh, g, col < n_heads);
     const char* kb = c.k + hk * c.k_sh + TT::k_off(g);
     const char* vb = c.v + hk * c.v_sh + TT::v_off(i);
@@ -354,13 +359,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, 
     for (int e = 0; e < TT::kAcc; e++) acc[e] = f32x4{0, 0, 0, 0};
     float m = -INFINITY, l = 0;
     TT t;
-    Where<TT, GROUPED> now, next;
-    int x = t0 + turn;
-    int32_t base = keys.tile_at(x) * TT::kKeys, base_next = 0;
     if (x < t1) {
-      now.look(c, row, base, keys.len, i, g);
-      base_next = keys.tile_at(min(x + turns, keys.count)) * TT::kKeys;
-      next.look(c, row, base_next, x + turns < t1 ? keys.len : 0, i, g);
       now.settle(c);
       now.template load_k<ONCE>(c, t, kb, i);
       now.template load_v<ONCE>(c, t, vb);
