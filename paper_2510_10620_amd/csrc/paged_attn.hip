@@ -278,8 +278,8 @@ __device__ __forceinline__ int32_t seq_at(const PagedArgs& a, int i) { return a.
 
 // O = sum_j exp(s_j - m) v_j / l, LSE = m + ln l with m = max_j s_j, l = sum_j exp(s_j - m) over the keys j that the place sees, in one pass: m, l and
 // O are carried along in fp32 (the weights too: fp32, or two bf16 parts), and rescaled where m grows.
-// Bound by HBM: 2 x keys x hkv x D values are read once, at 6.2 to 6.5 TB/s in large batches (a plain read of linear memory past the caches 7.0): 224 places
-// of 64 to 16 384 tokens, 32/8 heads of 128, pages of 16, 463 us of which the join is 6.  About 6 us pass before the first keys arrive (launch,
+// Bound by HBM: 2 x keys x hkv x D values are read once, at 6.3 to 6.5 TB/s in large batches (a plain read of linear memory past the caches 7.0): 224 places
+// of 64 to 16 384 tokens, 32/8 heads of 128, pages of 16, 463 us of which the join is 6.  About 5 us pass before the first keys are asked for (launch,
 // seqs, seq_len, page_table, one after the other), 4 to 7 are the join, which is what bounds short calls.  All tiles of the batch are dealt
 // out evenly, whatever the lengths, so that workgroups end together; tiles in flight: the next one's K and V (a second V in flight
 // gained nothing, nor did 768 or 1 024 workgroups).  The sums of a place are taken in an order that goes by the lengths of the whole batch, and by nothing else.
