@@ -408,7 +408,8 @@ dcp_status_t dcp_comm_volume(const int32_t* cu_seqlens_host, int32_t n_seq, int3
  * place with a negative number is padding: nothing is read or written for it.  A number >= n_seqs is no sequence: the place
  * gets DCP_PLACE_BAD where the call has a status array and is padding elsewhere.  Page numbers outside [0, n_pages) and lengths outside
  * [0, max_pages * page_size] are never followed: such a page holds nothing, such a length is cut.
- * `status` (int32 [n], device) receives DCP_PLACE_*; a place that is not OK leaves its sequence and every page as they were.
+ * `status` (int32 [n], device) receives DCP_PLACE_*; a place that is not OK leaves its sequence and every page as they were (entries of
+ * its row behind the pages that it holds may become -1).
  * At most DCP_CACHE_MAX_SEQS sequences in a cache and places in a call, 2^30 tokens in a row of the table; n == 0 is legal.  Calls that change one cache, and
  * those that read it meanwhile, must be ordered (one stream, or events).  Errors of the host's checks as elsewhere. */
 #define DCP_CACHE_MAX_SEQS 16384
@@ -438,7 +439,7 @@ dcp_status_t dcp_cache_reserve(const dcp_cache_t* cache, const int32_t* seqs, co
 /* Writes the keys and values of the tokens that dcp_cache_reserve made room for into the pages of one layer: place i has
  * the tokens [cu_new[i], cu_new[i + 1]) of k_new and v_new (cu_new NULL: token i alone), the last ones of its sequence.
  *   cu_new  int32 [n + 1], device, ascending; tokens that it leaves out or that are not below n_tokens are not read
- *   status  of dcp_cache_reserve (places that are not OK are left out), or NULL
+ *   status  of dcp_cache_reserve (places that are not OK are left out), or NULL; a sequence is named by one place that is written
  *   k_new, v_new  [n_tokens, hkv, d] of the cache's dtype, strides as for k and v of dcp_tensors_t; not part of the cache;
  *                n_tokens at most 2^26 */
 dcp_status_t dcp_cache_append(const dcp_cache_t* cache, int32_t layer, const int32_t* seqs, const int32_t* cu_new, int32_t n,
@@ -464,13 +465,14 @@ dcp_status_t dcp_cache_compact(const dcp_cache_t* cache, int32_t* counts, void* 
 
 /* Attention of one new token per place over its sequence: the query is the token at position seq_len - 1 (appended already) and
  * sees key j iff j < seq_len and, with window > 0, seq_len - 1 - j < window or j < sink (the predicate of WINDOW rows; window 0: no
- * window).  Keys in pages that do not exist are not seen.  Out and LSE as in dcp_block_attn_fwd: a place that sees no key gets
+ * window).  A sequence may be named by several places; one that dcp_cache_reserve refused still ends at its last token: give such a
+ * place as padding.  Keys in pages that do not exist are not seen.  Out and LSE as in dcp_block_attn_fwd: a place that sees no key gets
  * O = 0, LSE = -inf; padding is not written.  Inf and NaN in q, k and v reach the places that see them and no others.  The same
  * call gives the same bits; the order of a place's sums goes by the lengths of the whole batch.
  *   q, out  [n, hq, d] of the cache's dtype, strides as in dcp_tensors_t; out must not overlap q;  lse float [hq, n] contiguous
  *   workspace  device, >= dcp_paged_attn_workspace_bytes, 256-byte aligned; scratch, whatever it holds: calls that may run at the same
  *              time need one each.  One launch or two.
- * DCP_ERR_UNSUPPORTED: n * hkv * ceil(hq / hkv / 16) * ceil(max_pages * page_size / 32) (fp32: 16) of 2^31 or more. */
+ * DCP_ERR_UNSUPPORTED: hkv * ceil(hq / hkv / 16) above 4 096; that times n times ceil(max_pages * page_size / 32) (fp32: 16) of 2^31 or more. */
 typedef struct {
   int32_t n, hq, layer;
   float softmax_scale;
