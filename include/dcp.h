@@ -441,7 +441,7 @@ dcp_status_t dcp_cache_reserve(const dcp_cache_t* cache, const int32_t* seqs, co
  *   cu_new  int32 [n + 1], device, ascending; tokens that it leaves out or that are not below n_tokens are not read
  *   status  of dcp_cache_reserve (places that are not OK are left out), or NULL; a sequence is named by one place that is written
  *   k_new, v_new  [n_tokens, hkv, d] of the cache's dtype, strides as for k and v of dcp_tensors_t; not part of the cache;
- *                n_tokens at most 2^26 */
+ *                n_tokens at most 2^25 */
 dcp_status_t dcp_cache_append(const dcp_cache_t* cache, int32_t layer, const int32_t* seqs, const int32_t* cu_new, int32_t n,
                               const int32_t* status, const void* k_new, int64_t k_stride_t, int64_t k_stride_h,
                               const void* v_new, int64_t v_stride_t, int64_t v_stride_h, int64_t n_tokens, void* stream);

@@ -564,7 +564,7 @@ extern "C" dcp_status_t dcp_cache_append(const dcp_cache_t* cache, int32_t layer
   if ((st = check_places(c, seqs, n)) != DCP_OK) return st;
   if (layer < 0 || layer >= c.n_layers) return fail(DCP_ERR_INVALID_ARG, "layer out of range");
   if (n_tokens < 0) return fail(DCP_ERR_INVALID_ARG, "n_tokens must not be negative");
-  if (n_tokens > (1 << 26)) return fail(DCP_ERR_UNSUPPORTED, "dcp_cache_append covers at most 2^26 tokens");
+  if (n_tokens > (1 << 25)) return fail(DCP_ERR_UNSUPPORTED, "dcp_cache_append covers at most 2^25 tokens");   // 2^31 threads; a grid ends below 2^32
   if (!aligned(cu_new, 4) || !aligned(status, 4)) return fail(DCP_ERR_INVALID_ARG, "cu_new or status is misaligned");
   if (n == 0 || n_tokens == 0) return DCP_OK;
   if ((st = check_rows("k_new", k_new, k_st, k_sh, cache->d)) != DCP_OK) return st;

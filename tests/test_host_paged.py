@@ -94,6 +94,12 @@ def test_append_refuses():
                                     x["n_tokens"], None) == want, kw
 
 
+def test_append_refuses_more_tokens_than_a_grid_has_threads_for():
+    lib, c = _lib.load(), _cache()
+    for n_tokens in ((1 << 25) + 1, (1 << 26) - 3, 1 << 26):
+        assert lib.dcp_cache_append(_ref(c), 0, A, A, 3, None, A, 128, 64, A, 128, 64, n_tokens, None) == -4 and "2^25" in P.dcp_last_error()
+
+
 def test_attention_refuses():
     lib, c = _lib.load(), _cache()
     need = lib.dcp_paged_attn_workspace_bytes(_ref(c), 3, 4)
