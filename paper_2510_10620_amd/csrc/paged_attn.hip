@@ -579,7 +579,7 @@ struct Sets {
 static Sets sets_of(int32_t hkv, int32_t hq, int32_t d, int most_abreast) {
   const int32_t group = hq / hkv;
   Sets s;
-  s.per_kv = (group + kSetHeads - 1) / kSetHeads;
+  s.per_kv = (group - 1) / kSetHeads + 1;   // group up to 2^31 - 1
   s.heads = std::min(group, kSetHeads);
   const int64_t sets = (int64_t)hkv * s.per_kv;
   s.log_abreast = 0;
@@ -628,6 +628,7 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
   const int tile = cache->dtype == DCP_F32 ? 16 : 32;
   const int64_t most = ((t.window > 0 ? std::min<int64_t>(c.max_len, (int64_t)t.window + t.sink + 2 * tile) : c.max_len) + tile - 1) / tile;
   Sets sets = sets_of(c.hkv, t.hq, cache->d, kPagedWaves);
+  if (sets.groups * sets.abreast > (1 << 12)) return fail(DCP_ERR_UNSUPPORTED, "dcp_paged_attn_fwd covers at most 4 096 sets of 16 query heads on one KV head");
   bool whole = false;
   for (int abreast = 1; abreast <= sets.abreast && !whole; abreast *= 2) {
     const Sets x = sets_of(c.hkv, t.hq, cache->d, abreast);
@@ -636,7 +637,6 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
   }
   if (t.n * (int64_t)((c.max_len + tile - 1) / tile) * sets_of(c.hkv, t.hq, cache->d, 1).groups > INT32_MAX)
     return fail(DCP_ERR_UNSUPPORTED, "n x hkv x sets of 16 query heads on one KV head x tiles of 32 (fp32: 16) tokens in a row of the table must be below 2^31");
-  if (sets.groups * sets.abreast > (1 << 12)) return fail(DCP_ERR_UNSUPPORTED, "dcp_paged_attn_fwd covers at most 4 096 sets of 16 query heads on one KV head");
   c.k += t.layer * c.k_sl;   // the layer's
   c.v += t.layer * c.v_sl;
   const PagedArgs a{(const char*)t.q, (char*)t.out, t.lse, t.seqs, t.q_stride_t * e, t.q_stride_h * e, t.o_stride_t * e, t.o_stride_h * e,

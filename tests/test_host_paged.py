@@ -118,6 +118,16 @@ def test_attention_refuses():
     assert lib.dcp_paged_attn_fwd(_ref(c), ctypes.byref(_attn()), A + 128, need, None) == -5
 
 
+@pytest.mark.parametrize("hkv,hq", [(1, 2 ** 31 - 1), (1, 2 ** 31 - 15), (2, 2 ** 31 - 2), (2, 2 ** 17 + 2)])
+def test_attention_refuses_more_heads_than_it_can_count(hkv, hq):
+    """Sets of heads whose sums would leave 32 bits, and whose products with places and tiles 64."""
+    lib = _lib.load()
+    for c, n in ((_cache(hkv=hkv), 3), (_cache(hkv=hkv, max_pages=1 << 26), 16384)):
+        assert lib.dcp_paged_attn_workspace_bytes(_ref(c), n, hq) > 0
+        assert lib.dcp_paged_attn_fwd(_ref(c), ctypes.byref(_attn(hq=hq, n=n, out=1 << 62, o_stride_t=64)), A, 1 << 40, None) == -4
+        assert "4 096" in P.dcp_last_error()
+
+
 @pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
 def test_index_arithmetic_of_the_kernels(tmp_path):
     """csrc/paged.h on the CPU, under the undefined-behaviour sanitizer: tests/host_paged/driver.cpp."""
