@@ -13,13 +13,13 @@ static constexpr int kMapThreads = 1024, kMapWaves = kMapThreads / 64;
 static constexpr int kScan = 8;           // page_ref entries a lane has in flight
 static constexpr int kNoOwner = INT_MAX;
 
-// Inclusive sums over the workgroup, cut at `cap` (cutting is associative for numbers >= 0, and no sum passes 2^31).
+// Inclusive sums over the workgroup, cut at `cap`.
 __device__ __forceinline__ int block_sum(int x, int cap, int* wave_sum, int* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int y = __shfl_up(x, o);
-    if (lane >= o) x = min(x + y, cap);
+    if (lane >= o) x = add_capped(x, y, cap);
   }
   __syncthreads();
   if (lane == 63) wave_sum[wave] = x;
@@ -28,11 +28,11 @@ __device__ __forceinline__ int block_sum(int x, int cap, int* wave_sum, int* tot
 #pragma unroll
   for (int w = 0; w < kMapWaves; w++) {
     const int v = wave_sum[w];
-    if (w < wave) before = min(before + v, cap);
-    all = min(all + v, cap);
+    if (w < wave) before = add_capped(before, v, cap);
+    all = add_capped(all, v, cap);
   }
   *total = all;
-  return min(before + x, cap);
+  return add_capped(before, x, cap);
 }
 
 // What a place of dcp_cache_reserve (dcp_cache_fork) asks for: `need` pages for row `seq` of the table from entry `first` on,
@@ -118,8 +118,8 @@ __global__ __launch_bounds__(kMapThreads) void take_kernel(KCache c, const int32
     if (i < n) mine = base ? place_at<FORK>(c, a, b, i, owner) : place_of<FORK>(c, ask, i, owner);
     int all;
     const int x = block_sum(i < n ? min(mine.need, cap) : 0, cap, wave_sum, &all);
-    if (i < n) sums[i] = min(total + x, cap);
-    total = min(total + all, cap);
+    if (i < n) sums[i] = add_capped(total, x, cap);
+    total = add_capped(total, all, cap);
   }
   if (few) { seqs[tid] = mine.seq; firsts[tid] = mine.first; }
   __syncthreads();

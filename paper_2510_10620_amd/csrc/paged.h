@@ -25,6 +25,13 @@ inline FastDiv fast_div(uint32_t d) {
   return FastDiv{(uint32_t)(((uint64_t(1) << 32) * ((uint64_t(1) << s) - d)) / d + 1), s, d};
 }
 
+// x + y, cut at cap, for 0 <= x, y <= cap.  cap goes up to 2^30 + 1 (one more than the most pages of a cache): the sum fits into 32 bits without a
+// sign only.  Sums of more terms come out alike in any order.
+DCP_HD int32_t add_capped(int32_t x, int32_t y, int32_t cap) {
+  const uint32_t sum = (uint32_t)x + (uint32_t)y;
+  return sum < (uint32_t)cap ? (int32_t)sum : cap;
+}
+
 // dcp_cache_t by value, strides in bytes.
 struct KCache {
   char *k, *v;

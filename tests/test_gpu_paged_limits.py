@@ -1,0 +1,35 @@
+"""Calls on a paged cache at the ends of what they accept."""
+import ctypes
+
+import pytest
+
+import paper_2510_10620_amd as P
+from paper_2510_10620_amd import _lib
+from tests.test_gpu_paged import ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n_pages", [1 << 30, (1 << 30) - 1])
+def test_needs_whose_sum_passes_31_bits(n_pages):
+    """Two places that each want as many pages as a cache may have, of which three are free: neither is served, nothing changes."""
+    import torch
+    ref = torch.ones(n_pages, dtype=torch.int32, device="cuda")
+    ref[-3:] = 0
+    table, length, kv = torch.empty((2, n_pages), dtype=torch.int32, device="cuda"), ints([0, 0]), torch.zeros(64, device="cuda")
+    c = _lib.Cache()
+    c.n_layers, c.n_pages, c.page_size, c.hkv, c.d, c.dtype, c.n_seqs, c.max_pages = 1, n_pages, 1, 1, 32, P.DCP_BF16, 2, n_pages
+    for x in "kv":   # never followed here
+        setattr(c, x, kv.data_ptr())
+        for letter in "lpth":
+            setattr(c, f"{x}_stride_{letter}", 32)
+    c.page_ref, c.page_table, c.seq_len = ref.data_ptr(), table.data_ptr(), length.data_ptr()
+    status, new, stream = ints([7, 7]), ints([n_pages, n_pages]), torch.cuda.current_stream().cuda_stream
+    assert _lib.load().dcp_cache_reserve(ctypes.byref(c), None, new.data_ptr(), 2, status.data_ptr(), stream) == 0
+    assert status.tolist() == [P.DCP_PLACE_FULL] * 2 and length.tolist() == [0, 0]
+    assert int((ref == 0).sum()) == 3 and ref[-3:].tolist() == [0, 0, 0]
+    # what is there goes to the first that asks for no more
+    new.copy_(ints([3, n_pages]))
+    assert _lib.load().dcp_cache_reserve(ctypes.byref(c), None, new.data_ptr(), 2, status.data_ptr(), stream) == 0
+    assert status.tolist() == [P.DCP_PLACE_OK, P.DCP_PLACE_FULL] and length.tolist() == [3, 0]
+    assert table[0, :3].tolist() == [n_pages - 3, n_pages - 2, n_pages - 1] and ref[-3:].tolist() == [1, 1, 1]
