@@ -406,7 +406,7 @@ dcp_status_t dcp_comm_volume(const int32_t* cu_seqlens_host, int32_t n_seq, int3
  *
  * `seqs` (int32 [n], device) names the sequence of each place of a batch, or is NULL: place i is sequence i (n <= n_seqs).  A
  * place with a negative number is padding: nothing is read or written for it.  A number >= n_seqs is no sequence: the place
- * gets DCP_PLACE_BAD where the call has a status array and is padding elsewhere.  Page numbers outside [0, n_pages) and lengths outside
+ * gets DCP_PLACE_BAD where the call writes a status array and is padding elsewhere.  Page numbers outside [0, n_pages) and lengths outside
  * [0, max_pages * page_size] are never followed: such a page holds nothing, such a length is cut.
  * `status` (int32 [n], device) receives DCP_PLACE_*; a place that is not OK leaves its sequence and every page as they were (entries of
  * its row behind the pages that it holds may become -1).
@@ -465,8 +465,8 @@ dcp_status_t dcp_cache_compact(const dcp_cache_t* cache, int32_t* counts, void* 
 
 /* Attention of one new token per place over its sequence: the query is the token at position seq_len - 1 (appended already) and
  * sees key j iff j < seq_len and, with window > 0, seq_len - 1 - j < window or j < sink (the predicate of WINDOW rows; window 0: no
- * window).  A sequence may be named by several places; one that dcp_cache_reserve refused still ends at its last token: give such a
- * place as padding.  Keys in pages that do not exist are not seen.  Out and LSE as in dcp_block_attn_fwd: a place that sees no key gets
+ * window).  A sequence may be named by several places.  `status` (int32 [n], device, read) is that of dcp_cache_reserve, or NULL: a place
+ * that is not OK there has no token at seq_len - 1 and is padding.  Keys in pages that do not exist are not seen.  Out and LSE as in dcp_block_attn_fwd: a place that sees no key gets
  * O = 0, LSE = -inf; padding is not written.  Inf and NaN in q, k and v reach the places that see them and no others.  The same
  * call gives the same bits; the order of a place's sums goes by the lengths of the whole batch.
  *   q, out  [n, hq, d] of the cache's dtype, strides as in dcp_tensors_t; out must not overlap q;  lse float [hq, n] contiguous
@@ -481,6 +481,7 @@ typedef struct {
   const void* q; int64_t q_stride_t, q_stride_h;
   void* out;     int64_t o_stride_t, o_stride_h;
   float* lse;
+  const int32_t* status;      /* or NULL */
 } dcp_paged_attn_t;
 size_t dcp_paged_attn_workspace_bytes(const dcp_cache_t* cache, int32_t n, int32_t hq);
 dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t* args, void* workspace, size_t workspace_bytes, void* stream);

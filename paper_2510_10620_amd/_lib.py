@@ -64,6 +64,7 @@ class PagedAttn(ctypes.Structure):
         ("window", ctypes.c_int32), ("sink", ctypes.c_int32), ("seqs", vp),
         ("q", vp), ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
         ("out", vp), ("o_stride_t", ctypes.c_int64), ("o_stride_h", ctypes.c_int64), ("lse", vp),
+        ("status", vp),
     ]
 
 

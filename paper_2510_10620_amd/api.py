@@ -569,15 +569,16 @@ def dcp_paged_attn_workspace_bytes(cache, n, hq):
     return int(cache._lib.dcp_paged_attn_workspace_bytes(cache.ref, int(n), int(hq)))
 
 
-def dcp_paged_attn_fwd(cache, q, out, lse, softmax_scale, workspace, seqs=None, window=0, sink=0, layer=0):
-    """q, out [n, hq, d], lse float [hq, n]: one new token of each place over its sequence."""
+def dcp_paged_attn_fwd(cache, q, out, lse, softmax_scale, workspace, seqs=None, window=0, sink=0, layer=0, status=None):
+    """q, out [n, hq, d], lse float [hq, n]: one new token of each place over its sequence.  status: of dcp_cache_reserve; places that are
+    not OK are padding."""
     n, hq, d = q.shape
     if out.shape != q.shape or d != cache._d:
         raise ValueError("q, out: [n, hq, d] with the cache's d")
     if lse.dtype is not cache._f32 or lse.shape != (hq, n) or not lse.is_contiguous() or lse.get_device() != cache._index:
         raise ValueError("lse: contiguous float32 tensor [hq, n] on the cache's device")
     args = _lib.PagedAttn(n, hq, layer, softmax_scale, window, sink, cache._ints("seqs", seqs, n), *cache._token_rows("q", q),
-                          *cache._token_rows("out", out), lse.data_ptr())
+                          *cache._token_rows("out", out), lse.data_ptr(), cache._ints("status", status, n))
     _check(cache._lib.dcp_paged_attn_fwd(cache.ref, ctypes.byref(args), *cache._space(workspace), cache._stream()))
 
 

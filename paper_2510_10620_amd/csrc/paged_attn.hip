@@ -13,7 +13,7 @@ struct PagedArgs {
   const char* q;
   char* out;
   float* lse;
-  const int32_t* seqs;
+  const int32_t *seqs, *status;
   int64_t q_st, q_sh, o_st, o_sh;   // bytes
   int32_t n, group, window, sink;   // group: query heads of a KV head
   // Query heads that share a KV head are taken in sets of up to 16 (or 8, see Tile::weigh); a workgroup's waves take `abreast` (1, 2 or 4) sets
@@ -274,7 +274,11 @@ template <typename TT, bool GROUPED> struct Where {
   }
 };
 
-__device__ __forceinline__ int32_t seq_at(const PagedArgs& a, int i) { return a.seqs ? a.seqs[i] : i; }
+// A place that is not OK is padding.
+__device__ __forceinline__ int32_t seq_at(const PagedArgs& a, int i) {
+  const int32_t seq = a.seqs ? a.seqs[i] : i, code = a.status ? a.status[i] : DCP_PLACE_OK;
+  return code == DCP_PLACE_OK ? seq : -1;
+}
 
 // O = sum_j exp(s_j - m) v_j / l, LSE = m + ln l with m = max_j s_j, l = sum_j exp(s_j - m) over the keys j that the place sees, in one pass: m, l and
 // O are carried along in fp32 (the weights too: fp32, or two bf16 parts), and rescaled where m grows.
@@ -614,6 +618,7 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
   if ((st = check_rows("q", t.q, t.q_stride_t, t.q_stride_h, cache->d)) != DCP_OK) return st;
   if ((st = check_rows("out", t.out, t.o_stride_t, t.o_stride_h, cache->d)) != DCP_OK) return st;
   if (!t.lse || (reinterpret_cast<uintptr_t>(t.lse) & 3u)) return fail(DCP_ERR_INVALID_ARG, "lse is NULL or misaligned");
+  if (reinterpret_cast<uintptr_t>(t.status) & 3u) return fail(DCP_ERR_INVALID_ARG, "status is misaligned");
   if (!workspace || workspace_bytes < dcp_paged_attn_workspace_bytes(cache, t.n, t.hq))
     return fail(DCP_ERR_WORKSPACE, "workspace is NULL or smaller than dcp_paged_attn_workspace_bytes");
   if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(DCP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
@@ -639,7 +644,7 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
     return fail(DCP_ERR_UNSUPPORTED, "n x hkv x sets of 16 query heads on one KV head x tiles of 32 (fp32: 16) tokens in a row of the table must be below 2^31");
   c.k += t.layer * c.k_sl;   // the layer's
   c.v += t.layer * c.v_sl;
-  const PagedArgs a{(const char*)t.q, (char*)t.out, t.lse, t.seqs, t.q_stride_t * e, t.q_stride_h * e, t.o_stride_t * e, t.o_stride_h * e,
+  const PagedArgs a{(const char*)t.q, (char*)t.out, t.lse, t.seqs, t.status, t.q_stride_t * e, t.q_stride_h * e, t.o_stride_t * e, t.o_stride_h * e,
                     t.n, t.hq / c.hkv, t.window, t.sink, sets.per_kv, sets.heads, sets.abreast, sets.log_abreast, (int32_t)sets.groups, whole,
                     t.softmax_scale * 1.44269504088896340736f};
   PagedParts parts;

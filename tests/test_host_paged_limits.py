@@ -1,9 +1,14 @@
 """Arithmetic of the calls on a paged cache at the limits that the host accepts, on the CPU under the undefined-behaviour sanitizer."""
+import ctypes
 import os
 import shutil
 import subprocess
 
 import pytest
+
+import paper_2510_10620_amd as P
+from paper_2510_10620_amd import _lib
+from tests.test_host_paged import A, _attn, _cache, _ref
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -19,8 +24,14 @@ def _run(tmp_path, name):
     assert r.returncode == 0 and f"host-paged {name} ok" in r.stdout, r.stdout[-2000:] + r.stderr[-3000:]
 
 
-pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+gxx = pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
 
 
+@gxx
 def test_sums_of_needs_up_to_the_most_pages(tmp_path):
     _run(tmp_path, "sums")
+
+
+def test_attention_refuses_a_misaligned_status():
+    assert _lib.load().dcp_paged_attn_fwd(_ref(_cache()), ctypes.byref(_attn(status=A + 2)), A, 1 << 30, None) == P.DCP_ERR_INVALID_ARG
+    assert "status" in P.dcp_last_error()
