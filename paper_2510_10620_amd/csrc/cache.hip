@@ -50,7 +50,7 @@ __device__ __forceinline__ Asked asked_at(const KCache& c, const int32_t* a, con
   Asked x{a ? a[i] : i, 1, 0, 0};
   if (FORK || b) x.t = b[i];
   if (c.is_seq(x.s)) x.len = c.length(x.s);
-  if (FORK && c.is_seq(x.t)) x.len_t = c.len[x.t];
+  if (FORK && c.is_seq(x.t)) x.len_t = c.length(x.t);
   return x;
 }
 

@@ -33,3 +33,25 @@ def test_needs_whose_sum_passes_31_bits(n_pages):
     assert _lib.load().dcp_cache_reserve(ctypes.byref(c), None, new.data_ptr(), 2, status.data_ptr(), stream) == 0
     assert status.tolist() == [P.DCP_PLACE_OK, P.DCP_PLACE_FULL] and length.tolist() == [3, 0]
     assert table[0, :3].tolist() == [n_pages - 3, n_pages - 2, n_pages - 1] and ref[-3:].tolist() == [1, 1, 1]
+
+
+@pytest.mark.parametrize("lens", [[-1], [-5, 0, -(1 << 31)]])
+def test_fork_into_sequences_of_negative_length(lens):
+    """A length below 0 is cut to 0 in every call: such a sequence is empty, and may be forked into as it may be grown."""
+    import torch
+    cache = P.Cache.empty(2, 12, 8, 2, 32, 6, 3, torch.bfloat16)
+    cache.k.normal_()
+    cache.v.normal_()
+    status = ints([7])
+    P.dcp_cache_reserve(cache, ints([5]), status, n_new=ints([11]))
+    for i, n in enumerate(lens):
+        cache.seq_len[i] = n
+    status = ints([7] * len(lens))
+    P.dcp_cache_fork(cache, ints([5] * len(lens)), ints(range(len(lens))), status)
+    assert status.tolist() == [P.DCP_PLACE_OK] * len(lens)
+    assert cache.seq_len.tolist() == [11] * len(lens) + [0] * (5 - len(lens)) + [11]
+    pages = cache.page_table.cpu()
+    for i in range(len(lens)):
+        assert pages[i, 0] == pages[5, 0] == 0 and pages[i, 1] == 2 + i
+        assert torch.equal(cache.k[:, 2 + i, :3], cache.k[:, 1, :3]) and torch.equal(cache.v[:, 2 + i, :3], cache.v[:, 1, :3])
+    assert cache.page_ref.tolist() == [1 + len(lens), 1] + [1] * len(lens) + [0] * (10 - len(lens))
