@@ -469,7 +469,8 @@ dcp_status_t dcp_cache_compact(const dcp_cache_t* cache, int32_t* counts, void* 
  * that is not OK there has no token at seq_len - 1 and is padding.  Keys in pages that do not exist are not seen.  Out and LSE as in dcp_block_attn_fwd: a place that sees no key gets
  * O = 0, LSE = -inf; padding is not written.  Inf and NaN in q, k and v reach the places that see them and no others.  The same
  * call gives the same bits; the order of a place's sums goes by the lengths of the whole batch.
- *   q, out  [n, hq, d] of the cache's dtype, strides as in dcp_tensors_t; out must not overlap q;  lse float [hq, n] contiguous
+ *   q, out  [n, hq, d] of the cache's dtype, strides as in dcp_tensors_t; out must not overlap q (rows of it between those of q: with the
+ *              same strides only);  lse float [hq, n] contiguous
  *   workspace  device, >= dcp_paged_attn_workspace_bytes, 256-byte aligned; scratch, whatever it holds: calls that may run at the same
  *              time need one each.  One launch or two.
  * DCP_ERR_UNSUPPORTED: hkv * ceil(hq / hkv / 16) above 4 096; that times n times ceil(max_pages * page_size / 32) (fp32: 16) of 2^31 or more. */

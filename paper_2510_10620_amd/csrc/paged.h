@@ -88,4 +88,31 @@ template <int LOG> struct Shares {
   }
 };
 
+// A tensor [n, heads] of rows of `row` bytes, strides in bytes and positive.
+struct Rows {
+  const void* p;
+  int64_t st, sh;
+};
+// Whether a row of x shares a byte with a row of y, both [n, heads].  With the same strides: rows (i, h) of x and (i + a, h + b) of y lie
+// y - x + a st + b sh apart, and for every a (or every b, whichever are fewer) the nearest two b decide.  With others: whether the rows of the one
+// begin before the other's end and the other way round, which tensors between whose rows the other's lie do as well.
+inline bool rows_overlap(const Rows& x, const Rows& y, int32_t n, int32_t heads, int64_t row) {
+  typedef __int128 Wide;   // strides may be anything
+  const Wide apart = (Wide)(int64_t)((uintptr_t)y.p - (uintptr_t)x.p);
+  if (apart >= (Wide)(n - 1) * x.st + (Wide)(heads - 1) * x.sh + row || -apart >= (Wide)(n - 1) * y.st + (Wide)(heads - 1) * y.sh + row) return false;
+  if ((n > 1 && x.st != y.st) || (heads > 1 && x.sh != y.sh)) return true;
+  const bool by_token = n <= heads;
+  const int32_t outer = by_token ? n : heads, inner = by_token ? heads : n;
+  const int64_t so = by_token ? x.st : x.sh, si = by_token ? x.sh : x.st;
+  for (int64_t a = 1 - (int64_t)outer; a < outer; a++) {
+    const Wide d = apart + (Wide)a * so;
+    Wide b = -d / si;
+    for (Wide near = b - 1; near <= b + 1; near++) {
+      const Wide at = d + near * si;
+      if (near > -inner && near < inner && at < row && -at < row) return true;
+    }
+  }
+  return false;
+}
+
 }  // namespace dcp

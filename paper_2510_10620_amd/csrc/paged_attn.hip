@@ -623,12 +623,8 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
     return fail(DCP_ERR_WORKSPACE, "workspace is NULL or smaller than dcp_paged_attn_workspace_bytes");
   if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(DCP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   const int64_t e = cache->dtype == DCP_BF16 ? 2 : 4;
-  {
-    const char *q0 = (const char*)t.q, *o0 = (const char*)t.out;
-    const char* q1 = q0 + ((t.n - 1) * t.q_stride_t + (t.hq - 1) * t.q_stride_h + cache->d) * e;
-    const char* o1 = o0 + ((t.n - 1) * t.o_stride_t + (t.hq - 1) * t.o_stride_h + cache->d) * e;
-    if (q0 < o1 && o0 < q1) return fail(DCP_ERR_INVALID_ARG, "out overlaps q");
-  }
+  if (rows_overlap(Rows{t.q, t.q_stride_t * e, t.q_stride_h * e}, Rows{t.out, t.o_stride_t * e, t.o_stride_h * e}, t.n, t.hq, cache->d * e))
+    return fail(DCP_ERR_INVALID_ARG, "out overlaps q");
   // Whole items: the most tiles that one can have, as far as the host knows, over the waves that take them in turn
   const int tile = cache->dtype == DCP_F32 ? 16 : 32;
   const int64_t most = ((t.window > 0 ? std::min<int64_t>(c.max_len, (int64_t)t.window + t.sink + 2 * tile) : c.max_len) + tile - 1) / tile;

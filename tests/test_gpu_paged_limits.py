@@ -5,7 +5,7 @@ import pytest
 
 import paper_2510_10620_amd as P
 from paper_2510_10620_amd import _lib
-from tests.test_gpu_paged import ints
+from tests.test_gpu_paged import NAN, attend, check, ints, make_cache, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,41 @@ def test_fork_into_sequences_of_negative_length(lens):
         assert pages[i, 0] == pages[5, 0] == 0 and pages[i, 1] == 2 + i
         assert torch.equal(cache.k[:, 2 + i, :3], cache.k[:, 1, :3]) and torch.equal(cache.v[:, 2 + i, :3], cache.v[:, 1, :3])
     assert cache.page_ref.tolist() == [1 + len(lens), 1] + [1] * len(lens) + [0] * (10 - len(lens))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["beside", "halves", "heads first", "other heads"])
+def test_queries_and_outputs_in_one_buffer(dtype, layout):
+    """Outputs that lie between the queries of one buffer, and that overlap them by one row."""
+    import torch
+    n, hq, d = 5, 4, 64
+    cache, names = make_cache([70, 1, 333, 16, 0], 32, 2, d, dtype, seed=5)
+    places = [int(s) for s in names]
+    rand = randn((n, 2, hq, d), dtype, 6)
+    if layout == "beside":          # [n, 2, hq, d]: a token's queries, then its outputs
+        q, out = rand[:, 0], rand[:, 1]
+        bad = rand.view(n, 2 * hq, d)[:, 1: hq + 1]
+    elif layout == "halves":        # [n, hq, 2 d]: a head's query, then its output
+        both = rand.view(n, hq, 2 * d)
+        q, out = both[:, :, :d], both[:, :, d:]
+        bad = both[:, :, d // 2: d // 2 + d]
+    elif layout == "heads first":   # [2 hq, n, d]
+        both = rand.view(2 * hq, n, d).transpose(0, 1)
+        q, out = both[:, :hq], both[:, hq:]
+        bad = both[:, 1: hq + 1]
+    else:                           # every other head
+        both = rand.view(n, 2 * hq, d)
+        q, out = both[:, ::2], both[:, 1::2]
+        bad = q
+    kept = q.clone()
+    out.fill_(NAN)
+    lse, ws = torch.full((hq, n), NAN, device="cuda"), torch.empty(P.dcp_paged_attn_workspace_bytes(cache, n, hq), dtype=torch.uint8, device="cuda")
+    P.dcp_paged_attn_fwd(cache, q, out, lse, 0.1, ws, seqs=ints(names))
+    torch.cuda.synchronize()
+    assert torch.equal(q, kept)
+    check(cache, kept, out, lse, 0.1, places)
+    want, want_l = attend(cache, kept, 0.1, ints(names))
+    assert torch.equal(out, want) and torch.equal(lse, want_l)
+    with pytest.raises(P.DcpError) as ei:
+        P.dcp_paged_attn_fwd(cache, q, bad, lse, 0.1, ws, seqs=ints(names))
+    assert ei.value.status == P.DCP_ERR_INVALID_ARG and "overlaps" in str(ei.value)

@@ -32,6 +32,11 @@ def test_sums_of_needs_up_to_the_most_pages(tmp_path):
     _run(tmp_path, "sums")
 
 
+@gxx
+def test_queries_and_outputs_that_share_bytes(tmp_path):
+    _run(tmp_path, "overlap")
+
+
 def test_attention_refuses_a_misaligned_status():
     assert _lib.load().dcp_paged_attn_fwd(_ref(_cache()), ctypes.byref(_attn(status=A + 2)), A, 1 << 30, None) == P.DCP_ERR_INVALID_ARG
     assert "status" in P.dcp_last_error()
