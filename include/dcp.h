@@ -410,8 +410,8 @@ dcp_status_t dcp_comm_volume(const int32_t* cu_seqlens_host, int32_t n_seq, int3
  * [0, max_pages * page_size] are never followed: such a page holds nothing, such a length is cut.
  * `status` (int32 [n], device) receives DCP_PLACE_*; a place that is not OK leaves its sequence and every page as they were (entries of
  * its row behind the pages that it holds may become -1).
- * At most DCP_CACHE_MAX_SEQS sequences in a cache and places in a call, 2^30 tokens in a row of the table; n == 0 is legal.  Calls that change one cache, and
- * those that read it meanwhile, must be ordered (one stream, or events).  Errors of the host's checks as elsewhere. */
+ * At most DCP_CACHE_MAX_SEQS sequences in a cache and places in a call, 2^30 pages, 2^30 tokens in a row of the table, 2^16 layers, strides of
+ * 2^58 elements; n == 0 is legal.  Calls that change one cache, and those that read it meanwhile, must be ordered (one stream, or events).  Errors of the host's checks as elsewhere. */
 #define DCP_CACHE_MAX_SEQS 16384
 typedef enum {
   DCP_PLACE_OK = 0,    /* done, or padding                                                                   */

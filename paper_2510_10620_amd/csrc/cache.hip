@@ -484,6 +484,11 @@ __global__ __launch_bounds__(256) void append_kernel(KCache c, int32_t layer, co
 }
 
 // ------------------------------------------------------------------------------------------------ host
+// Strides in bytes, and the pieces that the calls copy, are counted in 64 bits: no stride beyond 2^58 elements (2^60 bytes), no more than 2^16 layers
+// (of up to 2^30 pages of 2^16 pieces of k and of v).
+static constexpr int64_t kMostStride = int64_t(1) << 58;
+static constexpr int32_t kMostLayers = 1 << 16;
+
 static bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 dcp_status_t check_rows(const char* name, const void* p, int64_t stride_t, int64_t stride_h, int32_t d) {
@@ -491,6 +496,7 @@ dcp_status_t check_rows(const char* name, const void* p, int64_t stride_t, int64
   if (!aligned(p, 16)) return fail(DCP_ERR_INVALID_ARG, std::string(name) + " must be 16-byte aligned");
   if (stride_h < d || stride_t < d || stride_h % 8 || stride_t % 8)
     return fail(DCP_ERR_INVALID_ARG, std::string(name) + ": strides must be >= d and multiples of 8 elements");
+  if (std::max(stride_t, stride_h) > kMostStride) return fail(DCP_ERR_UNSUPPORTED, std::string(name) + ": strides of at most 2^58 elements");
   return DCP_OK;
 }
 
@@ -502,6 +508,7 @@ dcp_status_t pack_cache(const dcp_cache_t* cache, KCache* out) {
   if (c.dtype != DCP_BF16 && c.dtype != DCP_F32) return fail(DCP_ERR_UNSUPPORTED, "dtype must be DCP_BF16 or DCP_F32");
   if (c.d != 32 && c.d != 64 && c.d != 128) return fail(DCP_ERR_UNSUPPORTED, "head_dim of a cache must be 32, 64 or 128");
   if (c.n_seqs > DCP_CACHE_MAX_SEQS) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most " + std::to_string(DCP_CACHE_MAX_SEQS) + " sequences");
+  if (c.n_layers > kMostLayers) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most 65 536 layers");
   if (c.n_pages > (1 << 30)) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most 2^30 pages");
   if ((int64_t)c.max_pages * c.page_size > (1 << 30)) return fail(DCP_ERR_UNSUPPORTED, "max_pages * page_size must be at most 2^30");
   const int32_t e = c.dtype == DCP_BF16 ? 2 : 4;
@@ -512,6 +519,8 @@ dcp_status_t pack_cache(const dcp_cache_t* cache, KCache* out) {
     if (!x.p || !aligned(x.p, 16)) return fail(DCP_ERR_INVALID_ARG, std::string(x.name) + " of the cache is NULL or not 16-byte aligned");
     if (x.l < c.d || x.page < c.d || x.t < c.d || x.h < c.d || x.l % 8 || x.page % 8 || x.t % 8 || x.h % 8)
       return fail(DCP_ERR_INVALID_ARG, std::string(x.name) + " of the cache: strides must be >= d and multiples of 8 elements");
+    if (std::max(std::max(x.l, x.page), std::max(x.t, x.h)) > kMostStride)
+      return fail(DCP_ERR_UNSUPPORTED, std::string(x.name) + " of the cache: strides of at most 2^58 elements");
   }
   if (!c.page_ref || !c.page_table || !c.seq_len || !aligned(c.page_ref, 4) || !aligned(c.page_table, 4) || !aligned(c.seq_len, 4))
     return fail(DCP_ERR_INVALID_ARG, "page_ref, page_table or seq_len is NULL or misaligned");
