@@ -1,8 +1,6 @@
 // The calls that change a paged key-value cache: pages are taken, shared, given back and moved to the front, and new
 // tokens are written into them.  Everything is decided on the device from page_ref, page_table and seq_len, so that a
 // decoding step never waits for the host.
-#include <algorithm>
-
 #include "cache_internal.h"
 
 using namespace dcp;
@@ -219,14 +217,6 @@ __device__ __forceinline__ void copy_chunks(const KCache& c, char* base, int64_t
   }
 }
 
-// What a workgroup copies at a time: kPieceChunks chunks (16 KiB) of a page, so that pages that are filled unevenly, or few, still fill the chip
-// (64 sequences forked, 4 layers, pages of 512 KiB: 93 us with a workgroup a page, 47 so).
-static constexpr int kPieceChunks = 1024;
-// Workgroups that share such pieces, each taking every kCopyWorkers-th: 2 430 pages of 512 KiB moved, 5.1 GB read and written, in 995 us with
-// 4 096, 980 with 16 384 and 64 KiB at a time, 842 to 960 (by where the pages lie) so: 5.3 to 6.0 TB/s.
-static constexpr int kCopyWorkers = 32768;
-inline int pieces_of(const KCache& c) { return (int)(((int64_t)c.page.d * c.hkv * c.head_chunks() + kPieceChunks - 1) / kPieceChunks); }
-
 // After take_kernel.  Of place i's units the first shares its whole pages, unit 1 + x copies a piece of the page being filled, x = 2 (layer pieces
 // + piece) + (0: k, 1: v).
 __global__ __launch_bounds__(256) void fork_kernel(KCache c, const int32_t* __restrict__ src, const int32_t* __restrict__ dst, int32_t n,
@@ -274,11 +264,6 @@ __global__ __launch_bounds__(256) void free_kernel(KCache c, const int32_t* __re
     if (c.is_page(page)) atomicSub(&c.ref[page], 1);
   }
 }
-
-// What the two launches of dcp_cache_compact share: the pages that move, and where every page goes.
-struct Moves {
-  int32_t *count, *from, *to, *where;   // [1], [n_pages / 2 + 1], [n_pages / 2 + 1], [n_pages]: of the pages behind those in use, -1: free
-};
 
 // One workgroup: counts the pages in use (u), then lists the free ones before u and the used ones behind it, which are as many.  Bound by
 // latency: page_ref is read twice, 8 192 pages at a time (the second time from the cache), once if there are no more; the lists of so
@@ -401,12 +386,6 @@ __global__ __launch_bounds__(256) void move_kernel(KCache c, Moves m, const int3
   }
 }
 
-struct NewTokens {
-  const char *k, *v;
-  int64_t k_st, k_sh, v_st, v_sh;   // bytes
-  int64_t n;
-};
-
 // A workgroup writes TOKENS tokens: their places in the cache are found by a thread each, then all threads copy, four chunks in flight.  HBM-bound
 // where there are many (83 396 tokens of 4 KiB 111 us, 6.1 TB/s read and written); few take a workgroup each and are bound by the trips
 // to memory: cu_new, seqs, seq_len, page_table, the tokens.
@@ -483,164 +462,27 @@ __global__ __launch_bounds__(256) void append_kernel(KCache c, int32_t layer, co
   }
 }
 
-// ------------------------------------------------------------------------------------------------ host
-// Strides in bytes, and the pieces that the calls copy, are counted in 64 bits: no stride beyond 2^58 elements (2^60 bytes), no more than 2^16 layers
-// (of up to 2^30 pages of 2^16 pieces of k and of v).
-static constexpr int64_t kMostStride = int64_t(1) << 58;
-static constexpr int32_t kMostLayers = 1 << 16;
-
-static bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-dcp_status_t check_rows(const char* name, const void* p, int64_t stride_t, int64_t stride_h, int32_t d) {
-  if (!p) return fail(DCP_ERR_INVALID_ARG, std::string(name) + " is NULL");
-  if (!aligned(p, 16)) return fail(DCP_ERR_INVALID_ARG, std::string(name) + " must be 16-byte aligned");
-  if (stride_h < d || stride_t < d || stride_h % 8 || stride_t % 8)
-    return fail(DCP_ERR_INVALID_ARG, std::string(name) + ": strides must be >= d and multiples of 8 elements");
-  if (std::max(stride_t, stride_h) > kMostStride) return fail(DCP_ERR_UNSUPPORTED, std::string(name) + ": strides of at most 2^58 elements");
-  return DCP_OK;
+// ------------------------------------------------------------------------------------------------ launches
+void launch_take(bool fork, const KCache& c, const int32_t* a, const int32_t* b, int32_t n, int32_t* status, hipStream_t s) {
+  if (!fork) hipLaunchKernelGGL(take_kernel<false>, dim3(1), dim3(kMapThreads), 0, s, c, a, b, n, status);
+  else hipLaunchKernelGGL(take_kernel<true>, dim3(1), dim3(kMapThreads), 0, s, c, a, b, n, status);
 }
-
-dcp_status_t pack_cache(const dcp_cache_t* cache, KCache* out) {
-  if (!cache) return fail(DCP_ERR_INVALID_ARG, "cache is NULL");
-  const dcp_cache_t& c = *cache;
-  if (c.n_layers <= 0 || c.n_pages <= 0 || c.page_size <= 0 || c.hkv <= 0 || c.d <= 0 || c.n_seqs <= 0 || c.max_pages <= 0)
-    return fail(DCP_ERR_INVALID_ARG, "n_layers, n_pages, page_size, hkv, d, n_seqs, max_pages must be positive");
-  if (c.dtype != DCP_BF16 && c.dtype != DCP_F32) return fail(DCP_ERR_UNSUPPORTED, "dtype must be DCP_BF16 or DCP_F32");
-  if (c.d != 32 && c.d != 64 && c.d != 128) return fail(DCP_ERR_UNSUPPORTED, "head_dim of a cache must be 32, 64 or 128");
-  if (c.n_seqs > DCP_CACHE_MAX_SEQS) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most " + std::to_string(DCP_CACHE_MAX_SEQS) + " sequences");
-  if (c.n_layers > kMostLayers) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most 65 536 layers");
-  if (c.n_pages > (1 << 30)) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most 2^30 pages");
-  if ((int64_t)c.max_pages * c.page_size > (1 << 30)) return fail(DCP_ERR_UNSUPPORTED, "max_pages * page_size must be at most 2^30");
-  const int32_t e = c.dtype == DCP_BF16 ? 2 : 4;
-  if ((int64_t)c.page_size * c.hkv * (c.d * e / 16) > (1 << 26)) return fail(DCP_ERR_UNSUPPORTED, "a page holds at most 1 GiB of keys");
-  struct { const char* name; const void* p; int64_t l, page, t, h; } kv[2] = {{"k", c.k, c.k_stride_l, c.k_stride_p, c.k_stride_t, c.k_stride_h},
-                                                                              {"v", c.v, c.v_stride_l, c.v_stride_p, c.v_stride_t, c.v_stride_h}};
-  for (auto& x : kv) {
-    if (!x.p || !aligned(x.p, 16)) return fail(DCP_ERR_INVALID_ARG, std::string(x.name) + " of the cache is NULL or not 16-byte aligned");
-    if (x.l < c.d || x.page < c.d || x.t < c.d || x.h < c.d || x.l % 8 || x.page % 8 || x.t % 8 || x.h % 8)
-      return fail(DCP_ERR_INVALID_ARG, std::string(x.name) + " of the cache: strides must be >= d and multiples of 8 elements");
-    if (std::max(std::max(x.l, x.page), std::max(x.t, x.h)) > kMostStride)
-      return fail(DCP_ERR_UNSUPPORTED, std::string(x.name) + " of the cache: strides of at most 2^58 elements");
-  }
-  if (!c.page_ref || !c.page_table || !c.seq_len || !aligned(c.page_ref, 4) || !aligned(c.page_table, 4) || !aligned(c.seq_len, 4))
-    return fail(DCP_ERR_INVALID_ARG, "page_ref, page_table or seq_len is NULL or misaligned");
-  KCache k{};
-  k.k = (char*)c.k; k.v = (char*)c.v;
-  k.k_sl = c.k_stride_l * e; k.k_sp = c.k_stride_p * e; k.k_st = c.k_stride_t * e; k.k_sh = c.k_stride_h * e;
-  k.v_sl = c.v_stride_l * e; k.v_sp = c.v_stride_p * e; k.v_st = c.v_stride_t * e; k.v_sh = c.v_stride_h * e;
-  k.ref = c.page_ref; k.table = c.page_table; k.len = c.seq_len;
-  k.n_layers = c.n_layers; k.n_pages = c.n_pages; k.hkv = c.hkv; k.n_seqs = c.n_seqs; k.max_pages = c.max_pages;
-  k.max_len = c.max_pages * c.page_size;
-  for (k.log_head_chunks = 2; (16 << k.log_head_chunks) < c.d * e; k.log_head_chunks++) {}
-  k.page = fast_div((uint32_t)c.page_size);
-  k.heads = fast_div((uint32_t)c.hkv);
-  *out = k;
-  return DCP_OK;
+void launch_fork(uint32_t grid, const KCache& c, const int32_t* src, const int32_t* dst, int32_t n, const int32_t* status, int32_t pieces, hipStream_t s) {
+  hipLaunchKernelGGL(fork_kernel, dim3(grid), dim3(256), 0, s, c, src, dst, n, status, pieces);
 }
-
-dcp_status_t check_places(const KCache& c, const int32_t* seqs, int32_t n) {
-  if (n < 0) return fail(DCP_ERR_INVALID_ARG, "n must not be negative");
-  if (n > DCP_CACHE_MAX_SEQS) return fail(DCP_ERR_UNSUPPORTED, "a call has at most " + std::to_string(DCP_CACHE_MAX_SEQS) + " places");
-  if (!seqs && n > c.n_seqs) return fail(DCP_ERR_INVALID_ARG, "seqs is NULL and n is more than the cache's sequences");
-  if (!aligned(seqs, 4)) return fail(DCP_ERR_INVALID_ARG, "seqs is misaligned");
-  return DCP_OK;
+void launch_free(uint32_t grid, const KCache& c, const int32_t* seqs, hipStream_t s) {
+  hipLaunchKernelGGL(free_kernel, dim3(grid), dim3(256), 0, s, c, seqs);
 }
-
-static size_t moves_bytes(int32_t n_pages) { return 4 * (64 + 2 * (size_t)n_pages + 2); }   // count, from and to (n_pages / 2 + 1 each), where
+void launch_list_moves(const KCache& c, const Moves& m, int32_t* counts, hipStream_t s) {
+  hipLaunchKernelGGL(list_moves_kernel, dim3(1), dim3(kMapThreads), 0, s, c, m, counts);
+}
+void launch_move(uint32_t grid, const KCache& c, const Moves& m, const int32_t* counts, int32_t pieces, hipStream_t s) {
+  hipLaunchKernelGGL(move_kernel, dim3(grid), dim3(256), 0, s, c, m, counts, pieces);
+}
+void launch_append(int32_t each, uint32_t grid, const KCache& c, int32_t layer, const int32_t* seqs, const int32_t* cu, int32_t n, const int32_t* status,
+                   const NewTokens& x, hipStream_t s) {
+  if (each == 1) hipLaunchKernelGGL(append_kernel<1>, dim3(grid), dim3(256), 0, s, c, layer, seqs, cu, n, status, x);
+  else hipLaunchKernelGGL(append_kernel<4>, dim3(grid), dim3(256), 0, s, c, layer, seqs, cu, n, status, x);
+}
 
 }  // namespace dcp
-
-extern "C" dcp_status_t dcp_cache_reserve(const dcp_cache_t* cache, const int32_t* seqs, const int32_t* n_new, int32_t n,
-                                          int32_t* status, void* stream) {
-  KCache c;
-  dcp_status_t st = pack_cache(cache, &c);
-  if (st != DCP_OK) return st;
-  if ((st = check_places(c, seqs, n)) != DCP_OK) return st;
-  if (n == 0) return DCP_OK;
-  if (!status || !aligned(status, 4) || !aligned(n_new, 4)) return fail(DCP_ERR_INVALID_ARG, "status is NULL, or status or n_new misaligned");
-  ProfScope ps(DCP_K_CACHE, (hipStream_t)stream);
-  hipLaunchKernelGGL(take_kernel<false>, dim3(1), dim3(kMapThreads), 0, (hipStream_t)stream, c, seqs, n_new, n, status);
-  DCP_HIP_TRY(hipGetLastError());
-  return DCP_OK;
-}
-
-extern "C" dcp_status_t dcp_cache_append(const dcp_cache_t* cache, int32_t layer, const int32_t* seqs, const int32_t* cu_new, int32_t n,
-                                         const int32_t* status, const void* k_new, int64_t k_st, int64_t k_sh, const void* v_new,
-                                         int64_t v_st, int64_t v_sh, int64_t n_tokens, void* stream) {
-  KCache c;
-  dcp_status_t st = pack_cache(cache, &c);
-  if (st != DCP_OK) return st;
-  if ((st = check_places(c, seqs, n)) != DCP_OK) return st;
-  if (layer < 0 || layer >= c.n_layers) return fail(DCP_ERR_INVALID_ARG, "layer out of range");
-  if (n_tokens < 0) return fail(DCP_ERR_INVALID_ARG, "n_tokens must not be negative");
-  if (n_tokens > (1 << 25)) return fail(DCP_ERR_UNSUPPORTED, "dcp_cache_append covers at most 2^25 tokens");   // 2^31 threads; a grid ends below 2^32
-  if (!aligned(cu_new, 4) || !aligned(status, 4)) return fail(DCP_ERR_INVALID_ARG, "cu_new or status is misaligned");
-  if (n == 0 || n_tokens == 0) return DCP_OK;
-  if ((st = check_rows("k_new", k_new, k_st, k_sh, cache->d)) != DCP_OK) return st;
-  if ((st = check_rows("v_new", v_new, v_st, v_sh, cache->d)) != DCP_OK) return st;
-  const int64_t e = cache->dtype == DCP_BF16 ? 2 : 4;
-  const NewTokens x{(const char*)k_new, (const char*)v_new, k_st * e, k_sh * e, v_st * e, v_sh * e, n_tokens};
-  ProfScope ps(DCP_K_CACHE, (hipStream_t)stream);
-  // up to four tokens a CU a workgroup each (64 tokens 6.4 -> 4.3 us against eight in one), else four in one (83 396 tokens in 2 / 4 / 8 / 16:
-  // 123 / 124 / 130 / 134 us with the reserve and the map's reset)
-  if (n_tokens <= 1024) hipLaunchKernelGGL(append_kernel<1>, dim3((unsigned)n_tokens), dim3(256), 0, (hipStream_t)stream, c, layer, seqs, cu_new, n, status, x);
-  else hipLaunchKernelGGL(append_kernel<4>, dim3((unsigned)((n_tokens + 3) / 4)), dim3(256), 0, (hipStream_t)stream, c, layer, seqs, cu_new, n, status, x);
-  DCP_HIP_TRY(hipGetLastError());
-  return DCP_OK;
-}
-
-extern "C" dcp_status_t dcp_cache_fork(const dcp_cache_t* cache, const int32_t* src, const int32_t* dst, int32_t n, int32_t* status,
-                                       void* stream) {
-  KCache c;
-  dcp_status_t st = pack_cache(cache, &c);
-  if (st != DCP_OK) return st;
-  if ((st = check_places(c, src, n)) != DCP_OK) return st;
-  if (n == 0) return DCP_OK;
-  if (!src || !dst || !status || !aligned(dst, 4) || !aligned(status, 4)) return fail(DCP_ERR_INVALID_ARG, "src, dst or status is NULL or misaligned");
-  const int pieces = pieces_of(c);
-  hipStream_t s = (hipStream_t)stream;
-  ProfScope ps(DCP_K_CACHE, s);
-  hipLaunchKernelGGL(take_kernel<true>, dim3(1), dim3(kMapThreads), 0, s, c, src, dst, n, status);
-  DCP_HIP_TRY(hipGetLastError());
-  const int64_t units = n * (1 + 2 * (int64_t)c.n_layers * pieces);
-  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)std::min<int64_t>(units, kCopyWorkers)), dim3(256), 0, s, c, src, dst, n, status, pieces);
-  DCP_HIP_TRY(hipGetLastError());
-  return DCP_OK;
-}
-
-extern "C" dcp_status_t dcp_cache_free(const dcp_cache_t* cache, const int32_t* seqs, int32_t n, void* stream) {
-  KCache c;
-  dcp_status_t st = pack_cache(cache, &c);
-  if (st != DCP_OK) return st;
-  if ((st = check_places(c, seqs, n)) != DCP_OK) return st;
-  if (n == 0) return DCP_OK;
-  ProfScope ps(DCP_K_CACHE, (hipStream_t)stream);
-  hipLaunchKernelGGL(free_kernel, dim3((unsigned)n), dim3(256), 0, (hipStream_t)stream, c, seqs);
-  DCP_HIP_TRY(hipGetLastError());
-  return DCP_OK;
-}
-
-extern "C" size_t dcp_cache_workspace_bytes(const dcp_cache_t* cache) {
-  return cache && cache->n_pages > 0 ? moves_bytes(cache->n_pages) : 0;
-}
-
-extern "C" dcp_status_t dcp_cache_compact(const dcp_cache_t* cache, int32_t* counts, void* workspace, size_t workspace_bytes, void* stream) {
-  KCache c;
-  dcp_status_t st = pack_cache(cache, &c);
-  if (st != DCP_OK) return st;
-  if (!counts || !aligned(counts, 4)) return fail(DCP_ERR_INVALID_ARG, "counts is NULL or misaligned");
-  if (!workspace || workspace_bytes < moves_bytes(c.n_pages)) return fail(DCP_ERR_WORKSPACE, "workspace is NULL or smaller than dcp_cache_workspace_bytes");
-  if (!aligned(workspace, 256)) return fail(DCP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  int32_t* w = (int32_t*)workspace;
-  const int32_t half = c.n_pages / 2 + 1;
-  const Moves m{w, w + 64, w + 64 + half, w + 64 + 2 * half};
-  hipStream_t s = (hipStream_t)stream;
-  ProfScope ps(DCP_K_CACHE, s);
-  hipLaunchKernelGGL(list_moves_kernel, dim3(1), dim3(kMapThreads), 0, s, c, m, counts);
-  DCP_HIP_TRY(hipGetLastError());
-  const int pieces = pieces_of(c);
-  const int64_t most = std::min<int64_t>((c.n_pages / 2 + 1) * (2 * (int64_t)c.n_layers * pieces), kCopyWorkers);
-  hipLaunchKernelGGL(move_kernel, dim3((unsigned)(c.n_seqs + most)), dim3(256), 0, s, c, m, counts, pieces);
-  DCP_HIP_TRY(hipGetLastError());
-  return DCP_OK;
-}

@@ -1,50 +1,10 @@
 // Attention of one new token per sequence over a paged key-value cache.
-#include <algorithm>
-#include <cmath>
-
 #include "cache_internal.h"
 #include "device_utils.h"
 
 using namespace dcp;
 
 namespace dcp {
-
-struct PagedArgs {
-  const char* q;
-  char* out;
-  float* lse;
-  const int32_t *seqs, *status;
-  int64_t q_st, q_sh, o_st, o_sh;   // bytes
-  int32_t n, group, window, sink;   // group: query heads of a KV head
-  // Query heads that share a KV head are taken in sets of up to 16 (or 8, see Tile::weigh); a workgroup's waves take `abreast` (1, 2 or 4) sets
-  // that lie side by side, and where there are fewer than four, the waves of a set take its tiles in turn.
-  int32_t per_kv, set_heads, abreast, log_abreast, groups;   // sets of a KV head, heads of a set at most, ..., sets / abreast
-  int32_t whole;   // items are not cut: nothing to join
-  float scale_log2e;
-};
-
-// Partial results of items (place, group of sets) that several workers share, unnormalised, in units of log2.  A worker's share of the tiles
-// begins in the middle of at most one item and ends in the middle of at most one: slot 2 w holds the first, 2 w + 1 the second.
-struct PagedParts {
-  int4* joins;     // [kWorkers] (place, group, first worker, last worker), place -1: nothing to join.  By item where there are no more
-                   // items than workers (not written for padding), else by the worker that has the item's first tile
-  float2* ml;      // [2 kWorkers][abreast][set_heads] running maximum, sum
-  float* o;        // [2 kWorkers][abreast][set_heads][D]
-  int32_t by_item;
-};
-
-// Two workgroups on a CU, all resident.  The four waves read neighbouring heads of the same keys: where each workgroup walks one head, a
-// quarter of what the memory reads lies in pages that others open again (8 KV heads of 256 bytes, a plain read of all keys
-// and values 5.8 TB/s against 6.9; linear 7.0).
-static constexpr int kLogWorkers = 9, kWorkers = 1 << kLogWorkers;
-static constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
-static constexpr int kSetHeads = 16;     // query heads of a matrix tile
-// Items are taken whole, so that nothing is to be joined, where a workgroup each is enough and none can have more than so many tiles a wave:
-// short sequences (or windows) in a table that has no room for more.  Whole and cut, us: one sequence of 30 tokens, 8 KV heads 7.5 and 13.6, of
-// 300 tokens 12.6 and 12.8; 64 of 90 13.6 and 20.1, of 380 27.5 and 29.0; 16 of 380, 2 KV heads 15.4 and 13.4; with one more
-// round 16 of 500 18.9 and 16.7.  Where they nearly fill the chip, cutting gains little and costs the joins and a start in the middle: 200 of 150
-// tokens, 8 KV heads 33 and 42, 256 of 1 to 200 34 and 41, of 200 44 and 46, 64 of 1 to 700 36.5 and 34; with 160 items fewer 40 of 1 to 700 33 and 27.
-static constexpr int kWholeRounds = 3, kWholeRoundsFull = 8, kFullItems = kWorkers * 3 / 4;
 
 // Of few items each is in many parts, which a join takes with more threads a head: up to kWideJoins entries of the list 1 024, up to
 // kMiddleJoins 256, else 64 (one sequence of 131 067 tokens, 2 entries, 101 / - / 116 us; 16 of 1 to 4 096, 16 entries, 22.6 / - / 22.0).
@@ -551,16 +511,15 @@ __global__ __launch_bounds__(THREADS) void paged_join_kernel(KCache c, PagedArgs
 }
 
 template <typename T, int D, int COLS, bool ONCE>
-static void launch_once(const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
-  const dim3 grid(a.whole ? a.n * a.groups : kWorkers);
-  if (c.page.d % Tile<T, D>::kGroup == 0) hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, true, ONCE>), grid, dim3(kPagedThreads), 0, s, c, a, parts);
-  else hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, false, ONCE>), grid, dim3(kPagedThreads), 0, s, c, a, parts);
+static void launch_once(uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
+  if (c.page.d % Tile<T, D>::kGroup == 0) hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, true, ONCE>), dim3(grid), dim3(kPagedThreads), 0, s, c, a, parts);
+  else hipLaunchKernelGGL((paged_attn_kernel<T, D, COLS, false, ONCE>), dim3(grid), dim3(kPagedThreads), 0, s, c, a, parts);
 }
 template <typename T, int D, int COLS>
-static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
-  if constexpr (D * sizeof(T) < 128) launch_once<T, D, COLS, false>(c, a, parts, s);
-  else if (a.per_kv == 1) launch_once<T, D, COLS, true>(c, a, parts, s);
-  else if constexpr (COLS == kSetHeads) launch_once<T, D, COLS, false>(c, a, parts, s);   // more sets than one are full ones
+static void launch(uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
+  if constexpr (D * sizeof(T) < 128) launch_once<T, D, COLS, false>(grid, c, a, parts, s);
+  else if (a.per_kv == 1) launch_once<T, D, COLS, true>(grid, c, a, parts, s);
+  else if constexpr (COLS == kSetHeads) launch_once<T, D, COLS, false>(grid, c, a, parts, s);   // more sets than one are full ones
   if (a.whole) return;
   const unsigned entries = parts.by_item ? a.n * a.groups : kWorkers, heads = a.abreast * a.set_heads;
   if (entries <= kWideJoins) hipLaunchKernelGGL((paged_join_kernel<T, D, 1024, 1>), dim3(entries, heads), dim3(1024), 0, s, c, a, parts);
@@ -568,91 +527,16 @@ static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts,
   else hipLaunchKernelGGL((paged_join_kernel<T, D, 256, 4>), dim3(entries, (heads + 3) / 4), dim3(256), 0, s, c, a, parts);
 }
 template <typename T, int COLS>
-static void launch(const KCache& c, const PagedArgs& a, const PagedParts& parts, int d, hipStream_t s) {
-  if (d == 128) launch<T, 128, COLS>(c, a, parts, s);
-  else if (d == 64) launch<T, 64, COLS>(c, a, parts, s);
-  else launch<T, 32, COLS>(c, a, parts, s);
+static void launch(uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, int32_t d, hipStream_t s) {
+  if (d == 128) launch<T, 128, COLS>(grid, c, a, parts, s);
+  else if (d == 64) launch<T, 64, COLS>(grid, c, a, parts, s);
+  else launch<T, 32, COLS>(grid, c, a, parts, s);
 }
 
-// How the query heads are taken: see PagedArgs.
-struct Sets {
-  int32_t per_kv, heads, abreast, log_abreast;
-  int64_t groups;
-  size_t bytes;   // of the workspace
-};
-static Sets sets_of(int32_t hkv, int32_t hq, int32_t d, int most_abreast) {
-  const int32_t group = hq / hkv;
-  Sets s;
-  s.per_kv = (group - 1) / kSetHeads + 1;   // group up to 2^31 - 1
-  s.heads = std::min(group, kSetHeads);
-  const int64_t sets = (int64_t)hkv * s.per_kv;
-  s.log_abreast = 0;
-  while (2 << s.log_abreast <= most_abreast && sets % (2 << s.log_abreast) == 0) s.log_abreast++;
-  s.abreast = 1 << s.log_abreast;
-  s.groups = sets / s.abreast;
-  s.bytes = kWorkers * (sizeof(int4) + 2 * (size_t)s.abreast * s.heads * (sizeof(float2) + d * sizeof(float)));
-  return s;
+void launch_paged_attn(int32_t dtype, int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
+  if (dtype == DCP_F32) launch<float, 16>(grid, c, a, parts, d, s);
+  else if (a.group <= 8) launch<bf16_t, 8>(grid, c, a, parts, d, s);
+  else launch<bf16_t, 16>(grid, c, a, parts, d, s);
 }
 
 }  // namespace dcp
-
-extern "C" size_t dcp_paged_attn_workspace_bytes(const dcp_cache_t* cache, int32_t n, int32_t hq) {
-  if (!cache || n <= 0 || hq <= 0 || cache->hkv <= 0 || cache->d <= 0) return 0;
-  return hq % cache->hkv ? 0 : sets_of(cache->hkv, hq, cache->d, kPagedWaves).bytes;
-}
-
-extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t* args, void* workspace, size_t workspace_bytes,
-                                           void* stream) {
-  KCache c;
-  dcp_status_t st = pack_cache(cache, &c);
-  if (st != DCP_OK) return st;
-  if (!args) return fail(DCP_ERR_INVALID_ARG, "args is NULL");
-  const dcp_paged_attn_t& t = *args;
-  if ((st = check_places(c, t.seqs, t.n)) != DCP_OK) return st;
-  if (t.hq <= 0) return fail(DCP_ERR_INVALID_ARG, "hq must be positive");
-  if (t.hq % c.hkv != 0) return fail(DCP_ERR_UNSUPPORTED, "hq must be a multiple of hkv");
-  if (t.layer < 0 || t.layer >= c.n_layers) return fail(DCP_ERR_INVALID_ARG, "layer out of range");
-  if (!(t.softmax_scale > 0.f) || !std::isfinite(t.softmax_scale)) return fail(DCP_ERR_INVALID_ARG, "softmax_scale must be positive and finite");
-  if (t.window < 0 || t.sink < 0) return fail(DCP_ERR_INVALID_ARG, "window and sink must not be negative");
-  if (t.n == 0) return DCP_OK;
-  if ((st = check_rows("q", t.q, t.q_stride_t, t.q_stride_h, cache->d)) != DCP_OK) return st;
-  if ((st = check_rows("out", t.out, t.o_stride_t, t.o_stride_h, cache->d)) != DCP_OK) return st;
-  if (!t.lse || (reinterpret_cast<uintptr_t>(t.lse) & 3u)) return fail(DCP_ERR_INVALID_ARG, "lse is NULL or misaligned");
-  if (reinterpret_cast<uintptr_t>(t.status) & 3u) return fail(DCP_ERR_INVALID_ARG, "status is misaligned");
-  if (!workspace || workspace_bytes < dcp_paged_attn_workspace_bytes(cache, t.n, t.hq))
-    return fail(DCP_ERR_WORKSPACE, "workspace is NULL or smaller than dcp_paged_attn_workspace_bytes");
-  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(DCP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  const int64_t e = cache->dtype == DCP_BF16 ? 2 : 4;
-  if (rows_overlap(Rows{t.q, t.q_stride_t * e, t.q_stride_h * e}, Rows{t.out, t.o_stride_t * e, t.o_stride_h * e}, t.n, t.hq, cache->d * e))
-    return fail(DCP_ERR_INVALID_ARG, "out overlaps q");
-  // Whole items: the most tiles that one can have, as far as the host knows, over the waves that take them in turn
-  const int tile = cache->dtype == DCP_F32 ? 16 : 32;
-  const int64_t most = ((t.window > 0 ? std::min<int64_t>(c.max_len, (int64_t)t.window + t.sink + 2 * tile) : c.max_len) + tile - 1) / tile;
-  Sets sets = sets_of(c.hkv, t.hq, cache->d, kPagedWaves);
-  if (sets.groups * sets.abreast > (1 << 12)) return fail(DCP_ERR_UNSUPPORTED, "dcp_paged_attn_fwd covers at most 4 096 sets of 16 query heads on one KV head");
-  bool whole = false;
-  for (int abreast = 1; abreast <= sets.abreast && !whole; abreast *= 2) {
-    const Sets x = sets_of(c.hkv, t.hq, cache->d, abreast);
-    whole = t.n * x.groups <= kWorkers && most <= (t.n * x.groups > kFullItems ? kWholeRoundsFull : kWholeRounds) * (kPagedWaves / x.abreast);
-    if (whole) sets = x;
-  }
-  if (t.n * (int64_t)((c.max_len + tile - 1) / tile) * sets_of(c.hkv, t.hq, cache->d, 1).groups > INT32_MAX)
-    return fail(DCP_ERR_UNSUPPORTED, "n x hkv x sets of 16 query heads on one KV head x tiles of 32 (fp32: 16) tokens in a row of the table must be below 2^31");
-  c.k += t.layer * c.k_sl;   // the layer's
-  c.v += t.layer * c.v_sl;
-  const PagedArgs a{(const char*)t.q, (char*)t.out, t.lse, t.seqs, t.status, t.q_stride_t * e, t.q_stride_h * e, t.o_stride_t * e, t.o_stride_h * e,
-                    t.n, t.hq / c.hkv, t.window, t.sink, sets.per_kv, sets.heads, sets.abreast, sets.log_abreast, (int32_t)sets.groups, whole,
-                    t.softmax_scale * 1.44269504088896340736f};
-  PagedParts parts;
-  parts.joins = (int4*)workspace;
-  parts.o = (float*)(parts.joins + kWorkers);
-  parts.ml = (float2*)(parts.o + 2 * (size_t)kWorkers * sets.abreast * sets.heads * cache->d);
-  parts.by_item = t.n * sets.groups <= kWorkers;
-  hipStream_t s = (hipStream_t)stream;
-  ProfScope ps(DCP_K_PAGED_ATTN, s);
-  if (cache->dtype == DCP_F32) launch<float, 16>(c, a, parts, cache->d, s);
-  else if (a.group <= 8) launch<bf16_t, 8>(c, a, parts, cache->d, s);
-  else launch<bf16_t, 16>(c, a, parts, cache->d, s);
-  DCP_HIP_TRY(hipGetLastError());
-  return DCP_OK;
-}
