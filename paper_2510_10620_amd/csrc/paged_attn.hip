@@ -6,9 +6,12 @@ using namespace dcp;
 
 namespace dcp {
 
-// Of few items each is in many parts, which a join takes with more threads a head: up to kWideJoins entries of the list 1 024, up to
-// kMiddleJoins 256, else 64 (one sequence of 131 067 tokens, 2 entries, 101 / - / 116 us; 16 of 1 to 4 096, 16 entries, 22.6 / - / 22.0).
-static constexpr unsigned kWideJoins = 7, kMiddleJoins = 31;
+// Of few items each is in many parts, which a join takes with more threads a head: up to kMiddleJoins entries of the list 256, else 64; heads of 128,
+// of which 256 threads take only 8 parts at a time, 1 024 threads up to kWideJoins.  Whole calls, us, with 1 024 / 256 / 64: D 128, 1 entry of
+// 30 000 tokens 27.9 / 32.8 / 62.3, 2 of 131 067 93.6 / 95.3 / 110, 3 of 30 000 44.7 / 45.3 / -, 5 63.3 / 63.1 / -, 8 of 20 000 66.0 / 65.3 / 69.1, 16 of
+// 2 048 26.2 / 24.9 / 26.3, 31 of 4 096 55.8 / 54.3 / 55.5, 70 of 2 048 65.9 / 62.5 / 61.7; D 64, 1 of 8 000 14.7 / 13.5 / -, of 30 000 20.8 / 21.1 / 37.3, 3 of
+// 30 000 28.9 / 27.2 / -, 16 of 2 048 18.1 / 16.7 / 16.8, 31 of 4 096 33.9 / 32.8 / 32.5; fp32 with D 64, 8 of 1 to 4 096 18.2 / 15.8 / 18.9.
+static constexpr unsigned kWideJoins = 3, kMiddleJoins = 31;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -522,8 +525,13 @@ static void launch(uint32_t grid, const KCache& c, const PagedArgs& a, const Pag
   else if constexpr (COLS == kSetHeads) launch_once<T, D, COLS, false>(grid, c, a, parts, s);   // more sets than one are full ones
   if (a.whole) return;
   const unsigned entries = parts.by_item ? a.n * a.groups : kWorkers, heads = a.abreast * a.set_heads;
-  if (entries <= kWideJoins) hipLaunchKernelGGL((paged_join_kernel<T, D, 1024, 1>), dim3(entries, heads), dim3(1024), 0, s, c, a, parts);
-  else if (entries <= kMiddleJoins) hipLaunchKernelGGL((paged_join_kernel<T, D, 256, 1>), dim3(entries, heads), dim3(256), 0, s, c, a, parts);
+  if constexpr (D == 128) {
+    if (entries <= kWideJoins) {
+      hipLaunchKernelGGL((paged_join_kernel<T, D, 1024, 1>), dim3(entries, heads), dim3(1024), 0, s, c, a, parts);
+      return;
+    }
+  }
+  if (entries <= kMiddleJoins) hipLaunchKernelGGL((paged_join_kernel<T, D, 256, 1>), dim3(entries, heads), dim3(256), 0, s, c, a, parts);
   else hipLaunchKernelGGL((paged_join_kernel<T, D, 256, 4>), dim3(entries, (heads + 3) / 4), dim3(256), 0, s, c, a, parts);
 }
 template <typename T, int COLS>
