@@ -266,8 +266,8 @@ __global__ __launch_bounds__(256) void free_kernel(KCache c, const int32_t* __re
 }
 
 // One workgroup: counts the pages in use (u), then lists the free ones before u and the used ones behind it, which are as many.  Bound by
-// latency: page_ref is read twice, 8 192 pages at a time (the second time from the cache), once if there are no more; the lists of so
-// few stay in LDS until they meet (240 pages 5.9 -> 4.6 us, 9 712 11.8 -> 8.9).
+// latency: page_ref is read twice, 8 192 pages at a time (the second time from the cache), once if there are no more, whose lists stay in LDS
+// until they meet (a call in a graph, with a copy of the map: 240 pages 9.4 -> 9.2 us, 8 192 14.65 -> 14.3).
 __global__ __launch_bounds__(kMapThreads) void list_moves_kernel(KCache c, Moves m, int32_t* __restrict__ counts) {
   constexpr int kOnce = kMapThreads * kScan;
   __shared__ int32_t wave_sum[kMapWaves], wave_high[kMapWaves], s_to[kOnce / 2], s_from[kOnce / 2];

@@ -137,8 +137,9 @@ extern "C" dcp_status_t dcp_cache_append(const dcp_cache_t* cache, int32_t layer
   const int64_t e = cache->dtype == DCP_BF16 ? 2 : 4;
   const NewTokens x{(const char*)k_new, (const char*)v_new, k_st * e, k_sh * e, v_st * e, v_sh * e, n_tokens};
   ProfScope ps(DCP_K_CACHE, (hipStream_t)stream);
-  // up to four tokens a CU a workgroup each (64 tokens 6.4 -> 4.3 us against eight in one), else four in one (83 396 tokens in 2 / 4 / 8 / 16:
-  // 123 / 124 / 130 / 134 us with the reserve and the map's reset)
+  // Up to four tokens a CU a workgroup each, else four in one.  In a graph, us, with one / four: tokens of 4 KiB, 64 2.95 / 3.44, 1 024 3.7 / 3.9,
+  // 2 048 4.3 / 4.4, 4 096 8.4 / 7.2, 32 768 54 / 39; of 512 bytes, 64 2.94 / 2.86, 1 024 3.25 / 3.0, 8 192 7.8 / 3.8.  83 396 of 4 KiB in
+  // 2 / 4 / 8 / 16: 123 / 124 / 130 / 134 with the reserve and the map's reset.
   const int32_t each = n_tokens <= 1024 ? 1 : 4;
   launch_append(each, (uint32_t)((n_tokens + each - 1) / each), c, layer, seqs, cu_new, n, status, x, (hipStream_t)stream);
   DCP_HIP_TRY(hipGetLastError());

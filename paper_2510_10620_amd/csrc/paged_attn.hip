@@ -250,7 +250,7 @@ __device__ __forceinline__ int32_t seq_at(const PagedArgs& a, int i) {
 // seqs, seq_len, page_table, one after the other), 4 to 7 are the join, which is what bounds short calls.  All tiles of the batch are dealt
 // out evenly, whatever the lengths, so that workgroups end together; tiles in flight: the next one's K and V (a second V in flight
 // gained nothing, nor did 768 or 1 024 workgroups).  The sums of a place are taken in an order that goes by the lengths of the whole batch, and by nothing else.
-// Conditions that select lanes are written with & and |: under && and || the compiler has dropped the first of the eight selects of a tile.
+// Conditions that select lanes are written with & and |: a select a key, where && and || make a branch a key (which takes as long).
 template <typename T, int D, int COLS, bool GROUPED, bool ONCE>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged_attn_kernel(KCache c, PagedArgs a, PagedParts parts) {
   typedef Tile<T, D> TT;
