@@ -66,7 +66,10 @@ typedef enum {
   DCP_MASK_NONE = 0, DCP_MASK_CAUSAL = 1, DCP_MASK_RANGES = 2, DCP_MASK_SKIP = 3, DCP_MASK_WINDOW = 4
 } dcp_mask_kind_t;
 
-typedef enum { DCP_BF16 = 0, DCP_F32 = 1 } dcp_dtype_t;
+typedef enum {
+  DCP_BF16 = 0, DCP_F32 = 1,
+  DCP_E4M3 = 3   /* 8 bits: sign, 4 of exponent (bias 7), 3 of fraction; largest 448, 0x7f and 0xff NaN, no infinity.  Of caches alone (dcp_cache_t) */
+} dcp_dtype_t;
 
 /* Which kernel family runs.  AUTO picks MFMA when (dtype, D) is covered, else SCALAR; outside bf16 with D = 128 it also
  * picks SCALAR where a token stride exceeds 2^24 elements, a launch would have 2^32 threads or more, or the plan's blocks
@@ -428,7 +431,24 @@ typedef struct {
   int32_t* page_ref;
   int32_t* page_table;
   int32_t* seq_len;
+  /* DCP_E4M3 only, see below; not read for other dtypes */
+  int32_t io_dtype;           /* DCP_BF16 or DCP_F32 */
+  int32_t scale_block;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
 } dcp_cache_t;
+
+/* A cache in 8 bits (dtype DCP_E4M3): every scale_block neighbouring tokens of a page (scale_block divides page_size) share a scale for each
+ * KV head, a power of two that is kept as its exponent with bias 127: a number stands for code x 2^(scale - 127).
+ *   k, v              strides are multiples of 16 elements
+ *   k_scale, v_scale  uint8 [n_layers, n_pages, page_size / scale_block, hkv] contiguous; 1 to 254 (0 is taken as 1, 255 as 254).  A block without tokens may
+ *                     hold anything
+ *   io_dtype          of what the calls take and give beside it: k_new, v_new, q, out, k_out, v_out
+ * A code is the value x 2^(127 - scale), rounded once to nearest, ties to even.  The scale is the least one, from 10 on (so that all values are normal
+ * numbers of bf16 and fp32), with which the largest finite of the block's values reaches 448 units at most.  Blocks are filled in several appends, in a
+ * step token by token: where later tokens need a larger scale, the codes of the block's earlier tokens are rounded again, from the values that they stand for.  NaN
+ * stays NaN, and an infinity becomes one (the format has none); neither counts for the scale.  What stands for more than the largest number of io_dtype, as values
+ * within 2^-5 of it may after rounding, is an infinity there. */
 
 /* Room for n_new[i] >= 0 more tokens (NULL: one each) of every place's sequence: seq_len advances and the pages that the new
  * tokens reach are taken, the lowest free ones first, in the order of the places.  Places are served in order until one finds too few
@@ -440,11 +460,18 @@ dcp_status_t dcp_cache_reserve(const dcp_cache_t* cache, const int32_t* seqs, co
  * the tokens [cu_new[i], cu_new[i + 1]) of k_new and v_new (cu_new NULL: token i alone), the last ones of its sequence.
  *   cu_new  int32 [n + 1], device, ascending; tokens that it leaves out or that are not below n_tokens are not read
  *   status  of dcp_cache_reserve (places that are not OK are left out), or NULL; a sequence is named by one place that is written
- *   k_new, v_new  [n_tokens, hkv, d] of the cache's dtype, strides as for k and v of dcp_tensors_t; not part of the cache;
- *                n_tokens at most 2^25 */
+ *   k_new, v_new  [n_tokens, hkv, d] of the cache's dtype (DCP_E4M3: of io_dtype), strides as for k and v of dcp_tensors_t; not part of
+ *                the cache; n_tokens at most 2^25 */
 dcp_status_t dcp_cache_append(const dcp_cache_t* cache, int32_t layer, const int32_t* seqs, const int32_t* cu_new, int32_t n,
                               const int32_t* status, const void* k_new, int64_t k_stride_t, int64_t k_stride_h,
                               const void* v_new, int64_t v_stride_t, int64_t v_stride_h, int64_t n_tokens, void* stream);
+
+/* Reads them back: rows [cu_new[i], cu_new[i + 1]) of k_out and v_out get the last tokens of place i's sequence, however many, in one layer: packed keys and
+ * values, as dcp_block_attn_fwd takes them.  Rows of places that dcp_cache_append leaves out, of positions before the sequence's first token and of
+ * pages that do not exist are not written.  Arguments as there; k_out, v_out must not overlap each other or the cache. */
+dcp_status_t dcp_cache_read(const dcp_cache_t* cache, int32_t layer, const int32_t* seqs, const int32_t* cu_new, int32_t n,
+                            const int32_t* status, void* k_out, int64_t k_stride_t, int64_t k_stride_h,
+                            void* v_out, int64_t v_stride_t, int64_t v_stride_h, int64_t n_tokens, void* stream);
 
 /* Sequence dst[i], which must be empty, becomes a copy of src[i]: it shares the whole pages (page_ref + 1) and gets a page of its own,
  * the lowest free one, with the tokens of the page that src[i] is filling, in all layers (the rest of that page stays as it is).  One
@@ -469,11 +496,11 @@ dcp_status_t dcp_cache_compact(const dcp_cache_t* cache, int32_t* counts, void* 
  * that is not OK there has no token at seq_len - 1 and is padding.  Keys in pages that do not exist are not seen.  Out and LSE as in dcp_block_attn_fwd: a place that sees no key gets
  * O = 0, LSE = -inf; padding is not written.  Inf and NaN in q, k and v reach the places that see them and no others.  The same
  * call gives the same bits; the order of a place's sums goes by the lengths of the whole batch.
- *   q, out  [n, hq, d] of the cache's dtype, strides as in dcp_tensors_t; out must not overlap q (rows of it between those of q: with the
+ *   q, out  [n, hq, d] of the cache's dtype (DCP_E4M3: of io_dtype), strides as in dcp_tensors_t; out must not overlap q (rows of it between those of q: with the
  *              same strides only);  lse float [hq, n] contiguous
  *   workspace  device, >= dcp_paged_attn_workspace_bytes, 256-byte aligned; scratch, whatever it holds: calls that may run at the same
  *              time need one each.  One launch or two.
- * DCP_ERR_UNSUPPORTED: hkv * ceil(hq / hkv / 16) above 4 096; that times n times ceil(max_pages * page_size / 32) (fp32: 16) of 2^31 or more. */
+ * DCP_ERR_UNSUPPORTED: hkv * ceil(hq / hkv / 16) above 4 096; that times n times ceil(max_pages * page_size / 32) (fp32: 16, DCP_E4M3: 64) of 2^31 or more. */
 typedef struct {
   int32_t n, hq, layer;
   float softmax_scale;

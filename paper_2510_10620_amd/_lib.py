@@ -54,6 +54,7 @@ class Cache(ctypes.Structure):
         ("k", vp), ("k_stride_l", ctypes.c_int64), ("k_stride_p", ctypes.c_int64), ("k_stride_t", ctypes.c_int64), ("k_stride_h", ctypes.c_int64),
         ("v", vp), ("v_stride_l", ctypes.c_int64), ("v_stride_p", ctypes.c_int64), ("v_stride_t", ctypes.c_int64), ("v_stride_h", ctypes.c_int64),
         ("page_ref", vp), ("page_table", vp), ("seq_len", vp),
+        ("io_dtype", ctypes.c_int32), ("scale_block", ctypes.c_int32), ("k_scale", vp), ("v_scale", vp),
     ]
 
 
@@ -103,6 +104,8 @@ _SIGS = {
     "dcp_cache_reserve": (ctypes.c_int, [ctypes.POINTER(Cache), vp, vp, ctypes.c_int32, vp, vp]),
     "dcp_cache_append": (ctypes.c_int, [ctypes.POINTER(Cache), ctypes.c_int32, vp, vp, ctypes.c_int32, vp, vp, ctypes.c_int64, ctypes.c_int64,
                                         vp, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, vp]),
+    "dcp_cache_read": (ctypes.c_int, [ctypes.POINTER(Cache), ctypes.c_int32, vp, vp, ctypes.c_int32, vp, vp, ctypes.c_int64, ctypes.c_int64,
+                                      vp, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, vp]),
     "dcp_cache_fork": (ctypes.c_int, [ctypes.POINTER(Cache), vp, vp, ctypes.c_int32, vp, vp]),
     "dcp_cache_free": (ctypes.c_int, [ctypes.POINTER(Cache), vp, ctypes.c_int32, vp]),
     "dcp_cache_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Cache)]),

@@ -12,7 +12,7 @@ DCP_OK = 0
 DCP_ERR_INVALID_ARG, DCP_ERR_BAD_CU_SEQLENS, DCP_ERR_BAD_TABLE = -1, -2, -3
 DCP_ERR_UNSUPPORTED, DCP_ERR_WORKSPACE, DCP_ERR_HIP = -4, -5, -6
 DCP_MASK_NONE, DCP_MASK_CAUSAL, DCP_MASK_RANGES, DCP_MASK_SKIP, DCP_MASK_WINDOW = 0, 1, 2, 3, 4
-DCP_BF16, DCP_F32 = 0, 1
+DCP_BF16, DCP_F32, DCP_E4M3 = 0, 1, 3
 DCP_IMPL_AUTO, DCP_IMPL_SCALAR, DCP_IMPL_MFMA = 0, 1, 2
 DCP_FORM_ROWS, DCP_FORM_SHARED, DCP_FORM_SPLIT, DCP_FORM_SPLIT8 = -1, 0, 1, 2
 DCP_PLACE_OK, DCP_PLACE_FULL, DCP_PLACE_BAD = 0, 1, 2
@@ -203,13 +203,17 @@ def dcp_plan_export_part_groups(plan, hq, hkv, d):
 
 
 # ------------------------------------------------------------------ launching calls (torch)
-def _dtype_code(t):
+def _dtype_code_of(dtype):
     import torch
-    if t.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return DCP_BF16
-    if t.dtype == torch.float32:
+    if dtype == torch.float32:
         return DCP_F32
-    raise TypeError(f"unsupported dtype {t.dtype}")
+    raise TypeError(f"unsupported dtype {dtype}")
+
+
+def _dtype_code(t):
+    return _dtype_code_of(t.dtype)
 
 
 def _stream():
@@ -461,9 +465,10 @@ class Program:
 class Cache:
     """dcp_cache_t over the caller's tensors, which it keeps alive: k, v [layers, pages, page_size, hkv, d] (any strides with d
     contiguous), page_ref int32 [pages], page_table int32 [seqs, max_pages], seq_len int32 [seqs], all on one device, which has to be
-    the current one when a call is made."""
+    the current one when a call is made.  In 8 bits (k, v of torch.float8_e4m3fn): k_scale, v_scale uint8 [layers, pages, page_size / scale_block, hkv],
+    contiguous, and io_dtype, the dtype of what the calls take and give beside the cache (torch.bfloat16 if None)."""
 
-    def __init__(self, k, v, page_ref, page_table, seq_len):
+    def __init__(self, k, v, page_ref, page_table, seq_len, k_scale=None, v_scale=None, io_dtype=None):
         import torch
         if k.dim() != 5 or v.shape != k.shape or v.dtype != k.dtype:
             raise ValueError("k and v: [layers, pages, page_size, hkv, d] of one shape and dtype")
@@ -471,33 +476,56 @@ class Cache:
             raise ValueError("page_ref [pages], page_table [seqs, max_pages], seq_len [seqs]")
         if not k.is_cuda:
             raise ValueError("k: device tensor required")
+        codes = k.dtype == torch.float8_e4m3fn
+        if not codes and (k_scale is not None or v_scale is not None or io_dtype not in (None, k.dtype)):
+            raise ValueError("k_scale, v_scale and io_dtype are of caches in torch.float8_e4m3fn")
         self.k, self.v, self.page_ref, self.page_table, self.seq_len = k, v, page_ref, page_table, seq_len
-        self.device, self._index, self._dtype, self._i32, self._f32 = k.device, k.get_device(), k.dtype, torch.int32, torch.float32
+        self.device, self._index, self._i32, self._f32 = k.device, k.get_device(), torch.int32, torch.float32
+        self.k_scale, self.v_scale, self._dtype = k_scale, v_scale, k.dtype if not codes else torch.bfloat16 if io_dtype is None else io_dtype
         self._hkv, self._d = k.shape[3:]
         # the current stream as a number; torch.cuda.current_stream builds an object, which takes longer than a launch
         self._raw_stream, self._raw_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         self._lib = _lib.load()
         d = self.descr = _lib.Cache()
         d.n_layers, d.n_pages, d.page_size, d.hkv, d.d = k.shape
-        d.dtype, d.n_seqs, d.max_pages = _dtype_code(k), page_table.shape[0], page_table.shape[1]
+        d.dtype, d.n_seqs, d.max_pages = DCP_E4M3 if codes else _dtype_code(k), page_table.shape[0], page_table.shape[1]
+        if codes:
+            layers, pages, page, hkv = k.shape[:4]
+            for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+                if t is None or t.dtype != torch.uint8 or t.dim() != 4 or t.shape != k_scale.shape or not t.is_contiguous() or t.get_device() != self._index:
+                    raise ValueError(f"{name}: contiguous uint8 tensor [layers, pages, page_size / scale_block, hkv] on the cache's device required")
+                setattr(d, name, t.data_ptr())
+            blocks = k_scale.shape[2]
+            if tuple(k_scale.shape) != (layers, pages, blocks, hkv) or blocks < 1 or page % blocks:
+                raise ValueError("k_scale, v_scale: [layers, pages, page_size / scale_block, hkv]")
+            d.io_dtype, d.scale_block = _dtype_code_of(self._dtype), page // blocks
         for name, t in (("k", k), ("v", v)):
             if t.get_device() != self._index or t.stride(-1) != 1:
                 raise ValueError(f"{name}: tensor with contiguous last dim on one device required")
             setattr(d, name, t.data_ptr())
             for axis, letter in enumerate("lpth"):
                 # a dimension of one element has no stride of its own
-                setattr(d, f"{name}_stride_{letter}", t.stride(axis) if t.shape[axis] > 1 else max(8, t.shape[4]))
+                setattr(d, f"{name}_stride_{letter}", t.stride(axis) if t.shape[axis] > 1 else max(16 if codes else 8, t.shape[4]))
         d.page_ref, d.seq_len = self._ints("page_ref", page_ref, page_ref.shape[0]), self._ints("seq_len", seq_len, seq_len.shape[0])
         d.page_table = self._ints("page_table", page_table, page_table.numel())
         self.ref = ctypes.byref(d)
 
     @classmethod
-    def empty(cls, layers, pages, page_size, hkv, d, seqs, max_pages, dtype, device="cuda"):
-        """An empty cache in new tensors."""
+    def empty(cls, layers, pages, page_size, hkv, d, seqs, max_pages, dtype, device="cuda", scale_block=None, io_dtype=None):
+        """An empty cache in new tensors.  dtype torch.float8_e4m3fn: scale_block tokens share a scale (None: those of a page)."""
         import torch
+        more = {}
+        if dtype == torch.float8_e4m3fn:
+            block = page_size if scale_block is None else scale_block
+            if block < 1 or page_size % block:
+                raise ValueError("scale_block must divide page_size")
+            scales = [torch.full((layers, pages, page_size // block, hkv), 127, dtype=torch.uint8, device=device) for _ in range(2)]
+            more = dict(k_scale=scales[0], v_scale=scales[1], io_dtype=io_dtype)
+        elif scale_block is not None or io_dtype not in (None, dtype):
+            raise ValueError("scale_block and io_dtype are of caches in torch.float8_e4m3fn")
         kv = [torch.empty((layers, pages, page_size, hkv, d), dtype=dtype, device=device) for _ in range(2)]
         zeros = [torch.zeros(n, dtype=torch.int32, device=device) for n in (pages, seqs)]
-        return cls(*kv, zeros[0], torch.full((seqs, max_pages), -1, dtype=torch.int32, device=device), zeros[1])
+        return cls(*kv, zeros[0], torch.full((seqs, max_pages), -1, dtype=torch.int32, device=device), zeros[1], **more)
 
     # The checks below run once per tensor and call: they are written for a call that is shorter than its launch.
     def _ints(self, name, t, n):
@@ -508,12 +536,12 @@ class Cache:
         raise ValueError(f"{name}: contiguous int32 tensor of {n} elements on the cache's device required")
 
     def _token_rows(self, name, t):
-        """[tokens, heads, d] of the cache's dtype: (address, token stride, head stride); a dimension of one element has no stride of its own."""
+        """[tokens, heads, d] of the cache's dtype (in 8 bits: of io_dtype): (address, token stride, head stride); a dimension of one element has no stride of its own."""
         n, h, d = t.shape
         st, sh, one = t.stride()
         if t.dtype is self._dtype and one == 1 and t.get_device() == self._index:
             return t.data_ptr(), st if n > 1 else max(8, d), sh if h > 1 else max(8, d)
-        raise ValueError(f"{name}: tensor of the cache's dtype with contiguous last dim on its device required")
+        raise ValueError(f"{name}: tensor of the cache's dtype (in 8 bits: its io_dtype) with contiguous last dim on its device required")
 
     def _space(self, workspace):
         if workspace.get_device() != self._index or not workspace.is_contiguous():
@@ -542,6 +570,17 @@ def dcp_cache_append(cache, k_new, v_new, seqs=None, cu_new=None, status=None, l
     _check(cache._lib.dcp_cache_append(cache.ref, layer, cache._ints("seqs", seqs, n), cache._ints("cu_new", cu_new, n + 1), n,
                                        cache._ints("status", status, n), *cache._token_rows("k_new", k_new), *cache._token_rows("v_new", v_new),
                                        tokens, cache._stream()))
+
+
+def dcp_cache_read(cache, k_out, v_out, seqs=None, cu_new=None, status=None, layer=0):
+    """k_out, v_out [tokens, hkv, d] get the last tokens of the sequences, packed as dcp_cache_append takes them."""
+    tokens, hkv, d = k_out.shape
+    if hkv != cache._hkv or d != cache._d or v_out.shape != k_out.shape:
+        raise ValueError("k_out, v_out: [tokens, hkv, d] with the cache's hkv and d")
+    n = cu_new.numel() - 1 if cu_new is not None else tokens
+    _check(cache._lib.dcp_cache_read(cache.ref, layer, cache._ints("seqs", seqs, n), cache._ints("cu_new", cu_new, n + 1), n,
+                                     cache._ints("status", status, n), *cache._token_rows("k_out", k_out), *cache._token_rows("v_out", v_out),
+                                     tokens, cache._stream()))
 
 
 def dcp_cache_fork(cache, src, dst, status):

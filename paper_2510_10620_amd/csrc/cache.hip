@@ -2,6 +2,7 @@
 // tokens are written into them.  Everything is decided on the device from page_ref, page_table and seq_len, so that a
 // decoding step never waits for the host.
 #include "cache_internal.h"
+#include "cache_tokens.h"
 
 using namespace dcp;
 
@@ -217,6 +218,13 @@ __device__ __forceinline__ void copy_chunks(const KCache& c, char* base, int64_t
   }
 }
 
+// The scales of the first `blocks` blocks of a page, of one layer of k or v, by a workgroup of 256 (a page has few beside its codes).
+__device__ __forceinline__ void copy_scales(const KCache& c, uint8_t* scales, int64_t layer, int from, int to, int blocks) {
+  scales += layer * c.layer_scales();
+  const int64_t page = (int64_t)c.blocks * c.hkv, n = (int64_t)blocks * c.hkv;
+  for (int64_t x = threadIdx.x; x < n; x += 256) scales[to * page + x] = scales[from * page + x];
+}
+
 // After take_kernel.  Of place i's units the first shares its whole pages, unit 1 + x copies a piece of the page being filled, x = 2 (layer pieces
 // + piece) + (0: k, 1: v).
 __global__ __launch_bounds__(256) void fork_kernel(KCache c, const int32_t* __restrict__ src, const int32_t* __restrict__ dst, int32_t n,
@@ -244,6 +252,7 @@ __global__ __launch_bounds__(256) void fork_kernel(KCache c, const int32_t* __re
     if (first >= last) continue;
     const int32_t page = from[whole], mine = to[whole];
     if (!c.is_page(page) || !c.is_page(mine)) continue;
+    if (c.k_scale && first == 0) copy_scales(c, y & 1 ? c.k_scale : c.v_scale, layer, page, mine, c.block.quot(c.page.rem(len, whole) - 1) + 1);
     if (y & 1) copy_chunks<true>(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, page, mine, first, last);
     else copy_chunks<true>(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, page, mine, first, last);
   }
@@ -381,6 +390,7 @@ __global__ __launch_bounds__(256) void move_kernel(KCache c, Moves m, const int3
       c.ref[to] = c.ref[from];
       c.ref[from] = 0;
     }
+    if (c.k_scale && first == 0) copy_scales(c, y & 1 ? c.v_scale : c.k_scale, layer, from, to, c.blocks);
     if (y & 1) copy_chunks<false>(c, c.v + layer * c.v_sl, c.v_sp, c.v_st, c.v_sh, from, to, first, last);
     else copy_chunks<false>(c, c.k + layer * c.k_sl, c.k_sp, c.k_st, c.k_sh, from, to, first, last);
   }
@@ -389,50 +399,16 @@ __global__ __launch_bounds__(256) void move_kernel(KCache c, Moves m, const int3
 // A workgroup writes TOKENS tokens: their places in the cache are found by a thread each, then all threads copy, four chunks in flight.  HBM-bound
 // where there are many (83 396 tokens of 4 KiB 111 us, 6.1 TB/s read and written); few take a workgroup each and are bound by the trips
 // to memory: cu_new, seqs, seq_len, page_table, the tokens.
-static constexpr int kCuInLds = 1024;   // entries of cu_new that are searched in LDS
 template <int TOKENS>
 __global__ __launch_bounds__(256) void append_kernel(KCache c, int32_t layer, const int32_t* __restrict__ seqs, const int32_t* __restrict__ cu,
                                                      int32_t n, const int32_t* __restrict__ status, NewTokens x) {
   __shared__ int32_t page_of[TOKENS], slot_of[TOKENS], s_cu[kCuInLds];
   const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
-  const bool in_lds = cu && n < kCuInLds;
-  if (in_lds) {
-    for (int y = threadIdx.x; y <= n; y += 256) s_cu[y] = cu[y];
-    __syncthreads();
-  }
+  const Begins begins(cu, n, s_cu);
   if (threadIdx.x < TOKENS) {
-    const int64_t t = t0 + threadIdx.x;
-    int page = -1, slot = 0;
-    int i = -1, behind = 0;   // the token's place, and the tokens of it from this one on
-    if (t < x.n) {
-      if (!cu) {
-        if (t < n) { i = (int)t; behind = 1; }
-      } else {
-        auto at = [&](int y) { return in_lds ? s_cu[y] : cu[y]; };
-        if (t >= at(0) && t < at(n)) {
-          int lo = 0, hi = n - 1;   // the last place that begins at or before t
-          while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (at(mid) <= t) lo = mid;
-            else hi = mid - 1;
-          }
-          i = lo;
-          behind = (int)(at(lo + 1) - t);
-        }
-      }
-    }
-    if (i >= 0) {
-      const int s = seqs ? seqs[i] : i, st = status ? status[i] : DCP_PLACE_OK;
-      if (c.is_seq(s) && st == DCP_PLACE_OK) {
-        const int pos = c.length(s) - behind;
-        if (pos >= 0 && behind > 0) {
-          const int p = c.page.quot(pos), entry = c.row(s)[p];
-          if (c.is_page(entry)) { page = entry; slot = c.page.rem(pos, p); }
-        }
-      }
-    }
-    page_of[threadIdx.x] = page;
-    slot_of[threadIdx.x] = slot;
+    const TokenPlace p = token_place(c, seqs, begins, n, status, t0 + threadIdx.x, x.n);
+    page_of[threadIdx.x] = p.page;
+    slot_of[threadIdx.x] = p.slot;
   }
   __syncthreads();
   const int all = TOKENS * c.hkv << c.log_head_chunks;   // chunks of k; as many of v
@@ -481,7 +457,8 @@ void launch_move(uint32_t grid, const KCache& c, const Moves& m, const int32_t* 
 }
 void launch_append(int32_t each, uint32_t grid, const KCache& c, int32_t layer, const int32_t* seqs, const int32_t* cu, int32_t n, const int32_t* status,
                    const NewTokens& x, hipStream_t s) {
-  if (each == 1) hipLaunchKernelGGL(append_kernel<1>, dim3(grid), dim3(256), 0, s, c, layer, seqs, cu, n, status, x);
+  if (c.k_scale) launch_append8(each, grid, c, layer, seqs, cu, n, status, x, s);
+  else if (each == 1) hipLaunchKernelGGL(append_kernel<1>, dim3(grid), dim3(256), 0, s, c, layer, seqs, cu, n, status, x);
   else hipLaunchKernelGGL(append_kernel<4>, dim3(grid), dim3(256), 0, s, c, layer, seqs, cu, n, status, x);
 }
 

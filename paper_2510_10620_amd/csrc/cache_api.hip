@@ -15,10 +15,11 @@ namespace dcp {
 static constexpr int64_t kMostStride = int64_t(1) << 58;
 static constexpr int32_t kMostLayers = 1 << 16;
 
-static bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+static bool aligned(const void* p, uintptr_t n) { return is_aligned(p, n); }
 
 // a tensor [tokens, heads, d] beside the cache
-static dcp_status_t check_rows(const char* name, const void* p, int64_t stride_t, int64_t stride_h, int32_t d) {
+dcp_status_t check_rows(const char* name, const void* p, int64_t stride_t, int64_t stride_h, const dcp_cache_t* cache) {
+  const int32_t d = cache->d;
   if (!p) return fail(DCP_ERR_INVALID_ARG, std::string(name) + " is NULL");
   if (!aligned(p, 16)) return fail(DCP_ERR_INVALID_ARG, std::string(name) + " must be 16-byte aligned");
   if (stride_h < d || stride_t < d || stride_h % 8 || stride_t % 8)
@@ -28,25 +29,31 @@ static dcp_status_t check_rows(const char* name, const void* p, int64_t stride_t
 }
 
 // Validates the descriptor and packs it for the kernels.
-static dcp_status_t pack_cache(const dcp_cache_t* cache, KCache* out) {
+dcp_status_t pack_cache(const dcp_cache_t* cache, KCache* out) {
   if (!cache) return fail(DCP_ERR_INVALID_ARG, "cache is NULL");
   const dcp_cache_t& c = *cache;
   if (c.n_layers <= 0 || c.n_pages <= 0 || c.page_size <= 0 || c.hkv <= 0 || c.d <= 0 || c.n_seqs <= 0 || c.max_pages <= 0)
     return fail(DCP_ERR_INVALID_ARG, "n_layers, n_pages, page_size, hkv, d, n_seqs, max_pages must be positive");
-  if (c.dtype != DCP_BF16 && c.dtype != DCP_F32) return fail(DCP_ERR_UNSUPPORTED, "dtype must be DCP_BF16 or DCP_F32");
+  const bool codes = c.dtype == DCP_E4M3;
+  if (!codes && c.dtype != DCP_BF16 && c.dtype != DCP_F32) return fail(DCP_ERR_UNSUPPORTED, "dtype must be DCP_BF16, DCP_F32 or DCP_E4M3");
   if (c.d != 32 && c.d != 64 && c.d != 128) return fail(DCP_ERR_UNSUPPORTED, "head_dim of a cache must be 32, 64 or 128");
   if (c.n_seqs > DCP_CACHE_MAX_SEQS) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most " + std::to_string(DCP_CACHE_MAX_SEQS) + " sequences");
   if (c.n_layers > kMostLayers) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most 65 536 layers");
   if (c.n_pages > (1 << 30)) return fail(DCP_ERR_UNSUPPORTED, "a cache holds at most 2^30 pages");
   if ((int64_t)c.max_pages * c.page_size > (1 << 30)) return fail(DCP_ERR_UNSUPPORTED, "max_pages * page_size must be at most 2^30");
-  const int32_t e = c.dtype == DCP_BF16 ? 2 : 4;
+  if (codes) {
+    if (c.io_dtype != DCP_BF16 && c.io_dtype != DCP_F32) return fail(DCP_ERR_UNSUPPORTED, "io_dtype must be DCP_BF16 or DCP_F32");
+    if (c.scale_block <= 0 || c.page_size % c.scale_block) return fail(DCP_ERR_INVALID_ARG, "scale_block must divide page_size");
+    if (!c.k_scale || !c.v_scale) return fail(DCP_ERR_INVALID_ARG, "k_scale or v_scale is NULL");
+  }
+  const int32_t e = codes ? 1 : c.dtype == DCP_BF16 ? 2 : 4, unit = codes ? 16 : 8;   // unit: elements of 16 bytes, or more
   if ((int64_t)c.page_size * c.hkv * (c.d * e / 16) > (1 << 26)) return fail(DCP_ERR_UNSUPPORTED, "a page holds at most 1 GiB of keys");
   struct { const char* name; const void* p; int64_t l, page, t, h; } kv[2] = {{"k", c.k, c.k_stride_l, c.k_stride_p, c.k_stride_t, c.k_stride_h},
                                                                               {"v", c.v, c.v_stride_l, c.v_stride_p, c.v_stride_t, c.v_stride_h}};
   for (auto& x : kv) {
     if (!x.p || !aligned(x.p, 16)) return fail(DCP_ERR_INVALID_ARG, std::string(x.name) + " of the cache is NULL or not 16-byte aligned");
-    if (x.l < c.d || x.page < c.d || x.t < c.d || x.h < c.d || x.l % 8 || x.page % 8 || x.t % 8 || x.h % 8)
-      return fail(DCP_ERR_INVALID_ARG, std::string(x.name) + " of the cache: strides must be >= d and multiples of 8 elements");
+    if (x.l < c.d || x.page < c.d || x.t < c.d || x.h < c.d || x.l % unit || x.page % unit || x.t % unit || x.h % unit)
+      return fail(DCP_ERR_INVALID_ARG, std::string(x.name) + " of the cache: strides must be >= d and multiples of " + (codes ? "16" : "8") + " elements");
     if (std::max(std::max(x.l, x.page), std::max(x.t, x.h)) > kMostStride)
       return fail(DCP_ERR_UNSUPPORTED, std::string(x.name) + " of the cache: strides of at most 2^58 elements");
   }
@@ -59,15 +66,22 @@ static dcp_status_t pack_cache(const dcp_cache_t* cache, KCache* out) {
   k.ref = c.page_ref; k.table = c.page_table; k.len = c.seq_len;
   k.n_layers = c.n_layers; k.n_pages = c.n_pages; k.hkv = c.hkv; k.n_seqs = c.n_seqs; k.max_pages = c.max_pages;
   k.max_len = c.max_pages * c.page_size;
-  for (k.log_head_chunks = 2; (16 << k.log_head_chunks) < c.d * e; k.log_head_chunks++) {}
+  for (k.log_head_chunks = 1; (16 << k.log_head_chunks) < c.d * e; k.log_head_chunks++) {}
   k.page = fast_div((uint32_t)c.page_size);
   k.heads = fast_div((uint32_t)c.hkv);
+  k.io_bytes = codes && c.io_dtype == DCP_BF16 ? 2 : codes ? 4 : e;
+  k.block = fast_div(1);
+  if (codes) {
+    k.k_scale = c.k_scale; k.v_scale = c.v_scale;
+    k.block = fast_div((uint32_t)c.scale_block);
+    k.blocks = c.page_size / c.scale_block;
+  }
   *out = k;
   return DCP_OK;
 }
 
 // n places, of sequences or (seqs NULL) the first n sequences of the cache
-static dcp_status_t check_places(const KCache& c, const int32_t* seqs, int32_t n) {
+dcp_status_t check_places(const KCache& c, const int32_t* seqs, int32_t n) {
   if (n < 0) return fail(DCP_ERR_INVALID_ARG, "n must not be negative");
   if (n > DCP_CACHE_MAX_SEQS) return fail(DCP_ERR_UNSUPPORTED, "a call has at most " + std::to_string(DCP_CACHE_MAX_SEQS) + " places");
   if (!seqs && n > c.n_seqs) return fail(DCP_ERR_INVALID_ARG, "seqs is NULL and n is more than the cache's sequences");
@@ -132,15 +146,16 @@ extern "C" dcp_status_t dcp_cache_append(const dcp_cache_t* cache, int32_t layer
   if (n_tokens > (1 << 25)) return fail(DCP_ERR_UNSUPPORTED, "dcp_cache_append covers at most 2^25 tokens");   // 2^31 threads; a grid ends below 2^32
   if (!aligned(cu_new, 4) || !aligned(status, 4)) return fail(DCP_ERR_INVALID_ARG, "cu_new or status is misaligned");
   if (n == 0 || n_tokens == 0) return DCP_OK;
-  if ((st = check_rows("k_new", k_new, k_st, k_sh, cache->d)) != DCP_OK) return st;
-  if ((st = check_rows("v_new", v_new, v_st, v_sh, cache->d)) != DCP_OK) return st;
-  const int64_t e = cache->dtype == DCP_BF16 ? 2 : 4;
+  if ((st = check_rows("k_new", k_new, k_st, k_sh, cache)) != DCP_OK) return st;
+  if ((st = check_rows("v_new", v_new, v_st, v_sh, cache)) != DCP_OK) return st;
+  const int64_t e = c.io_bytes;
   const NewTokens x{(const char*)k_new, (const char*)v_new, k_st * e, k_sh * e, v_st * e, v_sh * e, n_tokens};
   ProfScope ps(DCP_K_CACHE, (hipStream_t)stream);
   // Up to four tokens a CU a workgroup each, else four in one.  In a graph, us, with one / four: tokens of 4 KiB, 64 2.95 / 3.44, 1 024 3.7 / 3.9,
   // 2 048 4.3 / 4.4, 4 096 8.4 / 7.2, 32 768 54 / 39; of 512 bytes, 64 2.94 / 2.86, 1 024 3.25 / 3.0, 8 192 7.8 / 3.8.  83 396 of 4 KiB in
   // 2 / 4 / 8 / 16: 123 / 124 / 130 / 134 with the reserve and the map's reset.
-  const int32_t each = n_tokens <= 1024 ? 1 : 4;
+  // In 8 bits a workgroup has the blocks of tokens that begin among its own, 16 of them where there are many.
+  const int32_t each = n_tokens <= 1024 ? 1 : c.k_scale ? 16 : 4;
   launch_append(each, (uint32_t)((n_tokens + each - 1) / each), c, layer, seqs, cu_new, n, status, x, (hipStream_t)stream);
   DCP_HIP_TRY(hipGetLastError());
   return DCP_OK;
@@ -221,18 +236,18 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
   if (!(t.softmax_scale > 0.f) || !std::isfinite(t.softmax_scale)) return fail(DCP_ERR_INVALID_ARG, "softmax_scale must be positive and finite");
   if (t.window < 0 || t.sink < 0) return fail(DCP_ERR_INVALID_ARG, "window and sink must not be negative");
   if (t.n == 0) return DCP_OK;
-  if ((st = check_rows("q", t.q, t.q_stride_t, t.q_stride_h, cache->d)) != DCP_OK) return st;
-  if ((st = check_rows("out", t.out, t.o_stride_t, t.o_stride_h, cache->d)) != DCP_OK) return st;
+  if ((st = check_rows("q", t.q, t.q_stride_t, t.q_stride_h, cache)) != DCP_OK) return st;
+  if ((st = check_rows("out", t.out, t.o_stride_t, t.o_stride_h, cache)) != DCP_OK) return st;
   if (!t.lse || (reinterpret_cast<uintptr_t>(t.lse) & 3u)) return fail(DCP_ERR_INVALID_ARG, "lse is NULL or misaligned");
   if (reinterpret_cast<uintptr_t>(t.status) & 3u) return fail(DCP_ERR_INVALID_ARG, "status is misaligned");
   if (!workspace || workspace_bytes < dcp_paged_attn_workspace_bytes(cache, t.n, t.hq))
     return fail(DCP_ERR_WORKSPACE, "workspace is NULL or smaller than dcp_paged_attn_workspace_bytes");
   if (reinterpret_cast<uintptr_t>(workspace) & 255u) return fail(DCP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  const int64_t e = cache->dtype == DCP_BF16 ? 2 : 4;
+  const int64_t e = c.io_bytes;
   if (rows_overlap(Rows{t.q, t.q_stride_t * e, t.q_stride_h * e}, Rows{t.out, t.o_stride_t * e, t.o_stride_h * e}, t.n, t.hq, cache->d * e))
     return fail(DCP_ERR_INVALID_ARG, "out overlaps q");
   // Whole items: the most tiles that one can have, as far as the host knows, over the waves that take them in turn
-  const int tile = cache->dtype == DCP_F32 ? 16 : 32;
+  const int tile = cache->dtype == DCP_E4M3 ? 64 : cache->dtype == DCP_F32 ? 16 : 32;
   const int64_t most = ((t.window > 0 ? std::min<int64_t>(c.max_len, (int64_t)t.window + t.sink + 2 * tile) : c.max_len) + tile - 1) / tile;
   Sets sets = sets_of(c.hkv, t.hq, cache->d, kPagedWaves);
   if (sets.groups * sets.abreast > (1 << 12)) return fail(DCP_ERR_UNSUPPORTED, "dcp_paged_attn_fwd covers at most 4 096 sets of 16 query heads on one KV head");
@@ -243,9 +258,13 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
     if (whole) sets = x;
   }
   if (t.n * (int64_t)((c.max_len + tile - 1) / tile) * sets_of(c.hkv, t.hq, cache->d, 1).groups > INT32_MAX)
-    return fail(DCP_ERR_UNSUPPORTED, "n x hkv x sets of 16 query heads on one KV head x tiles of 32 (fp32: 16) tokens in a row of the table must be below 2^31");
+    return fail(DCP_ERR_UNSUPPORTED, "n x hkv x sets of 16 query heads on one KV head x tiles of 32 (fp32: 16, 8 bits: 64) tokens in a row of the table must be below 2^31");
   c.k += t.layer * c.k_sl;   // the layer's
   c.v += t.layer * c.v_sl;
+  if (c.k_scale) {
+    c.k_scale += t.layer * c.layer_scales();
+    c.v_scale += t.layer * c.layer_scales();
+  }
   const PagedArgs a{(const char*)t.q, (char*)t.out, t.lse, t.seqs, t.status, t.q_stride_t * e, t.q_stride_h * e, t.o_stride_t * e, t.o_stride_h * e,
                     t.n, t.hq / c.hkv, t.window, t.sink, sets.per_kv, sets.heads, sets.abreast, sets.log_abreast, (int32_t)sets.groups, whole,
                     t.softmax_scale * 1.44269504088896340736f};

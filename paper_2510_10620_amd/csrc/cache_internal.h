@@ -55,6 +55,18 @@ static constexpr int kLogWorkers = 9, kWorkers = 1 << kLogWorkers;
 static constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
 static constexpr int kSetHeads = 16;     // query heads of a matrix tile
 
+struct ReadTokens {
+  char *k, *v;
+  int64_t k_st, k_sh, v_st, v_sh;   // bytes
+  int64_t n;
+};
+
+// The checks that the calls share (cache_api.hip).
+dcp_status_t pack_cache(const dcp_cache_t* cache, KCache* out);
+dcp_status_t check_places(const KCache& c, const int32_t* seqs, int32_t n);
+dcp_status_t check_rows(const char* name, const void* p, int64_t stride_t, int64_t stride_h, const dcp_cache_t* cache);
+inline bool is_aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
 // One launch each, of `grid` workgroups where it goes by the call.
 void launch_take(bool fork, const KCache& c, const int32_t* a, const int32_t* b, int32_t n, int32_t* status, hipStream_t s);
 void launch_fork(uint32_t grid, const KCache& c, const int32_t* src, const int32_t* dst, int32_t n, const int32_t* status, int32_t pieces, hipStream_t s);
@@ -63,7 +75,12 @@ void launch_list_moves(const KCache& c, const Moves& m, int32_t* counts, hipStre
 void launch_move(uint32_t grid, const KCache& c, const Moves& m, const int32_t* counts, int32_t pieces, hipStream_t s);
 void launch_append(int32_t each, uint32_t grid, const KCache& c, int32_t layer, const int32_t* seqs, const int32_t* cu, int32_t n, const int32_t* status,
                    const NewTokens& x, hipStream_t s);   // each: tokens of a workgroup, 1 or 4
+void launch_append8(int32_t each, uint32_t grid, const KCache& c, int32_t layer, const int32_t* seqs, const int32_t* cu, int32_t n, const int32_t* status,
+                    const NewTokens& x, hipStream_t s);   // of launch_append, for a cache in 8 bits: each 1 or 16
+void launch_read(int32_t each, uint32_t grid, const KCache& c, int32_t layer, const int32_t* seqs, const int32_t* cu, int32_t n, const int32_t* status,
+                 const ReadTokens& x, hipStream_t s);     // each: 1 or 4
 // and the join where items are cut
+void launch_paged_attn8(int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s);
 void launch_paged_attn(int32_t dtype, int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s);
 
 }  // namespace dcp

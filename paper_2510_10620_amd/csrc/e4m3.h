@@ -1,0 +1,31 @@
+// Numbers of 8 bits with a scale: code x 2^(scale - 127).
+#pragma once
+#include "device_utils.h"
+
+namespace dcp {
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+// The scale's factor, as the conversions below take it: they look at its exponent alone.
+__device__ __forceinline__ float scale_factor(uint32_t scale) { return __uint_as_float(min(max(scale, 1u), 254u) << 23); }
+
+// Codes 2 HI, 2 HI + 1 of four as two bf16 numbers, exact: 4 significant bits, and 2^(scale - 127) moves the exponent.
+template <bool HI> __device__ __forceinline__ uint32_t e4m3_to_bf16x2(uint32_t four, float factor) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, factor, HI));
+}
+template <bool HI> __device__ __forceinline__ f32x2_t e4m3_to_f32x2(uint32_t four) {
+  return __builtin_bit_cast(f32x2_t, __builtin_amdgcn_cvt_pk_f32_fp8(four, HI));
+}
+// Four numbers as codes, rounded to nearest even; what is over 464, and NaN, becomes NaN.
+__device__ __forceinline__ uint32_t f32x4_to_e4m3(float a, float b, float c, float d) {
+  return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
+}
+
+// The least scale, from 10 on, whose 448 units reach a number with these bits (no sign, finite): 448 = 1.75 x 2^8.
+__device__ __forceinline__ uint32_t least_scale(uint32_t bits) {
+  const int32_t s = (int32_t)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u);
+  return (uint32_t)max(s, 10);
+}
+
+}  // namespace dcp

@@ -40,6 +40,11 @@ struct KCache {
   int32_t n_layers, n_pages, hkv, n_seqs, max_pages, max_len;   // max_len: tokens that a row of the table has room for
   int32_t log_head_chunks;   // log2 of the 16-byte chunks of one token's head
   FastDiv page, heads;
+  // in 8 bits: exponents of the scales, [layers, pages, blocks, KV heads]; else null
+  uint8_t *k_scale, *v_scale;
+  FastDiv block;             // tokens that share a scale
+  int32_t blocks;            // of a page
+  int32_t io_bytes;          // of a number beside the cache
 
   DCP_HD int32_t head_chunks() const { return 1 << log_head_chunks; }
   DCP_HD const int32_t* row(int32_t seq) const { return table + (int64_t)seq * max_pages; }
@@ -47,6 +52,9 @@ struct KCache {
   DCP_HD bool is_seq(int32_t seq) const { return (uint32_t)seq < (uint32_t)n_seqs; }
   DCP_HD bool is_page(int32_t p) const { return (uint32_t)p < (uint32_t)n_pages; }
   DCP_HD int32_t length(int32_t seq) const { const int32_t n = len[seq]; return n < 0 ? 0 : n > max_len ? max_len : n; }
+  DCP_HD int64_t layer_scales() const { return (int64_t)n_pages * blocks * hkv; }
+  // of KV head 0
+  DCP_HD int64_t scale_at(int32_t p, int32_t slot) const { return ((int64_t)p * blocks + block.quot(slot)) * hkv; }
   DCP_HD int32_t pages_of(int32_t tokens) const { const int32_t q = page.quot(tokens); return q + (q * (int32_t)page.d < tokens); }
 };
 
