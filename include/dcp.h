@@ -514,6 +514,20 @@ typedef struct {
 size_t dcp_paged_attn_workspace_bytes(const dcp_cache_t* cache, int32_t n, int32_t hq);
 dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t* args, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Attention of the last tokens of every place over its sequence, in a cache of DCP_E4M3 (those of other dtypes have dcp_block_attn_fwd over the pages, whose plan
+ * the host makes): a piece of a prompt behind the pieces before it, drafted tokens that are verified in one pass.  Place i has the rows
+ * [cu_new[i], cu_new[i + 1]) of q and out, as in dcp_cache_append, which wrote their keys and values before; the row of the token at position p sees key j iff j <= p
+ * and, with window > 0, p - j < window or j < sink.  Lengths stay on the device; the call may be captured.  Everything else as in
+ * dcp_paged_attn_fwd; rows whose position is negative, that no place has or that are not below n_tokens are not written.
+ *   args     n places; q, out [n_tokens, hq, d], lse float [hq, n_tokens]
+ *   cu_new   int32 [n + 1], device, ascending
+ *   workspace  device, >= dcp_paged_attn_chunk_workspace_bytes, 256-byte aligned, as there.  Three launches.
+ * DCP_ERR_UNSUPPORTED: another dtype; n_tokens above 2^25; n_tokens * hq of 2^31 or more; hkv times (ceil(n_tokens * hq / hkv / 128) + n) times
+ * ceil(max_pages * page_size / 64) of 2^31 or more. */
+size_t dcp_paged_attn_chunk_workspace_bytes(const dcp_cache_t* cache, int32_t n, int64_t n_tokens, int32_t hq);
+dcp_status_t dcp_paged_attn_chunk_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t* args, const int32_t* cu_new, int64_t n_tokens, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
 /* Per-kernel timing for benchmarks.  While enabled, every kernel the library launches is
  * bracketed by hipEvents recorded on the launch stream (the kernels of one backward call are timed
  * one by one; the one launch that small batches take for dQ and dK/dV together counts as DCP_K_DKV, and

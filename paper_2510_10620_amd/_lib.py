@@ -112,6 +112,8 @@ _SIGS = {
     "dcp_cache_compact": (ctypes.c_int, [ctypes.POINTER(Cache), vp, vp, ctypes.c_size_t, vp]),
     "dcp_paged_attn_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Cache), ctypes.c_int32, ctypes.c_int32]),
     "dcp_paged_attn_fwd": (ctypes.c_int, [ctypes.POINTER(Cache), ctypes.POINTER(PagedAttn), vp, ctypes.c_size_t, vp]),
+    "dcp_paged_attn_chunk_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Cache), ctypes.c_int32, ctypes.c_int64, ctypes.c_int32]),
+    "dcp_paged_attn_chunk_fwd": (ctypes.c_int, [ctypes.POINTER(Cache), ctypes.POINTER(PagedAttn), vp, ctypes.c_int64, vp, ctypes.c_size_t, vp]),
     "dcp_profile_enable": (ctypes.c_int, [ctypes.c_int32]),
     "dcp_profile_read": (ctypes.c_int, [ctypes.c_int32, ctypes.POINTER(ctypes.c_double), i64p]),
     "dcp_last_error": (ctypes.c_char_p, []),

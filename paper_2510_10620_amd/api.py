@@ -621,6 +621,24 @@ def dcp_paged_attn_fwd(cache, q, out, lse, softmax_scale, workspace, seqs=None, 
     _check(cache._lib.dcp_paged_attn_fwd(cache.ref, ctypes.byref(args), *cache._space(workspace), cache._stream()))
 
 
+def dcp_paged_attn_chunk_workspace_bytes(cache, n, n_tokens, hq):
+    return int(cache._lib.dcp_paged_attn_chunk_workspace_bytes(cache.ref, int(n), int(n_tokens), int(hq)))
+
+
+def dcp_paged_attn_chunk_fwd(cache, q, out, lse, softmax_scale, workspace, cu_new, seqs=None, window=0, sink=0, layer=0, status=None):
+    """q, out [tokens, hq, d], lse float [hq, tokens]: the last tokens of every place, rows [cu_new[i], cu_new[i + 1]), over its sequence."""
+    tokens, hq, d = q.shape
+    if out.shape != q.shape or d != cache._d:
+        raise ValueError("q, out: [tokens, hq, d] with the cache's d")
+    if lse.dtype is not cache._f32 or lse.shape != (hq, tokens) or not lse.is_contiguous() or lse.get_device() != cache._index:
+        raise ValueError("lse: contiguous float32 tensor [hq, tokens] on the cache's device")
+    n = cu_new.numel() - 1
+    args = _lib.PagedAttn(n, hq, layer, softmax_scale, window, sink, cache._ints("seqs", seqs, n), *cache._token_rows("q", q),
+                          *cache._token_rows("out", out), lse.data_ptr(), cache._ints("status", status, n))
+    _check(cache._lib.dcp_paged_attn_chunk_fwd(cache.ref, ctypes.byref(args), cache._ints("cu_new", cu_new, n + 1), tokens, *cache._space(workspace),
+                                               cache._stream()))
+
+
 KERNEL_IDS = dict(fwd=0, merge=1, delta=2, dq=3, dkv=4, sum=5, copy=6, paged_attn=7, cache=8)
 
 

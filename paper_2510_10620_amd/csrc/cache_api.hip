@@ -89,6 +89,16 @@ dcp_status_t check_places(const KCache& c, const int32_t* seqs, int32_t n) {
   return DCP_OK;
 }
 
+// heads, layer, scale and mask
+dcp_status_t check_attn_args(const KCache& c, const dcp_paged_attn_t& t) {
+  if (t.hq <= 0) return fail(DCP_ERR_INVALID_ARG, "hq must be positive");
+  if (t.hq % c.hkv != 0) return fail(DCP_ERR_UNSUPPORTED, "hq must be a multiple of hkv");
+  if (t.layer < 0 || t.layer >= c.n_layers) return fail(DCP_ERR_INVALID_ARG, "layer out of range");
+  if (!(t.softmax_scale > 0.f) || !std::isfinite(t.softmax_scale)) return fail(DCP_ERR_INVALID_ARG, "softmax_scale must be positive and finite");
+  if (t.window < 0 || t.sink < 0) return fail(DCP_ERR_INVALID_ARG, "window and sink must not be negative");
+  return DCP_OK;
+}
+
 static size_t moves_bytes(int32_t n_pages) { return 4 * (64 + 2 * (size_t)n_pages + 2); }   // count, from and to (n_pages / 2 + 1 each), where
 
 // Items are taken whole, so that nothing is to be joined, where a workgroup each is enough and none can have more than so many tiles a wave:
@@ -230,11 +240,7 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
   if (!args) return fail(DCP_ERR_INVALID_ARG, "args is NULL");
   const dcp_paged_attn_t& t = *args;
   if ((st = check_places(c, t.seqs, t.n)) != DCP_OK) return st;
-  if (t.hq <= 0) return fail(DCP_ERR_INVALID_ARG, "hq must be positive");
-  if (t.hq % c.hkv != 0) return fail(DCP_ERR_UNSUPPORTED, "hq must be a multiple of hkv");
-  if (t.layer < 0 || t.layer >= c.n_layers) return fail(DCP_ERR_INVALID_ARG, "layer out of range");
-  if (!(t.softmax_scale > 0.f) || !std::isfinite(t.softmax_scale)) return fail(DCP_ERR_INVALID_ARG, "softmax_scale must be positive and finite");
-  if (t.window < 0 || t.sink < 0) return fail(DCP_ERR_INVALID_ARG, "window and sink must not be negative");
+  if ((st = check_attn_args(c, t)) != DCP_OK) return st;
   if (t.n == 0) return DCP_OK;
   if ((st = check_rows("q", t.q, t.q_stride_t, t.q_stride_h, cache)) != DCP_OK) return st;
   if ((st = check_rows("out", t.out, t.o_stride_t, t.o_stride_h, cache)) != DCP_OK) return st;

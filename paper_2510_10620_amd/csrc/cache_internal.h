@@ -64,8 +64,32 @@ struct ReadTokens {
 // The checks that the calls share (cache_api.hip).
 dcp_status_t pack_cache(const dcp_cache_t* cache, KCache* out);
 dcp_status_t check_places(const KCache& c, const int32_t* seqs, int32_t n);
+dcp_status_t check_attn_args(const KCache& c, const dcp_paged_attn_t& t);
 dcp_status_t check_rows(const char* name, const void* p, int64_t stride_t, int64_t stride_h, const dcp_cache_t* cache);
 inline bool is_aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// dcp_paged_attn_chunk_fwd: the rows of a place and KV head (token after token, of each the query heads that share it) are taken in tiles of kChunkRows, the
+// items; kWorkers workgroups share all items' key tiles, KV head after KV head, evenly.
+static constexpr int kChunkRows = 128, kChunkKeys = 64;
+struct ChunkArgs {
+  const char* q;
+  char* out;
+  float* lse;
+  const int32_t *seqs, *status, *cu;
+  int64_t q_st, q_sh, o_st, o_sh;   // bytes
+  int64_t n_tokens;
+  int32_t n, window, sink, max_items;
+  FastDiv group;                    // query heads of a KV head
+  float scale_log2e;
+};
+struct ChunkPlan {
+  int4* head;     // [1] items, their key tiles (of one KV head)
+  int4* items;    // [max_items] place, row tile, key tiles, key tiles of those before
+  int4* starts;   // [kWorkers] KV head, item, key tile of it
+  int4* joins;    // [kWorkers] KV head, item, first worker, last worker of the item that a worker begins and does not end; item -1: none
+  float2* ml;     // [2 kWorkers][kChunkRows] running maximum, sum: of a worker's first item slot 2 w, of one that it begins and does not end 2 w + 1
+  float* o;       // [2 kWorkers][kChunkRows / 32][D / 32][4][64][4], as the lanes hold it
+};
 
 // One launch each, of `grid` workgroups where it goes by the call.
 void launch_take(bool fork, const KCache& c, const int32_t* a, const int32_t* b, int32_t n, int32_t* status, hipStream_t s);
@@ -79,6 +103,8 @@ void launch_append8(int32_t each, uint32_t grid, const KCache& c, int32_t layer,
                     const NewTokens& x, hipStream_t s);   // of launch_append, for a cache in 8 bits: each 1 or 16
 void launch_read(int32_t each, uint32_t grid, const KCache& c, int32_t layer, const int32_t* seqs, const int32_t* cu, int32_t n, const int32_t* status,
                  const ReadTokens& x, hipStream_t s);     // each: 1 or 4
+// The plan, the walk and the join.
+void launch_chunk(int32_t d, const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, hipStream_t s);
 // and the join where items are cut
 void launch_paged_attn8(int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s);
 void launch_paged_attn(int32_t dtype, int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s);

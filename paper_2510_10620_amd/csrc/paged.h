@@ -76,6 +76,23 @@ struct KeyTiles {
   DCP_HD bool sees(int32_t j) const { return (j < len) & ((j >= lo) | (j < head)); }
 };
 
+// What a place of dcp_paged_attn_chunk_fwd has: tokens [first, first + count) of the packed ones, the first of them at position pos of its sequence.
+struct ChunkPlace {
+  int32_t first, count, pos;
+  // [begin, end): the place's rows by cu_new, of which those below n_tokens are there; the last of all is the sequence's last token
+  DCP_HD ChunkPlace(int64_t begin, int64_t end, int64_t n_tokens, int32_t len) {
+    const int64_t from = end - len > begin ? end - len : begin, a = from < 0 ? 0 : from, b = end < n_tokens ? end : n_tokens;
+    count = b > a ? (int32_t)(b - a) : 0;
+    first = (int32_t)(count ? a : 0);
+    pos = (int32_t)(count ? len - (end - a) : 0);
+  }
+};
+// The keys that the tokens at positions [lo, hi] of a sequence see, some of them or all, as tiles (see KeyTiles).  Positions are below 2^30, and so is what a
+// larger window would cut off.
+DCP_HD KeyTiles chunk_tiles(int32_t lo, int32_t hi, int32_t window, int32_t sink, int32_t tile) {
+  return KeyTiles(hi + 1, window > 0 && window <= (1 << 30) ? window + (hi - lo) : 0, sink, tile);
+}
+
 // n / d by a 32-bit division where that is enough (a 64-bit one takes a few hundred instructions).
 DCP_HD int64_t quot64(int64_t n, int64_t d) { return ((uint64_t)(n | d) >> 32) == 0 ? (int64_t)((uint32_t)n / (uint32_t)d) : n / d; }
 

@@ -1,0 +1,295 @@
+"""Attention of the last tokens of every place over a paged key-value cache in 8 bits against the 64-bit oracle.  Rows that no place has, and slots
+without a token, hold NaN."""
+import numpy as np
+import pytest
+
+import paper_2510_10620_amd as P
+from oracle import e4m3
+from oracle import paged as OP
+from tests.paged8 import NAN, Held, check_rows, dtype_of, f64, ints, make_cache, randn
+
+pytestmark = pytest.mark.gpu
+
+# bf16 weights are rounded once, to half a step of 2^-8 at most; that is a relative error of each, and so of their sum over |v|
+WEIGHTS = 2.0 ** -8
+
+
+def chunk(cache, q, scale, cu, seqs=None, window=0, sink=0, layer=0, status=None, ws=None):
+    import torch
+    out, lse = torch.full_like(q, NAN), torch.full((q.shape[1], q.shape[0]), NAN, dtype=torch.float32, device="cuda")
+    if ws is None:
+        ws = torch.empty(P.dcp_paged_attn_chunk_workspace_bytes(cache, len(cu) - 1, q.shape[0], q.shape[1]), dtype=torch.uint8, device="cuda").random_()
+    P.dcp_paged_attn_chunk_fwd(cache, q, out, lse, scale, ws, ints(cu), seqs=seqs, window=window, sink=sink, layer=layer, status=status)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def rows_of(length, places, cu, tokens):
+    """(row, sequence, position) of the rows that exist"""
+    return [(t, s, int(length[s]) - cu[i + 1] + t) for i, s in enumerate(places) if 0 <= s < len(length)
+            for t in range(cu[i], min(cu[i + 1], tokens)) if int(length[s]) - cu[i + 1] + t >= 0]
+
+
+def batch(lens, new, names, pad=1):
+    places = [int(s) for s in names] + [-1] * pad
+    return places, np.concatenate([[0], np.cumsum(list(new) + [0] * pad)]).tolist()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [128, 64, 32])
+@pytest.mark.parametrize("page,block", [(1, 1), (16, 16), (20, 10), (37, 37), (64, 8), (256, 64)])
+def test_lengths_pages_and_blocks(io, d, page, block):
+    lens = [0, 1, 2, 31, 33, 63, 64, 65, 100, 129, 200, 300]
+    new = [3, 1, 2, 31, 1, 40, 64, 65, 2, 130, 0, 33]     # more than there are in the first and the tenth
+    cache, names = make_cache(lens, page, block, 2, d, io, seed=page)
+    places, cu = batch(lens, new, names)
+    q = randn((cu[-1] + 2, 6, d), io, 1)
+    out, lse = chunk(cache, q, d ** -0.5, cu, ints(places))
+    check_rows(cache, q, out, lse, d ** -0.5, rows_of(cache.seq_len.tolist(), places, cu, q.shape[0]), weights=WEIGHTS)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 3), (4, 1), (6, 2), (7, 1), (16, 1), (40, 1), (64, 2), (130, 1), (24, 8)])
+def test_heads(io, hq, hkv):
+    lens, new = [5, 300, 64], [5, 17, 3]
+    cache, names = make_cache(lens, 16, 16, hkv, 64, io, seed=hq)
+    places, cu = batch(lens, new, names)
+    q = randn((cu[-1], hq, 64), io, 2)
+    out, lse = chunk(cache, q, 0.125, cu, ints(places))
+    check_rows(cache, q, out, lse, 0.125, rows_of(cache.seq_len.tolist(), places, cu, cu[-1]), weights=WEIGHTS)
+
+
+@pytest.mark.parametrize("io,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("window,sink", [(1, 0), (1, 1), (5, 3), (16, 40), (64, 0), (100, 64), (33, 31), (5000, 7), (2 ** 31 - 1, 2 ** 31 - 1), (0, 9)])
+def test_window_and_sink(io, d, window, sink):
+    lens, new = [1, 20, 64, 130, 700], [1, 20, 9, 100, 80]
+    cache, names = make_cache(lens, 32, 16, 2, d, io)
+    places, cu = batch(lens, new, names)
+    q = randn((cu[-1], 4, d), io, 3)
+    out, lse = chunk(cache, q, d ** -0.5, cu, ints(places), window=window, sink=sink)
+    check_rows(cache, q, out, lse, d ** -0.5, rows_of(cache.seq_len.tolist(), places, cu, cu[-1]), window, sink, weights=WEIGHTS)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["token", "head", "gaps"])
+def test_layouts_layers_and_strides(io, layout):
+    import torch
+    lens, new = [40, 333, 3], [30, 40, 3]
+    cache, names = make_cache(lens, 16, 8, 3, 64, io, layers=3, layout=layout)
+    places, cu = batch(lens, new, names)
+    q = randn((cu[-1], 9, 72), io, 4)[:, :, :64]
+    rows = rows_of(cache.seq_len.tolist(), places, cu, cu[-1])
+    for layer in (0, 2):
+        out, lse = torch.full((9, cu[-1], 80), NAN, dtype=q.dtype, device="cuda").transpose(0, 1)[:, :, :64], torch.full((9, cu[-1]), NAN, device="cuda")
+        ws = torch.empty(P.dcp_paged_attn_chunk_workspace_bytes(cache, len(places), cu[-1], 9), dtype=torch.uint8, device="cuda")
+        P.dcp_paged_attn_chunk_fwd(cache, q, out, lse, 0.2, ws, ints(cu), seqs=ints(places), layer=layer)
+        check_rows(cache, q, out, lse, 0.2, rows, layer=layer, weights=WEIGHTS)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_large_scores_and_far_away_maxima(io):
+    import torch
+    cache, names = make_cache([900], 64, 16, 1, 128, io)
+    cache.k_scale[:, cache.page_table[int(names[0])][::2].long()] += 4
+    q = randn((200, 2, 128), io, 5, 3.0)
+    out, lse = chunk(cache, q, 0.3, [0, 200], ints(names))
+    check_rows(cache, q, out, lse, 0.3, rows_of(cache.seq_len.tolist(), [int(names[0])], [0, 200], 200), weights=WEIGHTS)
+
+
+def test_one_token_is_the_other_entry_point():
+    import torch
+    lens = [0, 1, 64, 65, 700, 3000]
+    cache, names = make_cache(lens, 32, 32, 2, 128)
+    q = randn((6, 8, 128), "bf16", 6)
+    out, lse = chunk(cache, q, 0.1, list(range(7)), ints(names))
+    o2, l2 = torch.full_like(out, NAN), torch.full_like(lse, NAN)
+    ws = torch.empty(P.dcp_paged_attn_workspace_bytes(cache, 6, 8), dtype=torch.uint8, device="cuda")
+    P.dcp_paged_attn_fwd(cache, q, o2, l2, 0.1, ws, seqs=ints(names))
+    held = Held(cache)
+    rows = [(i, int(s), n - 1) for i, (s, n) in enumerate(zip(names, lens)) if n]
+    check_rows(cache, q, out, lse, 0.1, rows, weights=WEIGHTS, held=held)
+    o2[0], l2[:, 0] = NAN, NAN          # an empty sequence: O = 0 there, no row here
+    check_rows(cache, q, o2, l2, 0.1, rows, held=held)
+
+
+def test_status_pages_and_rows_that_do_not_exist():
+    lens, new = [100, 100, 100, 64, 50], [20, 30, 10, 5, 40]
+    cache, names = make_cache(lens, 16, 16, 2, 128)
+    a, b, c, d, e = (int(s) for s in names)
+    cache.page_table[a, 1], cache.page_table[a, 5], cache.page_table[b, :] = -1, 10 ** 6, -5
+    places, cu = [a, b, c, d, e, 1000], [4] + (4 + np.cumsum(new + [3])).tolist()
+    q = randn((cu[5] - 7, 8, 128), "bf16", 7)               # the last rows of e are not there
+    out, lse = chunk(cache, q, 0.1, cu, ints(places), status=ints([0, 0, 1, 0, 0, 0]))
+    rows = rows_of([int(x) if s != c else 0 for s, x in enumerate(cache.seq_len.tolist())], places, cu, q.shape[0])
+    check_rows(cache, q, out, lse, 0.1, rows, weights=WEIGHTS)
+
+
+@pytest.mark.parametrize("io,d", [("bf16", 128), ("bf16", 32), ("f32", 64)])
+def test_nan_and_infinity_reach_who_sees_them(io, d):
+    import torch
+    cache, names = make_cache([200, 200, 200, 200], 16, 16, 1, d, io)
+    row = {i: cache.page_table[int(s)].tolist() for i, s in enumerate(names)}
+    k, v = cache.k.view(torch.uint8), cache.v.view(torch.uint8)
+    v[0, row[0][11], 9, 0, 7] = 0x7f        # place 0: V of token 185, number 7
+    k[0, row[1][11], 3, 0, 5] = 0xff        # place 1: K of token 179
+    v[0, row[2][12], 8:, :, :] = 0x7f       # place 2: behind the last token
+    # place 3: token 187 stands for infinities in its number 3, -infinities in 4 and both with 190 in 5
+    cache.v_scale[0, row[3][11]] = 247
+    v[0, row[3][11], :, 0, :] = 0
+    v[0, row[3][11], 11, 0, 3], v[0, row[3][11], 11, 0, 4], v[0, row[3][11], 11, 0, 5], v[0, row[3][11], 14, 0, 5] = 0x7e, 0xfe, 0x7e, 0xfe
+    places, cu = batch([200] * 4, [40] * 4, names, 0)
+    q = randn((160, 4, d), io, 8)
+    q[125, 2, 5] = NAN                      # place 3, one row
+    out, lse = chunk(cache, q, d ** -0.5, cu, ints(places))
+    o, l = f64(out), f64(lse)
+    at = lambda i: o[40 * i: 40 * i + 40]   # noqa: E731
+    assert np.isnan(at(0)[25:, :, 7]).all() and np.isfinite(at(0)[:25]).all() and np.isfinite(np.delete(at(0), 7, 2)).all() and np.isfinite(l[:, :40]).all()
+    assert np.isnan(at(1)[19:]).all() and np.isfinite(at(1)[:19]).all()
+    assert np.isfinite(at(2)).all()
+    x = at(3)
+    assert np.isnan(x[5, 2]).all()
+    x[5, 2] = x[5, 1]
+    assert np.isfinite(np.delete(x, [3, 4, 5], 2)).all() and np.isfinite(x[:27]).all()
+    assert (x[27:, :, 3] == np.inf).all() and (x[27:, :, 4] == -np.inf).all()
+    assert (x[27:30, :, 5] == np.inf).all() and np.isnan(x[30:, :, 5]).all()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_items_that_many_workgroups_share(io):
+    lens, new = [9000, 40, 5000, 700], [3, 40, 70, 300]
+    cache, names = make_cache(lens, 64, 64, 2, 128, io)
+    places, cu = batch(lens, new, names)
+    q = randn((cu[-1], 8, 128), io, 9)
+    rows = rows_of(cache.seq_len.tolist(), places, cu, cu[-1])
+    out, lse = chunk(cache, q, 0.088, cu, ints(places))
+    some = rows[::7]
+    import torch
+    keep = torch.zeros(cu[-1], dtype=torch.bool, device="cuda")
+    keep[[r for r, _, _ in some]] = True
+    assert not torch.isnan(out).any() and not torch.isnan(lse).any()
+    out[~keep], lse[:, ~keep] = NAN, NAN
+    check_rows(cache, q, out, lse, 0.088, some, weights=WEIGHTS)
+
+
+def test_thousands_of_places():
+    lens = [1 + i % 5 for i in range(3000)]
+    cache, names = make_cache(lens, 4, 4, 1, 32)
+    new = [1 + i % 3 for i in range(3000)]
+    places, cu = batch(lens, new, names)
+    q = randn((cu[-1], 2, 32), "bf16", 10)
+    out, lse = chunk(cache, q, 0.2, cu, ints(places))
+    check_rows(cache, q, out, lse, 0.2, rows_of(cache.seq_len.tolist(), places, cu, cu[-1]), weights=WEIGHTS)
+
+
+def test_begins_that_are_not_ascending_stay_inside():
+    """What the rows get is not said; nothing outside q, out and lse is touched, and the call ends."""
+    import torch
+    cache, names = make_cache([300, 300, 300], 16, 16, 2, 64)
+    q = randn((64, 4, 64), "bf16", 11)
+    room = torch.full((3, 64, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((3, 4, 64), 7.0, device="cuda")
+    for cu in ([50, 10, 64, 2], [-2 ** 31, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1], [0, 64, 0, 64]):
+        ws = torch.empty(P.dcp_paged_attn_chunk_workspace_bytes(cache, 3, 64, 4), dtype=torch.uint8, device="cuda")
+        P.dcp_paged_attn_chunk_fwd(cache, q, room[1], lse[1], 0.1, ws, ints(cu), seqs=ints(names))
+        torch.cuda.synchronize()
+    assert bool((room[0] == 7).all()) and bool((room[2] == 7).all()) and bool((lse[0] == 7).all()) and bool((lse[2] == 7).all())
+
+
+# ------------------------------------------------------------------------------------------------- as they are used
+@pytest.mark.parametrize("io,d,window,sink", [("bf16", 128, 0, 0), ("bf16", 64, 24, 4), ("f32", 32, 0, 0)])
+@pytest.mark.parametrize("graph", [False, True])
+def test_prompt_in_pieces_drafts_and_single_tokens(io, d, window, sink, graph):
+    """A prompt in two pieces, drafted tokens that are verified, then tokens one by one, for several layers; every step against the oracle, whose cache
+    takes the same steps.  graph: a step of each kind is recorded once and replayed."""
+    import torch
+    layers, hkv, hq, page, block, scale = 2, 2, 6, 16, 8, d ** -0.5
+    cache = P.Cache.empty(layers, 40, page, hkv, d, 4, 16, torch.float8_e4m3fn, scale_block=block, io_dtype=dtype_of(io))
+    held = Held(cache)
+    seqs = [2, 0, -1, 3]
+    sizes = [[37, 5, 0, 20], [30, 61, 0, 1], [4, 4, 0, 4], [4, 4, 0, 4], [1, 1, 0, 1], [1, 1, 0, 1], [1, 1, 0, 1]]
+    recorded = {}
+    for step, new in enumerate(sizes):
+        cu = np.concatenate([[0], np.cumsum(new)])
+        single = max(new) == 1 and step >= 4
+        tokens = 4 if single else int(cu[-1])
+        key = tuple(new)
+        if key not in recorded:
+            s = dict(k=torch.empty((layers, tokens, hkv, d), dtype=dtype_of(io), device="cuda"), status=ints([0] * 4), n_new=ints(new), cu=ints(cu), seqs=ints(seqs))
+            s.update(v=torch.empty_like(s["k"]), q=torch.empty((layers, tokens, hq, d), dtype=dtype_of(io), device="cuda"))
+            s.update(out=torch.empty_like(s["q"]), lse=torch.empty((layers, hq, tokens), device="cuda"))
+            size = P.dcp_paged_attn_workspace_bytes(cache, 4, hq) if single else P.dcp_paged_attn_chunk_workspace_bytes(cache, 4, tokens, hq)
+            s["ws"] = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+            def go(s=s, single=single):
+                P.dcp_cache_reserve(cache, s["seqs"], s["status"], n_new=None if single else s["n_new"])
+                for layer in range(layers):
+                    if single:
+                        P.dcp_cache_append(cache, s["k"][layer], s["v"][layer], seqs=s["seqs"], status=s["status"], layer=layer)
+                        P.dcp_paged_attn_fwd(cache, s["q"][layer], s["out"][layer], s["lse"][layer], scale, s["ws"], seqs=s["seqs"], window=window, sink=sink,
+                                             layer=layer, status=s["status"])
+                    else:
+                        P.dcp_cache_append(cache, s["k"][layer], s["v"][layer], seqs=s["seqs"], cu_new=s["cu"], status=s["status"], layer=layer)
+                        P.dcp_paged_attn_chunk_fwd(cache, s["q"][layer], s["out"][layer], s["lse"][layer], scale, s["ws"], s["cu"], seqs=s["seqs"], window=window,
+                                                   sink=sink, layer=layer, status=s["status"])
+            s["go"] = go
+            if graph:
+                g = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g):
+                    go()
+                s["go"] = g.replay
+            recorded[key] = s
+        s = recorded[key]
+        for name, seed in (("k", 1), ("v", 2), ("q", 3)):
+            s[name].copy_(randn(s[name].shape, io, 10 * step + seed))
+        s["out"].fill_(NAN)
+        s["lse"].fill_(NAN)
+        s["go"]()
+        torch.cuda.synchronize()
+        m = held.map()
+        assert s["status"].tolist() == m.reserve(seqs, [1, 1, 1, 1] if single else new) == [0] * 4
+        places_cu = list(range(5)) if single else cu.tolist()
+        for layer in range(layers):
+            e4m3.append(m, held.ks, held.vs, block, seqs, places_cu, f64(s["k"][layer]), f64(s["v"][layer]), [0] * 4, layer)
+            check_rows(cache, s["q"][layer], s["out"][layer], s["lse"][layer], scale, rows_of(held.length, seqs, places_cu, tokens), window, sink, layer,
+                       2.0 ** -15 if single else WEIGHTS, held)
+        torch.empty(1000, device="cuda").normal_().sum().item()    # other work between replays
+
+
+def test_two_streams_and_two_graphs_that_share_a_workspace():
+    import torch
+    lens, new = [500, 70, 1300], [33, 70, 9]
+    caches = [make_cache(lens, 32, 16, 2, 64, seed=s) for s in (1, 2)]
+    q = [randn((112, 4, 64), "bf16", s) for s in (3, 4)]
+    batches = [batch(lens, new, names) for _, names in caches]
+    want = [chunk(c, x, 0.125, cu, ints(places)) for (c, _), x, (places, cu) in zip(caches, q, batches)]
+    size = P.dcp_paged_attn_chunk_workspace_bytes(caches[0][0], 4, 112, 4)
+
+    def call(i, out, lse, ws, cu, seqs):
+        P.dcp_paged_attn_chunk_fwd(caches[i][0], q[i], out, lse, 0.125, ws, cu, seqs=seqs)
+    got = [(torch.full_like(q[i], NAN), torch.full_like(want[i][1], NAN)) for i in range(2)]
+    args = [(ints(cu), ints(places)) for places, cu in batches]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    spaces = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                call(i, *got[i], spaces[i], *args[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(got[i][0], want[i][0]) and torch.equal(got[i][1], want[i][1])
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(i, *got[i], spaces[0], *args[i])
+        graphs.append(g)
+    for order in ((0, 1), (1, 0, 1), (0, 0, 1)):
+        for i in range(2):
+            got[i][0].fill_(NAN)
+            got[i][1].fill_(NAN)
+        for i in order:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(got[i][0], want[i][0]) and torch.equal(got[i][1], want[i][1])
