@@ -500,7 +500,7 @@ dcp_status_t dcp_cache_compact(const dcp_cache_t* cache, int32_t* counts, void* 
  *              same strides only);  lse float [hq, n] contiguous
  *   workspace  device, >= dcp_paged_attn_workspace_bytes, 256-byte aligned; scratch, whatever it holds: calls that may run at the same
  *              time need one each.  One launch or two.
- * DCP_ERR_UNSUPPORTED: hkv * ceil(hq / hkv / 16) above 4 096; that times n times ceil(max_pages * page_size / 32) (fp32: 16, DCP_E4M3: 64) of 2^31 or more. */
+ * DCP_ERR_UNSUPPORTED: hkv * ceil(hq / hkv / 16) above 4 096; that times n times ceil(max_pages * page_size / 32) (fp32: 16) of 2^31 or more. */
 typedef struct {
   int32_t n, hq, layer;
   float softmax_scale;

@@ -12,20 +12,26 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ uint32_t finite_bits(uint32_t bits) {
-  bits &= 0x7fffffffu;
-  return bits < 0x7f800000u ? bits : 0u;
-}
-
-// The numbers of a 16-byte piece of k_new or v_new: 8 of bf16 or 4 of fp32.
+// The numbers of a 16-byte piece of k_new or v_new, 8 of bf16 or 4 of fp32, and the largest of several as bits: of both halves of a word for bf16.
 template <typename IO> struct Piece;
 template <> struct Piece<bf16_t> {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
   static constexpr int kNumbers = 8;
   static __device__ __forceinline__ float at(const u32x4& u, int y) { return __uint_as_float(y & 1 ? u[y / 2] & 0xffff0000u : u[y / 2] << 16); }
+  static __device__ __forceinline__ uint32_t larger(uint32_t top, uint32_t word) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, word & 0x7fff7fffu)));
+  }
+  static __device__ __forceinline__ uint32_t fp32_bits(uint32_t top) { return max(top << 16, top & 0xffff0000u); }
+  static __device__ __forceinline__ uint32_t finite(uint32_t word) {   // what is not becomes 0
+    return ((word & 0x7f80u) == 0x7f80u ? 0u : word & 0xffffu) | ((word & 0x7f800000u) == 0x7f800000u ? 0u : word & 0xffff0000u);
+  }
 };
 template <> struct Piece<float> {
   static constexpr int kNumbers = 4;
   static __device__ __forceinline__ float at(const u32x4& u, int y) { return __uint_as_float(u[y]); }
+  static __device__ __forceinline__ uint32_t larger(uint32_t top, uint32_t word) { return max(top, word & 0x7fffffffu); }
+  static __device__ __forceinline__ uint32_t fp32_bits(uint32_t top) { return top; }
+  static __device__ __forceinline__ uint32_t finite(uint32_t word) { return (word & 0x7f800000u) == 0x7f800000u ? 0u : word; }
 };
 
 // A wave takes a block of tokens of one head of K or V: the largest of the new values, the scale, the codes.  Bound by HBM where there are many tokens; few
@@ -38,27 +44,45 @@ __device__ __forceinline__ void append_block(const char* x, int64_t x_st, char* 
   constexpr int kHeld = 16;                                      // pieces of a lane that stay in registers: a block of up to kHeld kRows tokens is read once
   const int lane = threadIdx.x & 63, r = lane / kLanes, off = lane % kLanes;
   const uint32_t had = older ? min(max((uint32_t)*scale, 1u), 254u) : 0u;
+  x += r * x_st + off * 16;
   u32x4 held[kHeld];
-  uint32_t top = 0;
-  auto load = [&](int row) { return __builtin_nontemporal_load((const u32x4*)(x + row * x_st + off * 16)); };
-  auto measure = [&](const u32x4& u) {
-#pragma unroll
-    for (int y = 0; y < P::kNumbers; y++) top = max(top, finite_bits(__float_as_uint(P::at(u, y))));
-  };
 #pragma unroll
   for (int y = 0; y < kHeld; y++) {
     held[y] = u32x4{0, 0, 0, 0};
-    if (r + y * kRows < rows) held[y] = load(r + y * kRows);
+    if (r + y * kRows < rows) held[y] = __builtin_nontemporal_load((const u32x4*)(x + y * kRows * x_st));
   }
+  auto rest = [&](auto&& f) {   // of a longer block, which is read twice
+#pragma unroll 1
+    for (int y = kHeld * kRows; r + y < rows; y += kRows) f(y, *(const u32x4*)(x + y * x_st));
+  };
+  uint32_t top = 0;
 #pragma unroll
-  for (int y = 0; y < kHeld; y++) measure(held[y]);
-  for (int row = r + kHeld * kRows; row < rows; row += kRows) measure(*(const u32x4*)(x + row * x_st + off * 16));   // read again below
+  for (int y = 0; y < kHeld; y++)
+#pragma unroll
+    for (int z = 0; z < 4; z++) top = P::larger(top, held[y][z]);
+  rest([&](int, const u32x4& u) {
+#pragma unroll
+    for (int z = 0; z < 4; z++) top = P::larger(top, u[z]);
+  });
+  if (__any(P::fp32_bits(top) >= 0x7f800000u)) {   // an infinity or a NaN, which does not count
+    top = 0;
+#pragma unroll
+    for (int y = 0; y < kHeld; y++)
+#pragma unroll
+      for (int z = 0; z < 4; z++) top = P::larger(top, P::finite(held[y][z]));
+    rest([&](int, const u32x4& u) {
+#pragma unroll
+      for (int z = 0; z < 4; z++) top = P::larger(top, P::finite(u[z]));
+    });
+  }
+  top = P::fp32_bits(top);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
   const uint32_t now = max(had, least_scale(top));
   const float up = __uint_as_float(now >= 254 ? 0x400000u : (254 - now) << 23);   // 2^(127 - now)
-  auto store = [&](int row, const u32x4& u) {
-    char* p = to + row * to_st + off * P::kNumbers;
+  char* dst = to + r * to_st + off * P::kNumbers;
+  auto store = [&](int y, const u32x4& u) {
+    char* p = dst + y * to_st;
     if constexpr (P::kNumbers == 8) {
       *(uint2*)p = make_uint2(f32x4_to_e4m3(P::at(u, 0) * up, P::at(u, 1) * up, P::at(u, 2) * up, P::at(u, 3) * up),
                               f32x4_to_e4m3(P::at(u, 4) * up, P::at(u, 5) * up, P::at(u, 6) * up, P::at(u, 7) * up));
@@ -68,11 +92,12 @@ __device__ __forceinline__ void append_block(const char* x, int64_t x_st, char* 
   };
 #pragma unroll
   for (int y = 0; y < kHeld; y++)
-    if (r + y * kRows < rows) store(r + y * kRows, held[y]);
-  for (int row = r + kHeld * kRows; row < rows; row += kRows) store(row, *(const u32x4*)(x + row * x_st + off * 16));
+    if (r + y * kRows < rows) store(y * kRows, held[y]);
+  rest(store);
   if (older && now > had) {   // the earlier tokens' codes, from what they stand for: exact but for numbers that fall below the format's normal ones
     const float down = __uint_as_float((uint32_t)max((int)had - (int)now + 127, 1) << 23);
     constexpr int kWords = D / 4;
+#pragma unroll 1
     for (int y = lane; y < older * kWords; y += 64) {
       char* p = to - (int64_t)(older - y / kWords) * to_st + y % kWords * 4;
       const uint32_t u = *(const uint32_t*)p;
@@ -86,7 +111,7 @@ __device__ __forceinline__ void append_block(const char* x, int64_t x_st, char* 
 // A workgroup has TOKENS tokens, of which those count that begin a block or their place: the block is theirs, with the new tokens behind
 // them.  Column y of the grid: four of the 2 hkv heads of K and V, one a wave.
 template <typename IO, int D, int TOKENS>
-__global__ __launch_bounds__(256) void append8_kernel(KCache c, int32_t layer, const int32_t* __restrict__ seqs, const int32_t* __restrict__ cu, int32_t n,
+__global__ __launch_bounds__(256, sizeof(IO) == 4 ? 2 : 4) void append8_kernel(KCache c, int32_t layer, const int32_t* __restrict__ seqs, const int32_t* __restrict__ cu, int32_t n,
                                                       const int32_t* __restrict__ status, NewTokens x) {
   __shared__ int32_t page_of[TOKENS], slot_of[TOKENS], rows_of[TOKENS], older_of[TOKENS], s_cu[kCuInLds];
   const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
@@ -108,14 +133,12 @@ __global__ __launch_bounds__(256) void append8_kernel(KCache c, int32_t layer, c
     if (page < 0) continue;
     const int64_t at = c.scale_at(page, slot_of[y]), slot = slot_of[y];
     for (int64_t col = blockIdx.y * 4 + wave; col < 2 * (int64_t)c.hkv; col += gridDim.y * 4) {
-      const bool is_v = col >= c.hkv;
-      const int64_t h = is_v ? col - c.hkv : col;
-      if (!is_v)
-        append_block<IO, D>(x.k + (t0 + y) * x.k_st + h * x.k_sh, x.k_st, c.k + layer * c.k_sl + page * c.k_sp + slot * c.k_st + h * c.k_sh, c.k_st,
-                            c.k_scale + layer * c.layer_scales() + at + h, rows_of[y], older_of[y]);
-      else
-        append_block<IO, D>(x.v + (t0 + y) * x.v_st + h * x.v_sh, x.v_st, c.v + layer * c.v_sl + page * c.v_sp + slot * c.v_st + h * c.v_sh, c.v_st,
-                            c.v_scale + layer * c.layer_scales() + at + h, rows_of[y], older_of[y]);
+      const bool v = col >= c.hkv;
+      const int64_t h = v ? col - c.hkv : col;
+      const int64_t x_st = v ? x.v_st : x.k_st, to_st = v ? c.v_st : c.k_st;
+      append_block<IO, D>((v ? x.v : x.k) + (t0 + y) * x_st + h * (v ? x.v_sh : x.k_sh), x_st,
+                          (v ? c.v + layer * c.v_sl + page * c.v_sp + h * c.v_sh : c.k + layer * c.k_sl + page * c.k_sp + h * c.k_sh) + slot * to_st, to_st,
+                          (v ? c.v_scale : c.k_scale) + layer * c.layer_scales() + at + h, rows_of[y], older_of[y]);
     }
   }
 }

@@ -15,11 +15,12 @@ __device__ __forceinline__ float upper(float x) { return __uint_as_float(__float
 // numbers, and D / 16 bytes of each of 16 rows of V.  Codes become bf16 numbers with their scale in one conversion for two of them, without
 // rounding, so that the products take them as they take a cache in bf16.  IO is bf16 or fp32; an fp32 query goes in as three bf16 parts, and so do
 // the weights: exact products, summed in fp32.
-template <typename IO, int D> struct Tile8 {
+// HALVES: 2, and 1 for tiles of 32 keys where groups of 16 do not share a page and a scale (every key then has its own entry of the table, or every eight).
+template <typename IO, int D, int HALVES> struct Tile8 {
   typedef IO Out;
   static constexpr int kD = D, kRowBytes = D;
-  static constexpr bool kScaled = true, kF32 = sizeof(IO) == 4;
-  static constexpr int kGroup = 16, kKeys = 64, kRowTiles = 4, kAcc = D / 16;
+  static constexpr bool kScaled = true, kF32 = sizeof(IO) == 4, kUngrouped = HALVES == 1;
+  static constexpr int kGroup = 8 * HALVES, kKeys = 32 * HALVES, kRowTiles = 2 * HALVES, kAcc = D / 16;
   static constexpr int kSteps = D / 32;                     // products of 32 numbers of a row
   static constexpr int kVWords = D >= 64 ? D / 64 : 1;      // 4-byte words of a lane's columns of V
   static constexpr int kParts = kF32 ? 3 : 1;
@@ -114,7 +115,7 @@ template <typename IO, int D> struct Tile8 {
   // bf16: two parts of the weights, the first of them below the weight, as for a cache in bf16; fp32: three.
   template <int COLS> __device__ __forceinline__ void weigh(const float* p, bool second, f32x4* acc) const {
 #pragma unroll
-    for (int half = 0; half < 2; half++) {
+    for (int half = 0; half < HALVES; half++) {
       constexpr int kProducts = kF32 ? 3 : COLS == 8 ? 1 : 2;
       uint4 b[kProducts];
       float x[8];
@@ -167,11 +168,16 @@ template <typename IO, int D> struct Tile8 {
   static __device__ __forceinline__ int first(int r, int, int g) { return (4 * g + r) * kAcc; }
 };
 
+template <typename IO, int COLS, int HALVES>
+void launch8(int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
+  if (d == 128) launch_tiles<Tile8<IO, 128, HALVES>, COLS>(grid, c, a, parts, s);
+  else if (d == 64) launch_tiles<Tile8<IO, 64, HALVES>, COLS>(grid, c, a, parts, s);
+  else launch_tiles<Tile8<IO, 32, HALVES>, COLS>(grid, c, a, parts, s);
+}
 template <typename IO, int COLS>
 void launch8(int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
-  if (d == 128) launch_tiles<Tile8<IO, 128>, COLS>(grid, c, a, parts, s);
-  else if (d == 64) launch_tiles<Tile8<IO, 64>, COLS>(grid, c, a, parts, s);
-  else launch_tiles<Tile8<IO, 32>, COLS>(grid, c, a, parts, s);
+  if (paged8_tile(c) == 64) launch8<IO, COLS, 2>(d, grid, c, a, parts, s);
+  else launch8<IO, COLS, 1>(d, grid, c, a, parts, s);
 }
 
 }  // namespace

@@ -167,13 +167,18 @@ template <int D> struct Staged {
   }
   // As bf16 numbers; a key that is not there as zeros.  Sixteen lanes write 16 chunks of 16 bytes in four rows at a time, which fall into all banks if every
   // other row (D 64: pair of rows) writes its odd chunks first.
-  static __device__ __forceinline__ void write(char* tile, const uint32_t (&w)[kPieces][kWords], uint32_t scale) {
+  // CLEAN: what is not finite is left out (written as 0).
+  template <bool CLEAN> static __device__ __forceinline__ void write(char* tile, const uint32_t (&w)[kPieces][kWords], uint32_t scale) {
     typedef TileLayout<D> L;
     const float factor = scale_factor(scale);
     const int key = key_of(threadIdx.x), part = threadIdx.x & 3, odd = D == 128 ? key & 1 : (key >> 1) & 1;
     auto put = [&](int chunk, uint32_t a, uint32_t b) {
-      *(uint4*)(tile + L::off(key, chunk)) =
-          make_uint4(e4m3_to_bf16x2<false>(a, factor), e4m3_to_bf16x2<true>(a, factor), e4m3_to_bf16x2<false>(b, factor), e4m3_to_bf16x2<true>(b, factor));
+      uint32_t n[4] = {e4m3_to_bf16x2<false>(a, factor), e4m3_to_bf16x2<true>(a, factor), e4m3_to_bf16x2<false>(b, factor), e4m3_to_bf16x2<true>(b, factor)};
+      if constexpr (CLEAN) {
+#pragma unroll
+        for (int y = 0; y < 4; y++) n[y] = ((n[y] & 0x7f80u) == 0x7f80u ? 0u : n[y] & 0xffffu) | ((n[y] & 0x7f800000u) == 0x7f800000u ? 0u : n[y] & 0xffff0000u);
+      }
+      *(uint4*)(tile + L::off(key, chunk)) = make_uint4(n[0], n[1], n[2], n[3]);
     };
 #pragma unroll
     for (int x = 0; x < kPieces; x++) {
@@ -186,7 +191,7 @@ template <int D> struct Staged {
     }
   }
   // whether a number of V may not be finite as bf16: a NaN, or a scale that reaches 2^128
-  __device__ __forceinline__ bool odd_values() const {
+  __device__ __forceinline__ bool may_not_be_finite() const {
     uint32_t bad = 0;
 #pragma unroll
     for (int x = 0; x < kPieces; x++)
@@ -216,7 +221,7 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
   constexpr int kParts = sizeof(IO) == 4 ? 3 : 1;
   __shared__ __attribute__((aligned(1024))) char stages[4 * L::kBytes];   // two stages, each [K tile | V tile]
   __shared__ __attribute__((aligned(8))) uint16_t s_there[2][4];
-  __shared__ uint32_t s_odd[2][4];
+  __shared__ int32_t s_odd[2];   // by turns: the last piece of work that met a number of V that is not finite where not every row sees it
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), li = lane & 31, lh = lane >> 5;
   // Workgroups go to the 8 XCDs round-robin: an XCD's workers have neighbouring shares, so that its L2 serves their keys.
   const int w = (blockIdx.x & 7) * (kWorkers / 8) + (blockIdx.x >> 3);
@@ -229,8 +234,10 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
   int hk = uni(start.x), item = uni(start.y), t0 = uni(start.z), left = sh.start(w + 1) - sh.start(w);
   Frags<D> fa;
   fa.init(lane);
+  if (tid < 2) s_odd[tid] = -1;
+  __syncthreads();
 
-  while (left > 0) {
+  for (int piece = 0; left > 0; piece++) {
     const int4 it = plan.items[item];
     const int place = uni(it.x), count = uni(it.z);
     int32_t seq;
@@ -287,15 +294,20 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
     Staged<D> st;
     auto base_of = [&](int x) { return keys.tile_at(x) * kChunkKeys; };
     auto entry_of = [&](int x) { return x < t1 ? Staged<D>::look(c, table, base_of(x), keys.len) : -1; };
+    // every row of the workgroup sees all keys of the tile that are there
+    auto seen_by_all = [&](int base) { return base + kChunkKeys - 1 <= lo && (a.window <= 0 || hi - base < a.window || base + kChunkKeys <= a.sink); };
     auto publish = [&](int stage, int base) {
       st.drop_missing();
       char* tile = stages + stage * 2 * L::kBytes;
-      Staged<D>::write(tile, st.k, st.ks);
-      Staged<D>::write(tile + L::kBytes, st.v, st.vs);
+      Staged<D>::template write<false>(tile, st.k, st.ks);
+      // Where some row does not see every key, 0 x V would carry an infinity or a NaN to it: they are left out here and added at the end.
+      if (!seen_by_all(base) && __any(st.may_not_be_finite())) {
+        Staged<D>::template write<true>(tile + L::kBytes, st.v, st.vs);
+        if (lane == 0) s_odd[piece & 1] = piece;
+      } else {
+        Staged<D>::template write<false>(tile + L::kBytes, st.v, st.vs);
+      }
       const uint64_t there = __ballot(st.there);   // four lanes a key
-      const bool edge = base + kChunkKeys > lo || a.window > 0;
-      const bool odd = edge && __any(st.odd_values());
-      if (lane == 0) s_odd[stage][wave] = odd;
       uint32_t bits = 0;
 #pragma unroll
       for (int x = 0; x < 16; x++) bits |= (uint32_t)(there >> (4 * x) & 1) << x;
@@ -330,19 +342,14 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
               for (int part = 0; part < kParts; part++) s[kt] = mfma(kf, q[part][ks], s[kt]);
             }
           }
-          uint32_t seen[2] = {0xffffu, 0xffffu};
           if (!all) {
+            auto below = [](int x) { return x <= 0 ? uint64_t(0) : x >= 64 ? ~uint64_t(0) : (uint64_t(1) << x) - 1; };
+            const uint64_t sees = ((below(row.pos + 1 - base) & ~below(low - base)) | below(head_end - base)) & there;
+            const uint32_t seen[2] = {(uint32_t)sees >> (4 * lh), (uint32_t)(sees >> 32) >> (4 * lh)};   // bit 8 (y / 4) + y % 4: the key of s[kt][y]
 #pragma unroll
-            for (int kt = 0; kt < 2; kt++) {
-              seen[kt] = 0;
+            for (int kt = 0; kt < 2; kt++)
 #pragma unroll
-              for (int y = 0; y < 16; y++) {
-                const int at_key = 32 * kt + 8 * (y / 4) + 4 * lh + y % 4, j = base + at_key;
-                const bool sees = (there >> at_key & 1) & (j <= row.pos) & ((j >= low) | (j < head_end));
-                s[kt][y] = sees ? s[kt][y] : -INFINITY;
-                seen[kt] |= (uint32_t)sees << y;
-              }
-            }
+              for (int y = 0; y < 16; y++) s[kt][y] = seen[kt] >> (8 * (y / 4) + y % 4) & 1 ? s[kt][y] : -INFINITY;
           }
           float mx = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
@@ -359,7 +366,6 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
               for (int y = 0; y < 16; y++) o[dt][y] *= alpha;
           }
           m = m_new;
-          const bool odd = !all && (s_odd[stage][0] | s_odd[stage][1] | s_odd[stage][2] | s_odd[stage][3]);
 #pragma unroll
           for (int kt = 0; kt < 2; kt++) {
             float sum = 0.f;
@@ -374,51 +380,11 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
               bf16x8 pf[kParts];
               if constexpr (kParts == 1) pf[0] = pack_frag(s[kt], cc);
               else pack_split(s[kt], cc, pf);
-              if (!odd) {
 #pragma unroll
-                for (int dt = 0; dt < L::DT; dt++) {
-                  const bf16x8 vf = fa.cols(v_lds, 2 * kt + cc, dt);
+              for (int dt = 0; dt < L::DT; dt++) {
+                const bf16x8 vf = fa.cols(v_lds, 2 * kt + cc, dt);
 #pragma unroll
-                  for (int part = 0; part < kParts; part++) o[dt] = mfma(vf, pf[part], o[dt]);
-                }
-              } else {
-                // Some number of V is an infinity or a NaN, and some row does not see every key: 0 x V would carry it there.  What is finite is
-                // multiplied as ever, what is not is counted by the rows that see it.
-                uint4 ones;
-                uint32_t* words = (uint32_t*)&ones;
-#pragma unroll
-                for (int y = 0; y < 4; y++)
-                  words[y] = (seen[kt] >> (8 * cc + 2 * y) & 1 ? 0x3f80u : 0u) | (seen[kt] >> (8 * cc + 2 * y + 1) & 1 ? 0x3f800000u : 0u);
-#pragma unroll 1
-                for (int kind = 0; kind < 3; kind++) {   // NaN, infinity, -infinity
-#pragma unroll
-                  for (int dt = 0; dt < L::DT; dt++) {
-                    uint4 vf = __builtin_bit_cast(uint4, fa.cols(v_lds, 2 * kt + cc, dt)), is, fine;
-                    uint32_t *vw = (uint32_t*)&vf, *iw = (uint32_t*)&is, *fw = (uint32_t*)&fine;
-#pragma unroll
-                    for (int y = 0; y < 4; y++) {
-                      iw[y] = fw[y] = 0;
-#pragma unroll
-                      for (int z = 0; z < 2; z++) {
-                        const uint32_t u = vw[y] >> (16 * z) & 0xffffu, size = u & 0x7fffu;
-                        const bool that = kind == 0 ? size > 0x7f80u : u == (kind == 1 ? 0x7f80u : 0xff80u);
-                        iw[y] |= that ? 0x3f80u << (16 * z) : 0u;
-                        fw[y] |= size < 0x7f80u ? u << (16 * z) : 0u;
-                      }
-                    }
-                    if (kind == 0) {
-#pragma unroll
-                      for (int part = 0; part < kParts; part++) o[dt] = mfma(as_frag(fine), pf[part], o[dt]);
-                    }
-                    f32x16 n;
-#pragma unroll
-                    for (int y = 0; y < 16; y++) n[y] = 0.f;
-                    n = mfma(as_frag(is), as_frag(ones), n);
-#pragma unroll
-                    for (int y = 0; y < 16; y++)
-                      if (n[y] > 0.f) o[dt][y] += kind == 0 ? NAN : kind == 1 ? INFINITY : -INFINITY;
-                  }
-                }
+                for (int part = 0; part < kParts; part++) o[dt] = mfma(vf, pf[part], o[dt]);
               }
             }
           }
@@ -442,6 +408,34 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
           for (int y = 0; y < 4; y++)
             *(float4*)(part + ((dt * 4 + y) * 64 + lane) * 4) = make_float4(o[dt][4 * y], o[dt][4 * y + 1], o[dt][4 * y + 2], o[dt][4 * y + 3]);
         if (lh == 0) plan.ml[slot * kChunkRows + wave * 32 + li] = make_float2(m2, l);
+      }
+      if (s_odd[piece & 1] == piece) {   // rare: written by the lane that wrote the number before, straight into memory
+        char* out = a.out + row.token * a.o_st + row.head * a.o_sh;
+        float* part = plan.o + ((int64_t)(2 * w + (t0 == 0)) * (kChunkRows / 32) + wave) * (32 * D);
+        const bool done = t0 == 0 && t1 == count;
+        for (int x = t0; x < t1; x++) {
+          const int base = base_of(x);
+          if (seen_by_all(base)) continue;
+          for (int j = base; j < min(base + kChunkKeys, keys.len); j++) {
+            const int32_t q_page = c.page.quot(j), page = table[q_page], slot = c.page.rem(j, q_page);
+            if (!c.is_page(page)) continue;
+            const char* v = c.v + page * c.v_sp + slot * c.v_st + hk * c.v_sh;
+            const float factor = scale_factor(c.v_scale[c.scale_at(page, slot) + hk]);
+            const bool sees = row.real & (j <= row.pos) & ((j >= low) | (j < head_end));
+            for (int d0 = 0; d0 < D; d0 += 64) {
+              const uint32_t code = d0 + lane < D ? *(const uint8_t*)(v + d0 + lane) : 0u;
+              const uint32_t number = e4m3_to_bf16x2<false>(code, factor) << 16;
+              for (uint64_t left_over = __ballot((number & 0x7f800000u) == 0x7f800000u); left_over; left_over &= left_over - 1) {
+                const int at_lane = __ffsll((unsigned long long)left_over) - 1, d = d0 + at_lane;
+                const float add = __shfl(__uint_as_float(number), at_lane);
+                if (!sees || lh != (d >> 2 & 1)) continue;
+                if (!done) part[((d / 32 * 4 + d / 8 % 4) * 64 + lane) * 4 + d % 4] += add;
+                else if constexpr (sizeof(IO) == 4) *(float*)(out + 4 * d) += add;
+                else *(uint16_t*)(out + 2 * d) = f32_to_bf16(bf16_to_f32(*(const uint16_t*)(out + 2 * d)) + add);
+              }
+            }
+          }
+        }
       }
     }
     if (t0 == 0 && t1 < count && tid == 0) {
