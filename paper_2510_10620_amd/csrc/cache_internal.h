@@ -71,9 +71,10 @@ dcp_status_t check_attn_args(const KCache& c, const dcp_paged_attn_t& t);
 dcp_status_t check_rows(const char* name, const void* p, int64_t stride_t, int64_t stride_h, const dcp_cache_t* cache);
 inline bool is_aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// dcp_paged_attn_chunk_fwd: the rows of a place and KV head (token after token, of each the query heads that share it) are taken in tiles of kChunkRows, the
-// items; kWorkers workgroups share all items' key tiles, KV head after KV head, evenly.
-static constexpr int kChunkRows = 128, kChunkKeys = 64;
+// dcp_paged_attn_chunk_fwd: the rows of a place and KV head (token after token, of each the query heads that share it) are taken in tiles of `rows`, the
+// items; kWorkers workgroups share all items' key tiles, KV head after KV head, evenly.  Tiles have 128 rows and 64 keys in LDS, or, where places
+// have kFewRows between them on average at most, 16 or 32 rows and keys in registers, as for one token.
+static constexpr int kChunkRows = 128, kChunkKeys = 64, kFewRows = 32;
 struct ChunkArgs {
   const char* q;
   char* out;
@@ -82,16 +83,25 @@ struct ChunkArgs {
   int64_t q_st, q_sh, o_st, o_sh;   // bytes
   int64_t n_tokens;
   int32_t n, window, sink, max_items;
+  int32_t rows, tile;               // of an item at most; keys of a tile
   FastDiv group;                    // query heads of a KV head
   float scale_log2e;
 };
+struct ChunkItem {
+  int32_t seq, first, pos, rows;      // first token of the place (of the packed ones) and its position; rows of the place
+  int32_t row0, tiles, before, pad;   // first row of the item; its key tiles, and those of the items before
+};
+struct ChunkJoin {
+  int32_t hk, first_worker, last_worker, pad;   // last_worker -1: nothing to join
+  int32_t first, rows, row0, pad2;              // of the item
+};
 struct ChunkPlan {
-  int4* head;     // [1] items, their key tiles (of one KV head)
-  int4* items;    // [max_items] place, row tile, key tiles, key tiles of those before
-  int4* starts;   // [kWorkers] KV head, item, key tile of it
-  int4* joins;    // [kWorkers] KV head, item, first worker, last worker of the item that a worker begins and does not end; item -1: none
-  float2* ml;     // [2 kWorkers][kChunkRows] running maximum, sum: of a worker's first item slot 2 w, of one that it begins and does not end 2 w + 1
-  float* o;       // [2 kWorkers][kChunkRows / 32][D / 32][4][64][4], as the lanes hold it
+  int4* head;        // [1] items, their key tiles (of one KV head)
+  ChunkItem* items;  // [max_items]
+  int4* starts;      // [kWorkers] KV head, item, key tile of it
+  ChunkJoin* joins;  // [kWorkers] by the worker that begins an item and does not end it
+  float2* ml;        // [2 kWorkers][rows] running maximum, sum: of an item that a worker does not begin slot 2 w, of one that it does 2 w + 1
+  float* o;          // [2 kWorkers][rows][D], unnormalised
 };
 
 // One launch each, of `grid` workgroups where it goes by the call.
@@ -107,6 +117,7 @@ void launch_append8(int32_t each, uint32_t grid, const KCache& c, int32_t layer,
 void launch_read(int32_t each, uint32_t grid, const KCache& c, int32_t layer, const int32_t* seqs, const int32_t* cu, int32_t n, const int32_t* status,
                  const ReadTokens& x, hipStream_t s);     // each: 1 or 4
 // The plan, the walk and the join.
+void launch_chunk_few(int32_t d, const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, hipStream_t s);   // the walk with keys in registers
 void launch_chunk(int32_t d, const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, hipStream_t s);
 // and the join where items are cut
 void launch_paged_attn8(int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s);

@@ -22,6 +22,14 @@ __device__ __forceinline__ uint32_t f32x4_to_e4m3(float a, float b, float c, flo
   return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
 
+// The sign bits of those of four codes that are not finite as bf16 and fp32 numbers: NaN, and with a scale s from 247 on what reaches 2^128 = 256 x 2^120, code 0x78,
+// eight codes (a power of two) earlier for each further scale.
+__device__ __forceinline__ uint32_t not_finite(uint32_t four, uint32_t scale) {
+  const uint32_t least = scale < 247 ? 0x7f : 0x78 - 8 * (min(scale, 254u) - 247);
+  return ((four & 0x7f7f7f7fu) + (0x80 - least) * 0x01010101u) & 0x80808080u;
+}
+__device__ __forceinline__ uint32_t without(uint32_t four, uint32_t signs) { return four & ~((signs >> 7) * 0xffu); }   // those as 0
+
 // The least scale, from 10 on, whose 448 units reach a number with these bits (no sign, finite): 448 = 1.75 x 2^8.
 __device__ __forceinline__ uint32_t least_scale(uint32_t bits) {
   const int32_t s = (int32_t)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u);

@@ -1,8 +1,7 @@
 // Attention of the last tokens of every sequence over a paged key-value cache in 8 bits: pieces of prompts, tokens to be verified.
 #include <climits>
 
-#include "cache_internal.h"
-#include "e4m3.h"
+#include "paged_chunk.h"
 #include "tile_layout.h"
 
 using namespace dcp;
@@ -19,18 +18,6 @@ __device__ __forceinline__ ChunkPlace chunk_place(const KCache& c, const ChunkAr
   *seq = code == DCP_PLACE_OK && c.is_seq(s) ? s : -1;
   return *seq < 0 ? ChunkPlace(0, 0, 0, 0) : ChunkPlace(a.cu[i], a.cu[i + 1], a.n_tokens, c.length(s));
 }
-
-// The tokens of a row tile of a place.
-struct RowTile {
-  int32_t r0, rows;   // first row, rows that are there
-  int32_t lo, hi;     // positions of the first and the last
-  __device__ __forceinline__ RowTile(const ChunkArgs& a, const ChunkPlace& p, int tile) {
-    r0 = tile * kChunkRows;
-    rows = min(p.count * (int)a.group.d - r0, kChunkRows);
-    lo = p.pos + a.group.quot(r0);
-    hi = p.pos + a.group.quot(r0 + rows - 1);
-  }
-};
 
 // One workgroup lists the items with their key tiles and where every worker begins.  Bound by latency: two dependent trips to memory for the places, one for the workers.
 __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(KCache c, ChunkArgs a, ChunkPlan plan) {
@@ -59,7 +46,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(KCache c, Chun
   for (int base = 0; base < a.n; base += kPlanThreads) {
     const int i = base + tid;
     int mine = 0, all;
-    if (i < a.n) mine = (int)(((int64_t)chunk_place(c, a, i, &seq).count * a.group.d + kChunkRows - 1) / kChunkRows);
+    if (i < a.n) mine = (int)(((int64_t)chunk_place(c, a, i, &seq).count * a.group.d + a.rows - 1) / a.rows);
     const int x = block_sum(min(mine, a.max_items), a.max_items, &all);   // cu_new that is not ascending may name more rows than there are: what is beyond max_items is left out
     if (i < a.n) upto[i] = add_capped(n_items, x, a.max_items);
     n_items = add_capped(n_items, all, a.max_items);
@@ -68,7 +55,8 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(KCache c, Chun
   int tiles = 0;
   for (int base = 0; base < n_items; base += kPlanThreads) {
     const int i = base + tid;
-    int count = 0, place = 0, tile = 0, all;
+    int all;
+    ChunkItem item{};
     if (i < n_items) {
       int lo = 0, hi = a.n - 1;   // the first place whose sum is above i
       while (lo < hi) {
@@ -76,77 +64,70 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(KCache c, Chun
         if (upto[mid] > i) hi = mid;
         else lo = mid + 1;
       }
-      place = lo;
-      tile = i - (lo ? upto[lo - 1] : 0);
+      const int place = lo, tile = i - (lo ? upto[lo - 1] : 0);
       const ChunkPlace p = chunk_place(c, a, place, &seq);
-      const RowTile r(a, p, tile);
-      count = chunk_tiles(r.lo, r.hi, a.window, a.sink, kChunkKeys).count;
+      item = ChunkItem{seq, p.first, p.pos, p.count * (int)a.group.d, tile * a.rows, 0, 0, 0};
+      item.tiles = chunk_tiles(p.pos + a.group.quot(item.row0), p.pos + a.group.quot(min(item.row0 + a.rows, item.rows) - 1), a.window, a.sink, a.tile).count;
     }
-    const int x = block_sum(count, INT_MAX, &all);   // the host has seen to it that the sum is below 2^31
-    if (i < n_items) plan.items[i] = make_int4(place, tile, count, tiles + x - count);
+    const int x = block_sum(item.tiles, INT_MAX, &all);   // the host has seen to it that the sum is below 2^31
+    if (i < n_items) {
+      item.before = tiles + x - item.tiles;
+      plan.items[i] = item;
+    }
     tiles += all;
   }
   __syncthreads();
   if (tid == 0) *plan.head = make_int4(n_items, tiles, 0, 0);
   if (tid < kWorkers) {
-    plan.joins[tid] = make_int4(0, -1, 0, 0);
+    plan.joins[tid] = ChunkJoin{0, 0, -1, 0, 0, 0, 0, 0};
     const Shares<kLogWorkers> sh(tiles * c.hkv);   // below 2^31: the host has seen to it
     if (tid < sh.workers) {
       const int at = sh.start(tid), head = (int)((uint32_t)at / (uint32_t)tiles), rel = at - head * tiles;
       int lo = 0, hi = n_items - 1;   // the last item that begins at or before it
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (plan.items[mid].w <= rel) lo = mid;
+        if (plan.items[mid].before <= rel) lo = mid;
         else hi = mid - 1;
       }
-      plan.starts[tid] = make_int4(head, lo, rel - plan.items[lo].w, 0);
+      plan.starts[tid] = make_int4(head, lo, rel - plan.items[lo].before, 0);
     }
   }
 }
 
-// A wave's 32 rows: lane l has row l % 32 (both halves the same).
-struct Row {
-  bool real;
-  int32_t pos, token, head;   // token: of the packed ones; head: query head
-};
-
-// O^T of a wave (lane = row, register 4 x + y of tile dt: number 32 dt + 8 x + 4 h + y) to out, and the LSE.
+// O^T of a wave (lane = row, register 4 x + y of tile dt: number 32 dt + 8 x + 4 h + y) times `by`, as numbers of IO.
 template <typename IO, int D>
-__device__ __forceinline__ void store_row(const ChunkArgs& a, const Row& row, const f32x16* o, float m, float l, int dt0, int n_dt, bool lse) {
+__device__ __forceinline__ void store_row(char* out, const f32x16 (&o)[D / 32], float by) {
   const int lh = (threadIdx.x & 63) >> 5;
-  if (!row.real) return;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  char* out = a.out + row.token * a.o_st + row.head * a.o_sh;
-  for (int dt = 0; dt < n_dt; dt++)
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++)
 #pragma unroll
     for (int x = 0; x < 4; x++) {
       float v[4];
 #pragma unroll
-      for (int y = 0; y < 4; y++) v[y] = l == 0.f ? 0.f : o[dt][4 * x + y] * inv;
-      const int at = 32 * (dt0 + dt) + 8 * x + 4 * lh;
+      for (int y = 0; y < 4; y++) v[y] = by == 0.f ? 0.f : o[dt][4 * x + y] * by;
+      const int at = 32 * dt + 8 * x + 4 * lh;
       if constexpr (sizeof(IO) == 4) *(float4*)(out + 4 * at) = make_float4(v[0], v[1], v[2], v[3]);
       else *(uint2*)(out + 2 * at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
     }
-  if (lse && lh == 0) a.lse[row.head * a.n_tokens + row.token] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.6931471805599453f + logf(l);
 }
 
 // The keys and values of a tile of 64 on their way into LDS: thread t has 4 (D 32: 2) words of 16 (8) codes at a time of key t / 4.
 template <int D> struct Staged {
   static constexpr int kPieces = D >= 64 ? D / 64 : 1, kWords = D >= 64 ? 4 : 2;
   uint32_t k[kPieces][kWords], v[kPieces][kWords];
-  uint32_t ks, vs;
+  uint8_t ks, vs;   // scales
   bool there;
 
   static __device__ __forceinline__ int key_of(int tid) { return tid >> 2; }
-  // the page of the thread's key, -1: none
+  // The table's entry for the thread's key, to be handed to load(): nothing looks at it before, so that nothing waits for it.
   static __device__ __forceinline__ int32_t look(const KCache& c, const int32_t* row, int32_t base, int32_t end) {
-    const int32_t j = base + key_of(threadIdx.x);
-    return j < end ? row[c.page.quot(j)] : -1;
+    return row[c.page.quot(max(min(base + key_of((int)threadIdx.x), end - 1), 0))];
   }
-  __device__ __forceinline__ void load(const KCache& c, int32_t entry, int32_t base, int hk) {
+  // end: keys of the sequence, 0 where there is no such tile
+  __device__ __forceinline__ void load(const KCache& c, int32_t entry, int32_t base, int32_t end, int hk) {
     const int32_t j = base + key_of(threadIdx.x);
-    there = c.is_page(entry);
-    const int32_t page = there ? entry : 0, slot = there ? c.page.rem(j, c.page.quot(j)) : 0;
+    there = (j < end) & c.is_page(entry);
+    const int32_t in_page = c.page.rem(j, c.page.quot(j)), page = there ? entry : 0, slot = there ? in_page : 0;
     const char* kp = c.k + page * c.k_sp + slot * c.k_st + hk * c.k_sh + (threadIdx.x & 3) * (kWords * 4);
     const char* vp = c.v + page * c.v_sp + slot * c.v_st + hk * c.v_sh + (threadIdx.x & 3) * (kWords * 4);
 #pragma unroll
@@ -167,18 +148,13 @@ template <int D> struct Staged {
   }
   // As bf16 numbers; a key that is not there as zeros.  Sixteen lanes write 16 chunks of 16 bytes in four rows at a time, which fall into all banks if every
   // other row (D 64: pair of rows) writes its odd chunks first.
-  // CLEAN: what is not finite is left out (written as 0).
-  template <bool CLEAN> static __device__ __forceinline__ void write(char* tile, const uint32_t (&w)[kPieces][kWords], uint32_t scale) {
+  static __device__ __forceinline__ void write(char* tile, const uint32_t (&w)[kPieces][kWords], uint32_t scale) {
     typedef TileLayout<D> L;
     const float factor = scale_factor(scale);
     const int key = key_of(threadIdx.x), part = threadIdx.x & 3, odd = D == 128 ? key & 1 : (key >> 1) & 1;
     auto put = [&](int chunk, uint32_t a, uint32_t b) {
-      uint32_t n[4] = {e4m3_to_bf16x2<false>(a, factor), e4m3_to_bf16x2<true>(a, factor), e4m3_to_bf16x2<false>(b, factor), e4m3_to_bf16x2<true>(b, factor)};
-      if constexpr (CLEAN) {
-#pragma unroll
-        for (int y = 0; y < 4; y++) n[y] = ((n[y] & 0x7f80u) == 0x7f80u ? 0u : n[y] & 0xffffu) | ((n[y] & 0x7f800000u) == 0x7f800000u ? 0u : n[y] & 0xffff0000u);
-      }
-      *(uint4*)(tile + L::off(key, chunk)) = make_uint4(n[0], n[1], n[2], n[3]);
+      *(uint4*)(tile + L::off(key, chunk)) =
+          make_uint4(e4m3_to_bf16x2<false>(a, factor), e4m3_to_bf16x2<true>(a, factor), e4m3_to_bf16x2<false>(b, factor), e4m3_to_bf16x2<true>(b, factor));
     };
 #pragma unroll
     for (int x = 0; x < kPieces; x++) {
@@ -190,14 +166,18 @@ template <int D> struct Staged {
       }
     }
   }
-  // whether a number of V may not be finite as bf16: a NaN, or a scale that reaches 2^128
-  __device__ __forceinline__ bool may_not_be_finite() const {
+  // Leaves out what is not finite of V; whether anything was.
+  __device__ __forceinline__ bool clean() {
     uint32_t bad = 0;
 #pragma unroll
     for (int x = 0; x < kPieces; x++)
 #pragma unroll
-      for (int y = 0; y < kWords; y++) bad |= ((v[x][y] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-    return there & (bad != 0 || vs >= 247);
+      for (int y = 0; y < kWords; y++) {
+        const uint32_t signs = not_finite(v[x][y], vs);
+        v[x][y] = without(v[x][y], signs);
+        bad |= signs;
+      }
+    return bad != 0;
   }
   __device__ __forceinline__ void drop_missing() {
 #pragma unroll
@@ -238,27 +218,16 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
   __syncthreads();
 
   for (int piece = 0; left > 0; piece++) {
-    const int4 it = plan.items[item];
-    const int place = uni(it.x), count = uni(it.z);
-    int32_t seq;
-    const ChunkPlace p = chunk_place(c, a, place, &seq);
-    seq = uni(seq);
-    const RowTile rt(a, p, uni(it.y));
-    const int lo = uni(rt.lo), hi = uni(rt.hi), rows = uni(rt.rows);
+    const ChunkItem it = plan.items[item];
+    const int seq = uni(it.seq), count = uni(it.tiles), row0 = uni(it.row0), rows = uni(min(it.rows - row0, kChunkRows)), pos0 = uni(it.pos);
+    const int lo = pos0 + a.group.quot(row0), hi = pos0 + a.group.quot(row0 + rows - 1);   // positions of the item's first and last token
     const KeyTiles keys = chunk_tiles(lo, hi, a.window, a.sink, kChunkKeys);
     const int t1 = min(count, t0 + left);
     const int32_t* table = c.row(seq);
 
-    Row row;
-    const int r = min(wave * 32 + li, rows - 1), at = rt.r0 + r, token = a.group.quot(at);
-    row.real = wave * 32 + li < rows;
-    row.pos = p.pos + token;
-    row.token = p.first + token;
-    row.head = hk * (int)a.group.d + at - token * (int)a.group.d;
+    const ChunkRow row(a, hk, it.first, pos0, row0 + rows, row0 + wave * 32 + li);
     const bool works = wave * 32 < rows;
     const int w_lo = uni(row.pos), w_hi = uni(__shfl(row.pos, 31));   // rows are in the order of their positions
-    // the row's keys: [0, head_end) and [low, pos]
-    const int low = a.window > 0 ? max(0, row.pos + 1 - a.window) : 0, head_end = min(a.sink, low);
 
     bf16x8 q[kParts][L::KS];
     {
@@ -291,37 +260,41 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
       for (int x = 0; x < 16; x++) o[dt][x] = 0.f;
     float m = -INFINITY, l = 0.f;   // m in units of the scores
 
-    Staged<D> st;
+    Staged<D> st0, st1;   // two tiles on their way
     auto base_of = [&](int x) { return keys.tile_at(x) * kChunkKeys; };
-    auto entry_of = [&](int x) { return x < t1 ? Staged<D>::look(c, table, base_of(x), keys.len) : -1; };
+    auto end_of = [&](int x) { return x < t1 ? keys.len : 0; };
+    auto entry_of = [&](int x) { return Staged<D>::look(c, table, x < t1 ? base_of(x) : 0, end_of(x)); };
     // every row of the workgroup sees all keys of the tile that are there
     auto seen_by_all = [&](int base) { return base + kChunkKeys - 1 <= lo && (a.window <= 0 || hi - base < a.window || base + kChunkKeys <= a.sink); };
-    auto publish = [&](int stage, int base) {
+    auto publish = [&](Staged<D>& st, int stage, int base) {
       st.drop_missing();
       char* tile = stages + stage * 2 * L::kBytes;
-      Staged<D>::template write<false>(tile, st.k, st.ks);
       // Where some row does not see every key, 0 x V would carry an infinity or a NaN to it: they are left out here and added at the end.
-      if (!seen_by_all(base) && __any(st.may_not_be_finite())) {
-        Staged<D>::template write<true>(tile + L::kBytes, st.v, st.vs);
-        if (lane == 0) s_odd[piece & 1] = piece;
-      } else {
-        Staged<D>::template write<false>(tile + L::kBytes, st.v, st.vs);
-      }
+      if (!seen_by_all(base) && __any(st.clean()) && lane == 0) s_odd[piece & 1] = piece;
+      Staged<D>::write(tile, st.k, st.ks);
+      Staged<D>::write(tile + L::kBytes, st.v, st.vs);
       const uint64_t there = __ballot(st.there);   // four lanes a key
       uint32_t bits = 0;
 #pragma unroll
       for (int x = 0; x < 16; x++) bits |= (uint32_t)(there >> (4 * x) & 1) << x;
       if (lane == 0) s_there[stage][wave] = (uint16_t)bits;
     };
+    // While tile x is walked, tile x + 1 comes and tile x + 2 is asked for, whose entries of the table were before tile x + 1 was.  Loads come back in the
+    // order in which they were asked for, and what waits for one waits for those before it: so nothing here waits for a load of the same step, as long as every
+    // step asks for the same number (past the last tile: the first entry and the first key of the cache).
     int32_t entry = entry_of(t0), next = entry_of(t0 + 1);
-    st.load(c, entry, base_of(t0), hk);
-    publish(0, base_of(t0));
+    st0.load(c, entry, base_of(t0), end_of(t0), hk);
+    entry = entry_of(t0 + 2);
+    st1.load(c, next, t0 + 1 < t1 ? base_of(t0 + 1) : 0, end_of(t0 + 1), hk);
+    publish(st0, 0, base_of(t0));
     __syncthreads();
-    for (int x = t0; x < t1; x++) {
-      const int stage = (x - t0) & 1, base = base_of(x);
-      const bool more = x + 1 < t1;
-      if (more) st.load(c, next, base_of(x + 1), hk);
-      next = entry_of(x + 2);
+    auto ask = [&](int x, Staged<D>& free) {
+      const int32_t after = entry_of(x + 3);
+      free.load(c, entry, x + 2 < t1 ? base_of(x + 2) : 0, end_of(x + 2), hk);
+      entry = after;
+    };
+    auto walk = [&](int x, int stage) {
+      const int base = base_of(x);
       if (works) {
         const char* k_lds = stages + stage * 2 * L::kBytes;
         const char* v_lds = k_lds + L::kBytes;
@@ -344,7 +317,7 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
           }
           if (!all) {
             auto below = [](int x) { return x <= 0 ? uint64_t(0) : x >= 64 ? ~uint64_t(0) : (uint64_t(1) << x) - 1; };
-            const uint64_t sees = ((below(row.pos + 1 - base) & ~below(low - base)) | below(head_end - base)) & there;
+            const uint64_t sees = ((below(row.pos + 1 - base) & ~below(row.low - base)) | below(row.head_end - base)) & there;
             const uint32_t seen[2] = {(uint32_t)sees >> (4 * lh), (uint32_t)(sees >> 32) >> (4 * lh)};   // bit 8 (y / 4) + y % 4: the key of s[kt][y]
 #pragma unroll
             for (int kt = 0; kt < 2; kt++)
@@ -390,57 +363,44 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
           }
         }
       }
-      if (more) publish(stage ^ 1, base_of(x + 1));
+    };
+    for (int x = t0;;) {
+      ask(x, st0);
+      walk(x, 0);
+      if (++x >= t1) break;
+      publish(st1, 1, base_of(x));
+      __syncthreads();
+      ask(x, st1);
+      walk(x, 1);
+      if (++x >= t1) break;
+      publish(st0, 0, base_of(x));
       __syncthreads();
     }
+    __syncthreads();
 
     if (works) {
       l = xhalf_sum(l);
       const float m2 = m * a.scale_log2e;   // in units of log2
-      if (t0 == 0 && t1 == count) {
-        store_row<IO, D>(a, row, o, m2, l, 0, L::DT, true);
-      } else {
-        const int slot = 2 * w + (t0 == 0);
-        float* part = plan.o + ((int64_t)slot * (kChunkRows / 32) + wave) * (32 * D);
-#pragma unroll
-        for (int dt = 0; dt < L::DT; dt++)
-#pragma unroll
-          for (int y = 0; y < 4; y++)
-            *(float4*)(part + ((dt * 4 + y) * 64 + lane) * 4) = make_float4(o[dt][4 * y], o[dt][4 * y + 1], o[dt][4 * y + 2], o[dt][4 * y + 3]);
-        if (lh == 0) plan.ml[slot * kChunkRows + wave * 32 + li] = make_float2(m2, l);
-      }
-      if (s_odd[piece & 1] == piece) {   // rare: written by the lane that wrote the number before, straight into memory
-        char* out = a.out + row.token * a.o_st + row.head * a.o_sh;
-        float* part = plan.o + ((int64_t)(2 * w + (t0 == 0)) * (kChunkRows / 32) + wave) * (32 * D);
-        const bool done = t0 == 0 && t1 == count;
-        for (int x = t0; x < t1; x++) {
-          const int base = base_of(x);
-          if (seen_by_all(base)) continue;
-          for (int j = base; j < min(base + kChunkKeys, keys.len); j++) {
-            const int32_t q_page = c.page.quot(j), page = table[q_page], slot = c.page.rem(j, q_page);
-            if (!c.is_page(page)) continue;
-            const char* v = c.v + page * c.v_sp + slot * c.v_st + hk * c.v_sh;
-            const float factor = scale_factor(c.v_scale[c.scale_at(page, slot) + hk]);
-            const bool sees = row.real & (j <= row.pos) & ((j >= low) | (j < head_end));
-            for (int d0 = 0; d0 < D; d0 += 64) {
-              const uint32_t code = d0 + lane < D ? *(const uint8_t*)(v + d0 + lane) : 0u;
-              const uint32_t number = e4m3_to_bf16x2<false>(code, factor) << 16;
-              for (uint64_t left_over = __ballot((number & 0x7f800000u) == 0x7f800000u); left_over; left_over &= left_over - 1) {
-                const int at_lane = __ffsll((unsigned long long)left_over) - 1, d = d0 + at_lane;
-                const float add = __shfl(__uint_as_float(number), at_lane);
-                if (!sees || lh != (d >> 2 & 1)) continue;
-                if (!done) part[((d / 32 * 4 + d / 8 % 4) * 64 + lane) * 4 + d % 4] += add;
-                else if constexpr (sizeof(IO) == 4) *(float*)(out + 4 * d) += add;
-                else *(uint16_t*)(out + 2 * d) = f32_to_bf16(bf16_to_f32(*(const uint16_t*)(out + 2 * d)) + add);
-              }
-            }
-          }
+      const bool done = t0 == 0 && t1 == count;
+      const int64_t slot = (int64_t)(2 * w + (t0 == 0)) * kChunkRows + wave * 32 + li;
+      char* out = done ? a.out + row.token * a.o_st + row.head * a.o_sh : (char*)(plan.o + slot * D);
+      if (row.real) {
+        if (done) {
+          store_row<IO, D>(out, o, l == 0.f ? 0.f : 1.f / l);
+          if (lh == 0) a.lse[row.head * a.n_tokens + row.token] = lse_of(m2, l);
+        } else {
+          store_row<float, D>(out, o, 1.f);
+          if (lh == 0) plan.ml[slot] = make_float2(m2, l);
         }
       }
+      if (s_odd[piece & 1] == piece)
+        for (int x = t0; x < t1; x++)
+          if (!seen_by_all(base_of(x)))
+            add_not_finite<D>(c, table, hk, row, base_of(x), min(base_of(x) + kChunkKeys, keys.len), [&](int d) { return lh == (d >> 2 & 1); },
+                              [&](int d, float v) { if (done) add_to<IO>(out + sizeof(IO) * d, v); else add_to<float>(out + 4 * d, v); });
     }
     if (t0 == 0 && t1 < count && tid == 0) {
-      const int begin = hk * tiles + uni(it.w);
-      plan.joins[w] = make_int4(hk, item, w, sh.worker_of(begin + count - 1));
+      plan.joins[w] = ChunkJoin{hk, w, sh.worker_of(hk * tiles + it.before + count - 1), 0, it.first, it.rows, row0, 0};
     }
     left -= t1 - t0;
     t0 = 0;
@@ -448,51 +408,58 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
   }
 }
 
-// Joins the parts of an item that several workers shared: a wave takes 32 rows and 32 numbers of each.  Bound by latency where there are few.
+// Joins the parts of an item that several workers shared: D / 4 lanes a row, rows beyond those of a workgroup in turn.  Bound by latency where there are few.
 template <typename IO, int D>
-__global__ __launch_bounds__(kThreads) void chunk_join_kernel(KCache c, ChunkArgs a, ChunkPlan plan) {
-  if (plan.head->x == 0) return;
-  const int4 job = plan.joins[blockIdx.x];
-  if (job.y < 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 31, dt = blockIdx.y;
-  const int4 it = plan.items[job.y];
-  int32_t seq;
-  const ChunkPlace p = chunk_place(c, a, it.x, &seq);
-  const RowTile rt(a, p, it.y);
-  if (wave * 32 >= rt.rows) return;
-  Row row;
-  const int at = rt.r0 + min(wave * 32 + li, rt.rows - 1), token = a.group.quot(at);
-  row.real = wave * 32 + li < rt.rows;
-  row.token = p.first + token;
-  row.head = job.x * (int)a.group.d + at - token * (int)a.group.d;
-  float m = -INFINITY, l = 0.f;
-  f32x16 o;
+__global__ __launch_bounds__(kThreads) void chunk_join_kernel(ChunkArgs a, ChunkPlan plan) {
+  const ChunkJoin job = plan.joins[blockIdx.x];
+  if (job.last_worker < 0) return;
+  constexpr int kLanes = D / 4, kRows = kThreads / kLanes;
+  const int d = threadIdx.x % kLanes * 4, end = min(job.row0 + a.rows, job.rows);
+  for (int y = blockIdx.y * kRows + threadIdx.x / kLanes; job.row0 + y < end; y += gridDim.y * kRows) {
+    const ChunkRow row(a, job.hk, job.first, 0, end, job.row0 + y);
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0, 0, 0, 0);
+    constexpr int kAhead = 8;   // parts in flight
+    for (int x0 = job.first_worker; x0 <= job.last_worker; x0 += kAhead) {
+      float2 ml[kAhead];
+      float4 u[kAhead];
 #pragma unroll
-  for (int y = 0; y < 16; y++) o[y] = 0.f;
-  for (int x = job.z; x <= job.w; x++) {
-    const int slot = 2 * x + (x == job.z);
-    const float2 ml = plan.ml[slot * kChunkRows + wave * 32 + li];
-    const float* part = plan.o + ((int64_t)slot * (kChunkRows / 32) + wave) * (32 * D) + dt * 1024;
-    const float m2 = fmaxf(m, ml.x), zero = m2 == -INFINITY ? 0.f : m2;
-    const float f = __builtin_amdgcn_exp2f(m - zero), fx = __builtin_amdgcn_exp2f(ml.x - zero);
-    l = l * f + ml.y * fx;
+      for (int z = 0; z < kAhead; z++) {
+        const int x = x0 + z;
+        ml[z] = make_float2(-INFINITY, 0.f);
+        u[z] = make_float4(0, 0, 0, 0);
+        if (x <= job.last_worker) {
+          const int64_t slot = (int64_t)(2 * x + (x == job.first_worker)) * a.rows + y;
+          ml[z] = plan.ml[slot];
+          u[z] = *(const float4*)(plan.o + slot * D + d);
+        }
+      }
 #pragma unroll
-    for (int y = 0; y < 4; y++) {
-      const float4 u = *(const float4*)(part + (y * 64 + lane) * 4);
-      o[4 * y] = o[4 * y] * f + u.x * fx;
-      o[4 * y + 1] = o[4 * y + 1] * f + u.y * fx;
-      o[4 * y + 2] = o[4 * y + 2] * f + u.z * fx;
-      o[4 * y + 3] = o[4 * y + 3] * f + u.w * fx;
+      for (int z = 0; z < kAhead; z++) {
+        const float m2 = fmaxf(m, ml[z].x), zero = m2 == -INFINITY ? 0.f : m2;
+        const float f = __builtin_amdgcn_exp2f(m - zero), fx = __builtin_amdgcn_exp2f(ml[z].x - zero);
+        l = l * f + ml[z].y * fx;
+        o.x = o.x * f + u[z].x * fx;
+        o.y = o.y * f + u[z].y * fx;
+        o.z = o.z * f + u[z].z * fx;
+        o.w = o.w * f + u[z].w * fx;
+        m = m2;
+      }
     }
-    m = m2;
+    const float by = l == 0.f ? 0.f : 1.f / l;
+    char* out = a.out + row.token * a.o_st + row.head * a.o_sh + d * sizeof(IO);
+    if (l == 0.f) o = make_float4(0, 0, 0, 0);
+    if constexpr (sizeof(IO) == 4) *(float4*)out = make_float4(o.x * by, o.y * by, o.z * by, o.w * by);
+    else *(uint2*)out = make_uint2(pack_bf16x2(o.x * by, o.y * by), pack_bf16x2(o.z * by, o.w * by));
+    if (d == 0) a.lse[row.head * a.n_tokens + row.token] = lse_of(m, l);
   }
-  store_row<IO, D>(a, row, &o, m, l, dt, 1, dt == 0);
 }
 
 namespace {
 template <typename IO, int D> void launch_d(const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, hipStream_t s) {
-  hipLaunchKernelGGL((chunk_kernel<IO, D>), dim3(kWorkers), dim3(kThreads), 0, s, c, a, plan);
-  hipLaunchKernelGGL((chunk_join_kernel<IO, D>), dim3(kWorkers, D / 32), dim3(kThreads), 0, s, c, a, plan);
+  if (a.rows == kChunkRows) hipLaunchKernelGGL((chunk_kernel<IO, D>), dim3(kWorkers), dim3(kThreads), 0, s, c, a, plan);
+  else launch_chunk_few(D, c, a, plan, s);
+  hipLaunchKernelGGL((chunk_join_kernel<IO, D>), dim3(kWorkers, 4), dim3(kThreads), 0, s, a, plan);
 }
 template <typename IO> void launch_io(int32_t d, const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, hipStream_t s) {
   if (d == 128) launch_d<IO, 128>(c, a, plan, s);

@@ -6,16 +6,21 @@
 
 using namespace dcp;
 
-// Row tiles that n places with n_tokens rows between them can have.
-static int64_t chunk_items(int32_t n, int64_t n_tokens, int32_t group) { return (n_tokens * group + kChunkRows - 1) / kChunkRows + n; }
+// Rows of an item, by the rows that places have on average; items that n places with n_tokens tokens between them can have.
+static int32_t chunk_rows(int32_t n, int64_t n_tokens, int32_t group) {
+  const int64_t rows = n_tokens * group;
+  return rows <= 16 * (int64_t)n ? 16 : rows <= kFewRows * (int64_t)n ? 32 : kChunkRows;
+}
+static int64_t chunk_items(int32_t n, int64_t n_tokens, int32_t group, int32_t rows) { return (n_tokens * group + rows - 1) / rows + n; }
 
-static size_t chunk_bytes(int64_t items, int32_t d) {
-  return sizeof(int4) * (1 + 2 * kWorkers + (size_t)items) + 2 * (size_t)kWorkers * kChunkRows * (sizeof(float2) + d * sizeof(float));
+static size_t chunk_bytes(int64_t items, int32_t rows, int32_t d) {
+  return sizeof(int4) * (1 + kWorkers) + sizeof(ChunkJoin) * kWorkers + sizeof(ChunkItem) * (size_t)items + 2 * (size_t)kWorkers * rows * (sizeof(float2) + d * sizeof(float));
 }
 
 extern "C" size_t dcp_paged_attn_chunk_workspace_bytes(const dcp_cache_t* cache, int32_t n, int64_t n_tokens, int32_t hq) {
   if (!cache || n <= 0 || n_tokens <= 0 || n_tokens > (1 << 25) || hq <= 0 || cache->hkv <= 0 || cache->d <= 0 || hq % cache->hkv) return 0;
-  return chunk_bytes(chunk_items(n, n_tokens, hq / cache->hkv), cache->d);
+  const int32_t group = hq / cache->hkv, rows = chunk_rows(n, n_tokens, group);
+  return chunk_bytes(chunk_items(n, n_tokens, group, rows), rows, cache->d);
 }
 
 extern "C" dcp_status_t dcp_paged_attn_chunk_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t* args, const int32_t* cu_new, int64_t n_tokens,
@@ -38,10 +43,11 @@ extern "C" dcp_status_t dcp_paged_attn_chunk_fwd(const dcp_cache_t* cache, const
   if (!is_aligned(t.status, 4)) return fail(DCP_ERR_INVALID_ARG, "status is misaligned");
   if (n_tokens * t.hq > INT32_MAX) return fail(DCP_ERR_UNSUPPORTED, "n_tokens x hq must be below 2^31");
   const int32_t group = t.hq / c.hkv;
-  const int64_t items = chunk_items(t.n, n_tokens, group), tiles = (c.max_len + kChunkKeys - 1) / kChunkKeys;
+  const int32_t rows = chunk_rows(t.n, n_tokens, group), tile = rows == kChunkRows ? kChunkKeys : paged8_tile(c);
+  const int64_t items = chunk_items(t.n, n_tokens, group, rows), tiles = (c.max_len + 31) / 32;
   if (items * tiles > INT32_MAX || items * tiles * c.hkv > INT32_MAX)
-    return fail(DCP_ERR_UNSUPPORTED, "hkv x (n_tokens x hq / hkv / 128 + n) x tiles of 64 tokens in a row of the table must be below 2^31");
-  if (!workspace || workspace_bytes < chunk_bytes(items, cache->d))
+    return fail(DCP_ERR_UNSUPPORTED, "hkv x (tiles of 128 (few a place: 16 or 32) rows + n) x tiles of 32 tokens in a row of the table must be below 2^31");
+  if (!workspace || workspace_bytes < chunk_bytes(items, rows, cache->d))
     return fail(DCP_ERR_WORKSPACE, "workspace is NULL or smaller than dcp_paged_attn_chunk_workspace_bytes");
   if (!is_aligned(workspace, 256)) return fail(DCP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   const int64_t e = c.io_bytes;
@@ -52,14 +58,14 @@ extern "C" dcp_status_t dcp_paged_attn_chunk_fwd(const dcp_cache_t* cache, const
   c.k_scale += t.layer * c.layer_scales();
   c.v_scale += t.layer * c.layer_scales();
   const ChunkArgs a{(const char*)t.q, (char*)t.out, t.lse, t.seqs, t.status, cu_new, t.q_stride_t * e, t.q_stride_h * e, t.o_stride_t * e, t.o_stride_h * e,
-                    n_tokens, t.n, t.window, t.sink, (int32_t)items, fast_div((uint32_t)group), t.softmax_scale * 1.44269504088896340736f};
+                    n_tokens, t.n, t.window, t.sink, (int32_t)items, rows, tile, fast_div((uint32_t)group), t.softmax_scale * 1.44269504088896340736f};
   ChunkPlan plan;
   plan.head = (int4*)workspace;
   plan.starts = plan.head + 1;
-  plan.joins = plan.starts + kWorkers;
-  plan.items = plan.joins + kWorkers;
+  plan.joins = (ChunkJoin*)(plan.starts + kWorkers);
+  plan.items = (ChunkItem*)(plan.joins + kWorkers);
   plan.o = (float*)(plan.items + items);
-  plan.ml = (float2*)(plan.o + 2 * (size_t)kWorkers * kChunkRows * cache->d);
+  plan.ml = (float2*)(plan.o + 2 * (size_t)kWorkers * rows * cache->d);
   ProfScope ps(DCP_K_PAGED_ATTN, (hipStream_t)stream);
   launch_chunk(cache->d, c, a, plan, (hipStream_t)stream);
   DCP_HIP_TRY(hipGetLastError());

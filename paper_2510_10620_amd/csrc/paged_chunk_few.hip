@@ -1,0 +1,179 @@
+// Attention of the last tokens of every sequence over a paged key-value cache in 8 bits, where they are few: tokens to be verified.
+#include "paged_chunk.h"
+#include "paged_tile8.h"
+
+using namespace dcp;
+
+namespace dcp {
+
+// The walk of paged_attn_kernel over the items of the plan: rows in place of the query heads of one token, 16 of them a set; an item's one or two sets lie side by
+// side, and the waves of a set take its key tiles in turn.  Every wave multiplies, where the kernel with keys in LDS would leave three of four without rows: 16 sequences
+// of 512 to 8 192 tokens with five new ones each, 32/8 heads of 128, FEW_FIGURE.
+template <typename TT, bool GROUPED>
+__global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, ChunkArgs a, ChunkPlan plan) {
+  typedef typename TT::Out IO;
+  constexpr int D = TT::kD;
+  __shared__ float s_acc[kPagedWaves - 1][TT::kAcc * 4 + 2][64];
+  __shared__ int32_t s_odd[2];   // by turns: the last piece of work that met a number of V that is not finite where not every row sees it
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
+  const int w = (blockIdx.x & 7) * (kWorkers / 8) + (blockIdx.x >> 3);   // an XCD's workers have neighbouring shares
+  const int4 head = *plan.head;
+  const int n_items = head.x, tiles = head.y;
+  if (n_items == 0) return;
+  const Shares<kLogWorkers> sh(tiles * c.hkv);
+  if (w >= sh.workers) return;
+  const int4 start = plan.starts[w];
+  int hk = start.x, item = start.y, t0 = start.z, left = sh.start(w + 1) - sh.start(w);
+  if (tid < 2) s_odd[tid] = -1;
+  __syncthreads();
+  const int sets = a.rows >> 4, turns = kPagedWaves / sets, turn = wave / sets, set = wave & (sets - 1);
+  for (int piece = 0; left > 0; piece++) {
+    const ChunkItem it = plan.items[item];
+    const int end = min(it.row0 + a.rows, it.rows), count = it.tiles;
+    const int lo = it.pos + a.group.quot(it.row0), hi = it.pos + a.group.quot(end - 1);
+    const KeyTiles keys = chunk_tiles(lo, hi, a.window, a.sink, TT::kKeys);
+    const int t1 = min(count, t0 + left);
+    const int32_t* table = c.row(it.seq);
+    const ChunkRow row(a, hk, it.first, it.pos, end, it.row0 + 16 * set + i);
+    const bool works = it.row0 + 16 * set < end;
+    auto seen_by_all = [&](int base) { return (base + TT::kKeys - 1 <= lo) & ((a.window <= 0) | (hi - base < a.window) | (base + TT::kKeys <= a.sink)); };
+
+    Where<TT, GROUPED> now, next;
+    int x = t0 + turn;
+    int32_t base = keys.tile_at(x) * TT::kKeys, base_next = keys.tile_at(min(x + turns, keys.count)) * TT::kKeys;
+    now.look(c, table, base, x < t1 ? keys.len : 0, i, g);
+    next.look(c, table, base_next, x + turns < t1 ? keys.len : 0, i, g);
+    typename TT::Q q;
+    TT::load_q(q, a.q + row.token * a.q_st + row.head * a.q_sh, g, row.real);
+    const char* kb = c.k + hk * c.k_sh + TT::k_off(g);
+    const char* vb = c.v + hk * c.v_sh + TT::v_off(i);
+    f32x4 acc[TT::kAcc];
+#pragma unroll
+    for (int e = 0; e < TT::kAcc; e++) acc[e] = f32x4{0, 0, 0, 0};
+    float m = -INFINITY, l = 0;
+    bool odd = false;
+    TT t;
+    if (works && x < t1) {
+      now.settle(c);
+      now.template load_k<false>(c, t, kb, i, hk);
+      now.template load_v<false>(c, t, vb, hk);
+    }
+    for (; works && x < t1; x += turns) {
+      float s[TT::kGroup];
+      t.scores(q, s);
+      next.settle(c);
+      next.template load_k<false>(c, t, kb, i, hk);
+#pragma unroll
+      for (int j = 0; j < TT::kGroup; j++) s[j] *= a.scale_log2e;
+      if (!seen_by_all(base) || !__all(now.all_there())) {
+#pragma unroll
+        for (int j = 0; j < TT::kGroup; j++) {
+          const int key = base + g * TT::kGroup + j;
+          s[j] = row.sees(key) & now.there(j) ? s[j] : -INFINITY;
+          t.keep_v(j, (key <= hi) & now.there(j));
+          odd |= t.clean_v(j);
+        }
+      }
+      float top = s[0];
+#pragma unroll
+      for (int j = 1; j < TT::kGroup; j++) top = fmaxf(top, s[j]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m2 = fmaxf(m, top), zero = m2 == -INFINITY ? 0.f : m2, f = __builtin_amdgcn_exp2f(m - zero);
+      float sum = 0, p[TT::kGroup];
+#pragma unroll
+      for (int j = 0; j < TT::kGroup; j++) {
+        p[j] = __builtin_amdgcn_exp2f(s[j] - zero);
+        sum += p[j];
+      }
+      l = l * f + sum;
+      if (__any(m2 != m)) {
+#pragma unroll
+        for (int e = 0; e < TT::kAcc; e++) acc[e] *= f;
+      }
+      m = m2;
+      t.template weigh<16>(p, false, acc);
+      next.template load_v<false>(c, t, vb, hk);
+      now = next;
+      base = base_next;
+      base_next = keys.tile_at(min(x + 2 * turns, keys.count)) * TT::kKeys;
+      next.look(c, table, base_next, x + 2 * turns < t1 ? keys.len : 0, i, g);
+    }
+    if (__any(odd) && lane == 0) s_odd[piece & 1] = piece;
+    // the waves of a set meet, lane by lane
+    if (works && turn > 0 && t0 + turn < t1) {
+      float (*to)[64] = s_acc[wave - sets];
+#pragma unroll
+      for (int e = 0; e < TT::kAcc; e++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) to[4 * e + r][lane] = acc[e][r];
+      to[4 * TT::kAcc][lane] = m;
+      to[4 * TT::kAcc + 1][lane] = l;
+    }
+    __syncthreads();
+    if (works && turn == 0) {
+      for (int v = 1; v < turns && t0 + v < t1; v++) {
+        const float (*from)[64] = s_acc[(v - 1) * sets + wave];
+        const float mv = from[4 * TT::kAcc][lane], m2 = fmaxf(m, mv), zero = m2 == -INFINITY ? 0.f : m2;
+        const float f = __builtin_amdgcn_exp2f(m - zero), fv = __builtin_amdgcn_exp2f(mv - zero);
+        l = l * f + from[4 * TT::kAcc + 1][lane] * fv;
+#pragma unroll
+        for (int e = 0; e < TT::kAcc; e++)
+#pragma unroll
+          for (int r = 0; r < 4; r++) acc[e][r] = acc[e][r] * f + from[4 * e + r][lane] * fv;
+        m = m2;
+      }
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      const bool done = t0 == 0 && t1 == count;
+      const int64_t slot = (int64_t)(2 * w + (t0 == 0)) * a.rows + 16 * set + i;
+      char* out = done ? a.out + row.token * a.o_st + row.head * a.o_sh : (char*)(plan.o + slot * D);
+      const float by = !done ? 1.f : l == 0.f ? 0.f : 1.f / l;
+      if (row.real) {
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+          float o[TT::kRun];
+#pragma unroll
+          for (int z = 0; z < TT::kRun; z++) o[z] = by == 0.f ? 0.f : acc[z][r] * by;
+          if (done) store_run<IO, TT::kRun>(out + TT::first(r, 0, g) * sizeof(IO), o);
+          else store_run<float, TT::kRun>(out + TT::first(r, 0, g) * sizeof(float), o);
+        }
+        if (g == 0) {
+          if (done) a.lse[row.head * a.n_tokens + row.token] = lse_of(m, l);
+          else plan.ml[slot] = make_float2(m, l);
+        }
+      }
+      if (s_odd[piece & 1] == piece)
+        for (int y = t0; y < t1; y++) {
+          const int from = keys.tile_at(y) * TT::kKeys;
+          if (!seen_by_all(from))
+            add_not_finite<D>(c, table, hk, row, from, min(from + TT::kKeys, keys.len), [&](int d) { return g == (d / TT::kAcc) >> 2; },
+                              [&](int d, float v) { if (done) add_to<IO>(out + sizeof(IO) * d, v); else add_to<float>(out + 4 * d, v); });
+        }
+    }
+    __syncthreads();   // s_acc is free
+    if (t0 == 0 && t1 < count && tid == 0)
+      plan.joins[w] = ChunkJoin{hk, w, sh.worker_of(hk * tiles + it.before + count - 1), 0, it.first, it.rows, it.row0, 0};
+    left -= t1 - t0;
+    t0 = 0;
+    if (++item == n_items) { item = 0; hk++; }
+  }
+}
+
+template <typename IO, int D> static void few(const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, hipStream_t s) {
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(kWorkers), dim3(kPagedThreads), 0, s, c, a, plan); };
+  if (paged8_tile(c) == 64) go(chunk_few_kernel<Tile8<IO, D, 2>, true>);
+  else if (c.page.d % 8 == 0 && c.block.d % 8 == 0) go(chunk_few_kernel<Tile8<IO, D, 1>, true>);
+  else go(chunk_few_kernel<Tile8<IO, D, 1>, false>);
+}
+template <typename IO> static void few(int32_t d, const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, hipStream_t s) {
+  if (d == 128) few<IO, 128>(c, a, plan, s);
+  else if (d == 64) few<IO, 64>(c, a, plan, s);
+  else few<IO, 32>(c, a, plan, s);
+}
+void launch_chunk_few(int32_t d, const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, hipStream_t s) {
+  if (c.io_bytes == 4) few<float>(d, c, a, plan, s);
+  else few<bf16_t>(d, c, a, plan, s);
+}
+
+}  // namespace dcp

@@ -49,6 +49,21 @@ def test_lengths_pages_and_blocks(io, d, page, block):
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [128, 64, 32])
+@pytest.mark.parametrize("page,block", [(1, 1), (8, 8), (16, 16), (20, 10), (24, 8), (37, 37), (64, 4), (256, 64)])
+@pytest.mark.parametrize("hq", [4, 8])
+def test_few_tokens(io, d, page, block, hq):
+    """Up to 16 and up to 32 rows of a place and KV head on average; one place has many."""
+    lens = [0, 1, 2, 31, 33, 63, 64, 65, 100, 129, 200, 300, 1000, 77, 78, 5, 4, 3]
+    new = [3, 1, 2, 5, 1, 4, 8, 7, 60, 8, 0, 6, 3, 1, 1, 5, 1, 3]
+    cache, names = make_cache(lens, page, block, 2, d, io, seed=page)
+    places, cu = batch(lens, new, names)
+    q = randn((cu[-1] + 2, hq, d), io, 1)
+    out, lse = chunk(cache, q, d ** -0.5, cu, ints(places))
+    check_rows(cache, q, out, lse, d ** -0.5, rows_of(cache.seq_len.tolist(), places, cu, q.shape[0]), weights=WEIGHTS)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 3), (4, 1), (6, 2), (7, 1), (16, 1), (40, 1), (64, 2), (130, 1), (24, 8)])
 def test_heads(io, hq, hkv):
     lens, new = [5, 300, 64], [5, 17, 3]
@@ -61,8 +76,9 @@ def test_heads(io, hq, hkv):
 
 @pytest.mark.parametrize("io,d", [("bf16", 128), ("f32", 64)])
 @pytest.mark.parametrize("window,sink", [(1, 0), (1, 1), (5, 3), (16, 40), (64, 0), (100, 64), (33, 31), (5000, 7), (2 ** 31 - 1, 2 ** 31 - 1), (0, 9)])
-def test_window_and_sink(io, d, window, sink):
-    lens, new = [1, 20, 64, 130, 700], [1, 20, 9, 100, 80]
+@pytest.mark.parametrize("new", [[1, 20, 9, 100, 80], [1, 5, 9, 4, 6]])
+def test_window_and_sink(io, d, window, sink, new):
+    lens = [1, 20, 64, 130, 700]
     cache, names = make_cache(lens, 32, 16, 2, d, io)
     places, cu = batch(lens, new, names)
     q = randn((cu[-1], 4, d), io, 3)
@@ -125,6 +141,36 @@ def test_status_pages_and_rows_that_do_not_exist():
 
 
 @pytest.mark.parametrize("io,d", [("bf16", 128), ("bf16", 32), ("f32", 64)])
+@pytest.mark.parametrize("page,block", [(16, 16), (20, 5)])
+@pytest.mark.parametrize("shared", [False, True])
+def test_few_tokens_nan_and_infinity_reach_who_sees_them(io, d, page, block, shared):
+    """shared: a sequence so long that several workgroups walk it."""
+    import torch
+    n = 5000 if shared else 200
+    cache, names = make_cache([n] * 3, page, block, 1, d, io)
+    k, v = cache.k.view(torch.uint8), cache.v.view(torch.uint8)
+    where = lambda i, pos: (0, int(cache.page_table[int(names[i]), pos // page]), pos % page, 0)   # noqa: E731
+    v[(*where(0, n - 4), 7)] = 0x7f           # seen by the last four of eight tokens
+    v[(*where(0, n - 90), 8)] = 0xff          # and by all
+    k[(*where(1, n - 3), 5)] = 0x7f
+    at = where(2, n - 2)
+    cache.v_scale[0, at[1], at[2] // block] = 250
+    for pos in range(n - 2 - (n - 2) % page % block, n):
+        if where(2, pos)[1] == at[1] and where(2, pos)[2] // block == at[2] // block:
+            v[where(2, pos)] = 0
+    v[(*at, 3)], v[(*at, 4)], v[(*at, 5)] = 0x60, 0xe8, 0x08   # 2^5 and -2^6 times 2^123: infinities; 2^-6 times it
+    places, cu = batch([n] * 3, [8] * 3, names, 0)
+    q = randn((24, 4, d), io, 8)
+    out, lse = chunk(cache, q, d ** -0.5, cu, ints(places))
+    o, l = f64(out).reshape(3, 8, 4, d), f64(lse).T.reshape(3, 8, 4)
+    assert np.isnan(o[0, 4:, :, 7]).all() and np.isfinite(o[0, :4, :, 7]).all() and np.isnan(o[0, :, :, 8]).all() and np.isfinite(l[0]).all()
+    assert np.isfinite(np.delete(o[0], [7, 8], 2)).all()
+    assert np.isnan(o[1, 5:]).all() and np.isnan(l[1, 5:]).all() and np.isfinite(o[1, :5]).all() and np.isfinite(l[1, :5]).all()
+    assert np.isfinite(o[2, :6]).all() and (o[2, 6:, :, 3] == np.inf).all() and (o[2, 6:, :, 4] == -np.inf).all()
+    assert np.isfinite(o[2, 6:, :, 5]).all() and (np.abs(o[2, 6:, :, 5]) > 1e25).all()
+
+
+@pytest.mark.parametrize("io,d", [("bf16", 128), ("bf16", 32), ("f32", 64)])
 def test_nan_and_infinity_reach_who_sees_them(io, d):
     import torch
     cache, names = make_cache([200, 200, 200, 200], 16, 16, 1, d, io)
@@ -155,8 +201,9 @@ def test_nan_and_infinity_reach_who_sees_them(io, d):
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
-def test_items_that_many_workgroups_share(io):
-    lens, new = [9000, 40, 5000, 700], [3, 40, 70, 300]
+@pytest.mark.parametrize("new", [[3, 40, 70, 300], [3, 4, 7, 3]])
+def test_items_that_many_workgroups_share(io, new):
+    lens = [9000, 40, 5000, 700]
     cache, names = make_cache(lens, 64, 64, 2, 128, io)
     places, cu = batch(lens, new, names)
     q = randn((cu[-1], 8, 128), io, 9)
