@@ -41,7 +41,7 @@ extern "C" dcp_status_t dcp_paged_attn_chunk_fwd(const dcp_cache_t* cache, const
   if ((st = check_rows("out", t.out, t.o_stride_t, t.o_stride_h, cache)) != DCP_OK) return st;
   if (!t.lse || !is_aligned(t.lse, 4)) return fail(DCP_ERR_INVALID_ARG, "lse is NULL or misaligned");
   if (!is_aligned(t.status, 4)) return fail(DCP_ERR_INVALID_ARG, "status is misaligned");
-  if (n_tokens * t.hq > INT32_MAX) return fail(DCP_ERR_UNSUPPORTED, "n_tokens x hq must be below 2^31");
+  if (n_tokens * t.hq > INT32_MAX - kChunkRows) return fail(DCP_ERR_UNSUPPORTED, "n_tokens x hq must be below 2^31 - 128");   // a row behind an item's is counted too
   const int32_t group = t.hq / c.hkv;
   const int32_t rows = chunk_rows(t.n, n_tokens, group), tile = rows == kChunkRows ? kChunkKeys : paged8_tile(c);
   const int64_t items = chunk_items(t.n, n_tokens, group, rows), tiles = (c.max_len + 31) / 32;
