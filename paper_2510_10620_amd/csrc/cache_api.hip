@@ -253,7 +253,7 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
   if (rows_overlap(Rows{t.q, t.q_stride_t * e, t.q_stride_h * e}, Rows{t.out, t.o_stride_t * e, t.o_stride_h * e}, t.n, t.hq, cache->d * e))
     return fail(DCP_ERR_INVALID_ARG, "out overlaps q");
   // Whole items: the most tiles that one can have, as far as the host knows, over the waves that take them in turn
-  const int tile = cache->dtype == DCP_E4M3 ? paged8_tile(c) : cache->dtype == DCP_F32 ? 16 : 32, least = std::min(tile, 32);
+  const int tile = cache->dtype == DCP_F32 ? kPagedKeysF32 : kPagedKeys;
   const int64_t most = ((t.window > 0 ? std::min<int64_t>(c.max_len, (int64_t)t.window + t.sink + 2 * tile) : c.max_len) + tile - 1) / tile;
   Sets sets = sets_of(c.hkv, t.hq, cache->d, kPagedWaves);
   if (sets.groups * sets.abreast > (1 << 12)) return fail(DCP_ERR_UNSUPPORTED, "dcp_paged_attn_fwd covers at most 4 096 sets of 16 query heads on one KV head");
@@ -263,7 +263,7 @@ extern "C" dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_p
     whole = t.n * x.groups <= kWorkers && most <= (t.n * x.groups > kFullItems ? kWholeRoundsFull : kWholeRounds) * (kPagedWaves / x.abreast);
     if (whole) sets = x;
   }
-  if (t.n * (int64_t)((c.max_len + least - 1) / least) * sets_of(c.hkv, t.hq, cache->d, 1).groups > INT32_MAX)
+  if (t.n * (int64_t)((c.max_len + tile - 1) / tile) * sets_of(c.hkv, t.hq, cache->d, 1).groups > INT32_MAX)
     return fail(DCP_ERR_UNSUPPORTED, "n x hkv x sets of 16 query heads on one KV head x tiles of 32 (fp32: 16) tokens in a row of the table must be below 2^31");
   c.k += t.layer * c.k_sl;   // the layer's
   c.v += t.layer * c.v_sl;

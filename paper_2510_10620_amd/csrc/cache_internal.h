@@ -38,9 +38,6 @@ struct PagedArgs {
   float scale_log2e;
 };
 
-// Keys of a tile in 8 bits: 64 where 16 neighbouring keys share a page and a scale.
-inline int paged8_tile(const KCache& c) { return c.page.d % 16 == 0 && c.block.d % 16 == 0 ? 64 : 32; }
-
 // Partial results of items (place, group of sets) that several workers share, unnormalised, in units of log2.  A worker's share of the tiles
 // begins in the middle of at most one item and ends in the middle of at most one: slot 2 w holds the first, 2 w + 1 the second.
 struct PagedParts {
@@ -57,6 +54,7 @@ struct PagedParts {
 static constexpr int kLogWorkers = 9, kWorkers = 1 << kLogWorkers;
 static constexpr int kPagedWaves = 4, kPagedThreads = 64 * kPagedWaves;
 static constexpr int kSetHeads = 16;     // query heads of a matrix tile
+static constexpr int kPagedKeys = 32, kPagedKeysF32 = 16;   // keys of a tile, in fp32 caches
 
 struct ReadTokens {
   char *k, *v;

@@ -16,7 +16,7 @@ template <typename T, int D> struct Tile;
 template <int D> struct Tile<bf16_t, D> {
   typedef bf16_t Out;
   static constexpr int kD = D, kRowBytes = 2 * D;
-  static constexpr bool kScaled = false, kUngrouped = true;
+  static constexpr bool kScaled = false;
   static constexpr int kGroup = 8, kKeys = 32, kRowTiles = 2, kAcc = D / 16;
   static constexpr int kWords = D / 32;   // 4-byte words of a lane's columns of V
   struct V { uint32_t w[kWords]; };
@@ -93,7 +93,7 @@ template <int D> struct Tile<bf16_t, D> {
 template <int D> struct Tile<float, D> {
   typedef float Out;
   static constexpr int kD = D, kRowBytes = 4 * D;
-  static constexpr bool kScaled = false, kUngrouped = true;
+  static constexpr bool kScaled = false;
   static constexpr int kGroup = 4, kKeys = 16, kRowTiles = 1, kAcc = D / 16;
   static constexpr int kVec = D >= 64 ? 4 : 2, kParts = D / (16 * kVec);   // a lane has kParts pieces of kVec columns of V
   f32x4 k[D / 16];

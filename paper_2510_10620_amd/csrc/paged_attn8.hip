@@ -7,16 +7,11 @@ namespace dcp {
 
 namespace {
 
-template <typename IO, int COLS, int HALVES>
-void launch8(int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
-  if (d == 128) launch_tiles<Tile8<IO, 128, HALVES>, COLS>(grid, c, a, parts, s);
-  else if (d == 64) launch_tiles<Tile8<IO, 64, HALVES>, COLS>(grid, c, a, parts, s);
-  else launch_tiles<Tile8<IO, 32, HALVES>, COLS>(grid, c, a, parts, s);
-}
 template <typename IO, int COLS>
 void launch8(int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
-  if (paged8_tile(c) == 64) launch8<IO, COLS, 2>(d, grid, c, a, parts, s);
-  else launch8<IO, COLS, 1>(d, grid, c, a, parts, s);
+  if (d == 128) launch_tiles<Tile8<IO, 128>, COLS>(grid, c, a, parts, s);
+  else if (d == 64) launch_tiles<Tile8<IO, 64>, COLS>(grid, c, a, parts, s);
+  else launch_tiles<Tile8<IO, 32>, COLS>(grid, c, a, parts, s);
 }
 
 }  // namespace

@@ -391,8 +391,7 @@ template <typename TT, int COLS, bool ONCE>
 inline void launch_once(uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
   if (c.page.d % TT::kGroup == 0 && (!TT::kScaled || c.block.d % TT::kGroup == 0))
     hipLaunchKernelGGL((paged_attn_kernel<TT, COLS, true, ONCE>), dim3(grid), dim3(kPagedThreads), 0, s, c, a, parts);
-  else if constexpr (TT::kUngrouped)
-    hipLaunchKernelGGL((paged_attn_kernel<TT, COLS, false, ONCE>), dim3(grid), dim3(kPagedThreads), 0, s, c, a, parts);
+  else hipLaunchKernelGGL((paged_attn_kernel<TT, COLS, false, ONCE>), dim3(grid), dim3(kPagedThreads), 0, s, c, a, parts);
 }
 template <typename TT, int COLS>
 inline void launch_tiles(uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {

@@ -43,8 +43,8 @@ extern "C" dcp_status_t dcp_paged_attn_chunk_fwd(const dcp_cache_t* cache, const
   if (!is_aligned(t.status, 4)) return fail(DCP_ERR_INVALID_ARG, "status is misaligned");
   if (n_tokens * t.hq > INT32_MAX - kChunkRows) return fail(DCP_ERR_UNSUPPORTED, "n_tokens x hq must be below 2^31 - 128");   // a row behind an item's is counted too
   const int32_t group = t.hq / c.hkv;
-  const int32_t rows = chunk_rows(t.n, n_tokens, group), tile = rows == kChunkRows ? kChunkKeys : paged8_tile(c);
-  const int64_t items = chunk_items(t.n, n_tokens, group, rows), tiles = (c.max_len + 31) / 32;
+  const int32_t rows = chunk_rows(t.n, n_tokens, group), tile = rows == kChunkRows ? kChunkKeys : kPagedKeys;
+  const int64_t items = chunk_items(t.n, n_tokens, group, rows), tiles = (c.max_len + kPagedKeys - 1) / kPagedKeys;
   if (items * tiles > INT32_MAX || items * tiles * c.hkv > INT32_MAX)
     return fail(DCP_ERR_UNSUPPORTED, "hkv x (tiles of 128 (few a place: 16 or 32) rows + n) x tiles of 32 tokens in a row of the table must be below 2^31");
   if (!workspace || workspace_bytes < chunk_bytes(items, rows, cache->d))

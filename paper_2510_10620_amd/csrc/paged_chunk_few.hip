@@ -13,6 +13,7 @@ template <typename TT, bool GROUPED>
 __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, ChunkArgs a, ChunkPlan plan) {
   typedef typename TT::Out IO;
   constexpr int D = TT::kD;
+  static_assert(TT::kKeys == kPagedKeys, "the host counts tiles of so many keys");
   __shared__ float s_acc[kPagedWaves - 1][TT::kAcc * 4 + 2][64];
   __shared__ int32_t s_odd[2];   // by turns: the last piece of work that met a number of V that is not finite where not every row sees it
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
@@ -162,9 +163,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
 
 template <typename IO, int D> static void few(const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, hipStream_t s) {
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(kWorkers), dim3(kPagedThreads), 0, s, c, a, plan); };
-  if (paged8_tile(c) == 64) go(chunk_few_kernel<Tile8<IO, D, 2>, true>);
-  else if (c.page.d % 8 == 0 && c.block.d % 8 == 0) go(chunk_few_kernel<Tile8<IO, D, 1>, true>);
-  else go(chunk_few_kernel<Tile8<IO, D, 1>, false>);
+  if (c.page.d % 8 == 0 && c.block.d % 8 == 0) go(chunk_few_kernel<Tile8<IO, D>, true>);
+  else go(chunk_few_kernel<Tile8<IO, D>, false>);
 }
 template <typename IO> static void few(int32_t d, const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, hipStream_t s) {
   if (d == 128) few<IO, 128>(c, a, plan, s);

@@ -8,16 +8,16 @@ namespace dcp {
 // A finite number's parts of 8 significant bits each, whose sum it is: the upper half of it, and of what is left.
 __device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 
-// A wave's walk as in paged_attn.hip (the same lanes hold the same keys and columns), in tiles of 64 keys: a lane has 16 bytes of a key's row, 16 of its
-// numbers, and D / 16 bytes of each of 16 rows of V.  Codes become bf16 numbers with their scale in one conversion for two of them, without
+// A wave's walk as in paged_attn.hip (the same lanes hold the same keys and columns), in tiles of 32 keys: a lane has 16 bytes of a key's row, 16 of its
+// numbers, and D / 16 bytes of each of eight rows of V.  (Tiles of 64 keys, as many bytes as 32 in bf16, took longer: 32 places of 512 to 8 192 tokens, 32/8 heads of 128, 48.7
+// and 47.5 us, one of 300 tokens 7.9 and 7.6.)  Codes become bf16 numbers with their scale in one conversion for two of them, without
 // rounding, so that the products take them as they take a cache in bf16.  IO is bf16 or fp32; an fp32 query goes in as three bf16 parts, and so do
 // the weights: exact products, summed in fp32.
-// HALVES: 2, and 1 for tiles of 32 keys where groups of 16 do not share a page and a scale (every key then has its own entry of the table, or every eight).
-template <typename IO, int D, int HALVES> struct Tile8 {
+template <typename IO, int D> struct Tile8 {
   typedef IO Out;
   static constexpr int kD = D, kRowBytes = D;
-  static constexpr bool kScaled = true, kF32 = sizeof(IO) == 4, kUngrouped = HALVES == 1;
-  static constexpr int kGroup = 8 * HALVES, kKeys = 32 * HALVES, kRowTiles = 2 * HALVES, kAcc = D / 16;
+  static constexpr bool kScaled = true, kF32 = sizeof(IO) == 4;
+  static constexpr int kGroup = 8, kKeys = 32, kRowTiles = 2, kAcc = D / 16;
   static constexpr int kSteps = D / 32;                     // products of 32 numbers of a row
   static constexpr int kVWords = D >= 64 ? D / 64 : 1;      // 4-byte words of a lane's columns of V
   static constexpr int kParts = kF32 ? 3 : 1;
@@ -122,53 +122,50 @@ template <typename IO, int D, int HALVES> struct Tile8 {
   }
   // bf16: two parts of the weights, the first of them below the weight, as for a cache in bf16; fp32: three.
   template <int COLS> __device__ __forceinline__ void weigh(const float* p, bool second, f32x4* acc) const {
+    constexpr int kProducts = kF32 ? 3 : COLS == 8 ? 1 : 2;
+    uint4 b[kProducts];
+    float x[8];
 #pragma unroll
-    for (int half = 0; half < HALVES; half++) {
-      constexpr int kProducts = kF32 ? 3 : COLS == 8 ? 1 : 2;
-      uint4 b[kProducts];
-      float x[8];
+    for (int j = 0; j < 8; j++) x[j] = p[j];
+    if constexpr (kF32) {
 #pragma unroll
-      for (int j = 0; j < 8; j++) x[j] = p[8 * half + j];
-      if constexpr (kF32) {
+      for (int part = 0; part < 3; part++) {
+        uint32_t* words = (uint32_t*)&b[part];
 #pragma unroll
-        for (int part = 0; part < 3; part++) {
-          uint32_t* words = (uint32_t*)&b[part];
+        for (int j = 0; j < 8; j += 2) words[j / 2] = __builtin_amdgcn_perm(__float_as_uint(x[j + 1]), __float_as_uint(x[j]), 0x07060302u);
 #pragma unroll
-          for (int j = 0; j < 8; j += 2) words[j / 2] = __builtin_amdgcn_perm(__float_as_uint(x[j + 1]), __float_as_uint(x[j]), 0x07060302u);
+        for (int j = 0; j < 8; j++) x[j] -= upper(x[j]);
+      }
+    } else {
+      float hi[8], lo[8];
 #pragma unroll
-          for (int j = 0; j < 8; j++) x[j] -= upper(x[j]);
-        }
+      for (int j = 0; j < 8; j++) { hi[j] = upper(x[j] * 0.99609375f); lo[j] = x[j] - hi[j]; }
+      auto pack = [](const float* y) { return make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])); };
+      if constexpr (COLS == 8) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) hi[j] = second ? lo[j] : hi[j];
+        b[0] = pack(hi);
       } else {
-        float hi[8], lo[8];
+        b[0] = pack(hi);
+        b[1] = pack(lo);
+      }
+    }
 #pragma unroll
-        for (int j = 0; j < 8; j++) { hi[j] = upper(x[j] * 0.99609375f); lo[j] = x[j] - hi[j]; }
-        auto pack = [](const float* y) { return make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])); };
-        if constexpr (COLS == 8) {
+    for (int e = 0; e < kAcc; e += 2) {                   // two columns at a time
+      uint32_t w[8];
 #pragma unroll
-          for (int j = 0; j < 8; j++) hi[j] = second ? lo[j] : hi[j];
-          b[0] = pack(hi);
-        } else {
-          b[0] = pack(hi);
-          b[1] = pack(lo);
-        }
+      for (int j = 0; j < 8; j++) {
+        const float factor = scale_factor(vs[j]);
+        w[j] = e & 2 ? e4m3_to_bf16x2<true>(v[j][e / 4], factor) : e4m3_to_bf16x2<false>(v[j][e / 4], factor);
       }
 #pragma unroll
-      for (int e = 0; e < kAcc; e += 2) {                   // two columns at a time
-        uint32_t w[8];
+      for (int odd = 0; odd < 2; odd++) {
+        const uint32_t sel = odd ? 0x07060302u : 0x05040100u;
+        const uint4 a = make_uint4(__builtin_amdgcn_perm(w[1], w[0], sel), __builtin_amdgcn_perm(w[3], w[2], sel), __builtin_amdgcn_perm(w[5], w[4], sel),
+                                   __builtin_amdgcn_perm(w[7], w[6], sel));
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-          const float factor = scale_factor(vs[8 * half + j]);
-          w[j] = e & 2 ? e4m3_to_bf16x2<true>(v[8 * half + j][e / 4], factor) : e4m3_to_bf16x2<false>(v[8 * half + j][e / 4], factor);
-        }
-#pragma unroll
-        for (int odd = 0; odd < 2; odd++) {
-          const uint32_t sel = odd ? 0x07060302u : 0x05040100u;
-          const uint4 a = make_uint4(__builtin_amdgcn_perm(w[1], w[0], sel), __builtin_amdgcn_perm(w[3], w[2], sel), __builtin_amdgcn_perm(w[5], w[4], sel),
-                                     __builtin_amdgcn_perm(w[7], w[6], sel));
-#pragma unroll
-          for (int x = 0; x < kProducts; x++)
-            acc[e + odd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b[x]), acc[e + odd], 0, 0, 0);
-        }
+        for (int x = 0; x < kProducts; x++)
+          acc[e + odd] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b[x]), acc[e + odd], 0, 0, 0);
       }
     }
   }

@@ -112,7 +112,7 @@ void launch_read(int32_t each, uint32_t grid, const KCache& c, int32_t layer, co
 void launch_paged_attn_other(int32_t dtype, int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s);
 void launch_paged_attn(int32_t dtype, int32_t d, uint32_t grid, const KCache& c, const PagedArgs& a, const PagedParts& parts, hipStream_t s) {
   if (dtype != DCP_E4M3) return launch_paged_attn_other(dtype, d, grid, c, a, parts, s);
-  const int tile = paged8_tile(c), e = c.io_bytes;
+  const int tile = kPagedKeys, e = c.io_bytes;
   const size_t slots = 2 * (size_t)kWorkers * a.abreast * a.set_heads;
   if (!a.whole) {
     in_workspace(parts.joins, kWorkers * sizeof(int4));
