@@ -8,8 +8,7 @@ using namespace dcp;
 
 // Rows of an item, by the rows that places have on average; items that n places with n_tokens tokens between them can have.
 static int32_t chunk_rows(int32_t n, int64_t n_tokens, int32_t group) {
-  const int64_t rows = n_tokens * group;
-  return rows <= 16 * (int64_t)n ? 16 : rows <= kFewRows * (int64_t)n ? 32 : kChunkRows;
+  return n_tokens * group <= kFewRows * (int64_t)n ? kFewItem : kChunkRows;
 }
 static int64_t chunk_items(int32_t n, int64_t n_tokens, int32_t group, int32_t rows) { return (n_tokens * group + rows - 1) / rows + n; }
 
@@ -46,7 +45,7 @@ extern "C" dcp_status_t dcp_paged_attn_chunk_fwd(const dcp_cache_t* cache, const
   const int32_t rows = chunk_rows(t.n, n_tokens, group), tile = rows == kChunkRows ? kChunkKeys : kPagedKeys;
   const int64_t items = chunk_items(t.n, n_tokens, group, rows), tiles = (c.max_len + kPagedKeys - 1) / kPagedKeys;
   if (items * tiles > INT32_MAX || items * tiles * c.hkv > INT32_MAX)
-    return fail(DCP_ERR_UNSUPPORTED, "hkv x (tiles of 128 (few a place: 16 or 32) rows + n) x tiles of 32 tokens in a row of the table must be below 2^31");
+    return fail(DCP_ERR_UNSUPPORTED, "hkv x (tiles of 128 (few a place: 16) rows + n) x tiles of 32 tokens in a row of the table must be below 2^31");
   if (!workspace || workspace_bytes < chunk_bytes(items, rows, cache->d))
     return fail(DCP_ERR_WORKSPACE, "workspace is NULL or smaller than dcp_paged_attn_chunk_workspace_bytes");
   if (!is_aligned(workspace, 256)) return fail(DCP_ERR_WORKSPACE, "workspace must be 256-byte aligned");

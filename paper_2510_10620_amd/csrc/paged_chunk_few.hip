@@ -6,14 +6,14 @@ using namespace dcp;
 
 namespace dcp {
 
-// The walk of paged_attn_kernel over the items of the plan: rows in place of the query heads of one token, 16 of them a set; an item's one or two sets lie side by
-// side, and the waves of a set take its key tiles in turn.  Every wave multiplies, where the kernel with keys in LDS would leave three of four without rows: 16 sequences
-// of 512 to 8 192 tokens with five new ones each, 32/8 heads of 128, FEW_FIGURE.
+// The walk of paged_attn_kernel over the items of the plan: 16 rows in place of the query heads of one token, a column of the matrix tile each with keys of its own; the
+// four waves take an item's key tiles in turn.  Every wave multiplies, where the kernel with keys in LDS would leave three of four without rows.  Bound by the
+// trips to memory: 16 sequences of 512 to 8 192 tokens, up to five new ones each, 32/8 heads of 128, 39.6 us of which plan and join are 10, 92 MB of codes (49.5 with keys in LDS).
 template <typename TT, bool GROUPED>
 __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, ChunkArgs a, ChunkPlan plan) {
   typedef typename TT::Out IO;
   constexpr int D = TT::kD;
-  static_assert(TT::kKeys == kPagedKeys, "the host counts tiles of so many keys");
+  static_assert(TT::kKeys == kPagedKeys && kFewItem == 16, "the host counts tiles of so many keys and rows");
   __shared__ float s_acc[kPagedWaves - 1][TT::kAcc * 4 + 2][64];
   __shared__ int32_t s_odd[2];   // by turns: the last piece of work that met a number of V that is not finite where not every row sees it
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
@@ -27,7 +27,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
   int hk = start.x, item = start.y, t0 = start.z, left = sh.start(w + 1) - sh.start(w);
   if (tid < 2) s_odd[tid] = -1;
   __syncthreads();
-  const int sets = a.rows >> 4, turns = kPagedWaves / sets, turn = wave / sets, set = wave & (sets - 1);
+  constexpr int turns = kPagedWaves;
+  const int turn = wave;
   for (int piece = 0; left > 0; piece++) {
     const ChunkItem it = plan.items[item];
     const int end = min(it.row0 + a.rows, it.rows), count = it.tiles;
@@ -35,8 +36,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
     const KeyTiles keys = chunk_tiles(lo, hi, a.window, a.sink, TT::kKeys);
     const int t1 = min(count, t0 + left);
     const int32_t* table = c.row(it.seq);
-    const ChunkRow row(a, hk, it.first, it.pos, end, it.row0 + 16 * set + i);
-    const bool works = it.row0 + 16 * set < end;
+    const ChunkRow row(a, hk, it.first, it.pos, end, it.row0 + i);
     auto seen_by_all = [&](int base) { return (base + TT::kKeys - 1 <= lo) & ((a.window <= 0) | (hi - base < a.window) | (base + TT::kKeys <= a.sink)); };
 
     Where<TT, GROUPED> now, next;
@@ -54,12 +54,12 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
     float m = -INFINITY, l = 0;
     bool odd = false;
     TT t;
-    if (works && x < t1) {
+    if (x < t1) {
       now.settle(c);
       now.template load_k<false>(c, t, kb, i, hk);
       now.template load_v<false>(c, t, vb, hk);
     }
-    for (; works && x < t1; x += turns) {
+    for (; x < t1; x += turns) {
       float s[TT::kGroup];
       t.scores(q, s);
       next.settle(c);
@@ -101,9 +101,9 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
       next.look(c, table, base_next, x + 2 * turns < t1 ? keys.len : 0, i, g);
     }
     if (__any(odd) && lane == 0) s_odd[piece & 1] = piece;
-    // the waves of a set meet, lane by lane
-    if (works && turn > 0 && t0 + turn < t1) {
-      float (*to)[64] = s_acc[wave - sets];
+    // the waves meet, lane by lane
+    if (turn > 0 && t0 + turn < t1) {
+      float (*to)[64] = s_acc[turn - 1];
 #pragma unroll
       for (int e = 0; e < TT::kAcc; e++)
 #pragma unroll
@@ -112,9 +112,9 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
       to[4 * TT::kAcc + 1][lane] = l;
     }
     __syncthreads();
-    if (works && turn == 0) {
+    if (turn == 0) {
       for (int v = 1; v < turns && t0 + v < t1; v++) {
-        const float (*from)[64] = s_acc[(v - 1) * sets + wave];
+        const float (*from)[64] = s_acc[v - 1];
         const float mv = from[4 * TT::kAcc][lane], m2 = fmaxf(m, mv), zero = m2 == -INFINITY ? 0.f : m2;
         const float f = __builtin_amdgcn_exp2f(m - zero), fv = __builtin_amdgcn_exp2f(mv - zero);
         l = l * f + from[4 * TT::kAcc + 1][lane] * fv;
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
       l += __shfl_xor(l, 16);
       l += __shfl_xor(l, 32);
       const bool done = t0 == 0 && t1 == count;
-      const int64_t slot = (int64_t)(2 * w + (t0 == 0)) * a.rows + 16 * set + i;
+      const int64_t slot = (int64_t)(2 * w + (t0 == 0)) * a.rows + i;
       char* out = done ? a.out + row.token * a.o_st + row.head * a.o_sh : (char*)(plan.o + slot * D);
       const float by = !done ? 1.f : l == 0.f ? 0.f : 1.f / l;
       if (row.real) {

@@ -150,7 +150,7 @@ void launch_chunk(int32_t d, const KCache& c, const ChunkArgs& a, const ChunkPla
   LOOK((char*)(plan.head + 1) <= (char*)plan.starts && (char*)(plan.starts + kWorkers) <= (char*)plan.joins && (char*)(plan.joins + kWorkers) <= (char*)plan.items);
   LOOK((char*)(plan.items + a.max_items) <= (char*)plan.o && (char*)(plan.o + 2 * (size_t)kWorkers * a.rows * d) <= (char*)plan.ml);
   LOOK((reinterpret_cast<uintptr_t>(plan.joins) | reinterpret_cast<uintptr_t>(plan.items) | reinterpret_cast<uintptr_t>(plan.o)) % 16 == 0 && reinterpret_cast<uintptr_t>(plan.ml) % 8 == 0);
-  LOOK(a.rows == 16 || a.rows == 32 || a.rows == kChunkRows);
+  LOOK((a.rows == kFewItem && a.tile == kPagedKeys) || (a.rows == kChunkRows && a.tile == kChunkKeys));
   (a.rows == kChunkRows ? g_fake_tiles : g_fake_few)++;
   g_fake_cache_launches += 2;
   if (!launched(kWorkers * 4, 256)) return;

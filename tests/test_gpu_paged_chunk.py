@@ -53,7 +53,7 @@ def test_lengths_pages_and_blocks(io, d, page, block):
 @pytest.mark.parametrize("page,block", [(1, 1), (8, 8), (16, 16), (20, 10), (24, 8), (37, 37), (64, 4), (256, 64)])
 @pytest.mark.parametrize("hq", [4, 8])
 def test_few_tokens(io, d, page, block, hq):
-    """Up to 16 and up to 32 rows of a place and KV head on average; one place has many."""
+    """Up to 24 rows of a place and KV head on average (hq 4: 13), and some more (hq 8: 25); one place has many."""
     lens = [0, 1, 2, 31, 33, 63, 64, 65, 100, 129, 200, 300, 1000, 77, 78, 5, 4, 3]
     new = [3, 1, 2, 5, 1, 4, 8, 7, 60, 8, 0, 6, 3, 1, 1, 5, 1, 3]
     cache, names = make_cache(lens, page, block, 2, d, io, seed=page)
