@@ -73,7 +73,7 @@ inline bool is_aligned(const void* p, uintptr_t n) { return (reinterpret_cast<ui
 // workgroups share all items' key tiles, KV head after KV head, evenly.  Tiles have 128 rows and 64 keys in LDS, or, where places have kFewRows between
 // them on average at most, 16 rows and 32 keys in registers, as for one token.  Whole calls, us, with keys in LDS / in registers, 32/8 heads of 128, 16 sequences of 300, 2 048 and
 // 8 192 tokens: 6 rows 21.4 / 20.3, 38.9 / 32.2, 94 / 65; 12 rows 22.6 / 22.4, 41.0 / 34.6, 93 / 73; 24 rows 25.9 / 22.5, 43.9 / 39.4, 102 / 93; 30 rows 27.2 / 25.8, 45.3 / 42.5,
-// 103 / 119; 39 rows 30.1 / 27.7, 48.6 / 48.3, 107 / 150; 80 rows 42.9 / 34.7, 59.9 / 70.5, 121 / 229; two sequences, 24 rows 17.9 / 16.9, 30.2 / 23.2, 38.7 / 35.1; 16/4 heads of 64,
+// 103 / 119; 39 rows 29.2 / 27.7, 45.5 / 48.3, 103 / 150; 80 rows 37.5 / 34.7, 51.4 / 70.5, 115 / 229; two sequences, 24 rows 17.9 / 16.9, 30.2 / 23.2, 38.7 / 35.1; 16/4 heads of 64,
 // 16 sequences, 24 rows 16.5 / 18.2, 28.3 / 25.3, 47.7 / 44.4, 39 rows 17.9 / 18.8, 31.2 / 28.3, 48.9 / 72.5.  Items of 32 rows in registers were between the two.
 static constexpr int kChunkRows = 128, kChunkKeys = 64, kFewRows = 24, kFewItem = 16;
 struct ChunkArgs {
