@@ -164,8 +164,10 @@ extern "C" dcp_status_t dcp_cache_append(const dcp_cache_t* cache, int32_t layer
   // Up to four tokens a CU a workgroup each, else four in one.  In a graph, us, with one / four: tokens of 4 KiB, 64 2.95 / 3.44, 1 024 3.7 / 3.9,
   // 2 048 4.3 / 4.4, 4 096 8.4 / 7.2, 32 768 54 / 39; of 512 bytes, 64 2.94 / 2.86, 1 024 3.25 / 3.0, 8 192 7.8 / 3.8.  83 396 of 4 KiB in
   // 2 / 4 / 8 / 16: 123 / 124 / 130 / 134 with the reserve and the map's reset.
-  // In 8 bits a workgroup has the blocks of tokens that begin among its own, 16 of them where there are many.
-  const int32_t each = n_tokens <= 1024 ? 1 : c.k_scale ? 16 : 4;
+  // In 8 bits a workgroup has the blocks that begin among its tokens.  With 1 / 16 / 64, blocks of 8, 16 and 64 tokens, 8 KV heads of 128: 607 tokens 8.4 / 9.8 / 22.9, 8.2 / 9.7 / 17.9,
+  // 8.3 / 8.7 / 13.2; 6 070 tokens 47 / 21.6 / 29.1, 48 / 18.3 / 23.0, 49 / 16.4 / 17.1; 49 714 tokens 324 / 111 / 102, 336 / 82 / 72, 342 / 110 / 61.  Blocks of one
+  // token go row by row, as in the other caches.
+  const int32_t each = n_tokens <= 1024 ? 1 : !c.k_scale || c.block.d == 1 ? 4 : n_tokens <= 16384 ? 16 : 64;
   launch_append(each, (uint32_t)((n_tokens + each - 1) / each), c, layer, seqs, cu_new, n, status, x, (hipStream_t)stream);
   DCP_HIP_TRY(hipGetLastError());
   return DCP_OK;

@@ -114,7 +114,7 @@ void launch_move(uint32_t grid, const KCache& c, const Moves& m, const int32_t* 
 void launch_append(int32_t each, uint32_t grid, const KCache& c, int32_t layer, const int32_t* seqs, const int32_t* cu, int32_t n, const int32_t* status,
                    const NewTokens& x, hipStream_t s);   // each: tokens of a workgroup, 1 or 4
 void launch_append8(int32_t each, uint32_t grid, const KCache& c, int32_t layer, const int32_t* seqs, const int32_t* cu, int32_t n, const int32_t* status,
-                    const NewTokens& x, hipStream_t s);   // of launch_append, for a cache in 8 bits: each 1 or 16
+                    const NewTokens& x, hipStream_t s);   // of launch_append, for a cache in 8 bits: each 1, 16 or 64, with blocks of one token 1 or 4
 void launch_read(int32_t each, uint32_t grid, const KCache& c, int32_t layer, const int32_t* seqs, const int32_t* cu, int32_t n, const int32_t* status,
                  const ReadTokens& x, hipStream_t s);     // each: 1 or 4
 // The plan, the walk and the join.

@@ -61,8 +61,8 @@ void launch_append_other(int32_t each, uint32_t grid, const KCache& c, int32_t l
 void launch_append(int32_t each, uint32_t grid, const KCache& c, int32_t layer, const int32_t* seqs, const int32_t* cu, int32_t n, const int32_t* status,
                    const NewTokens& x, hipStream_t s) {
   if (!c.k_scale) return launch_append_other(each, grid, c, layer, seqs, cu, n, status, x, s);
-  LOOK((each == 1 || each == 16) && (int64_t)grid * each >= x.n && (int64_t)(grid - 1) * each < x.n);
-  const uint64_t columns = std::min<int64_t>((2 * (int64_t)c.hkv + 3) / 4, std::max<int64_t>(1, (1 << 23) / grid));
+  LOOK((each == 1 || each == 4 || each == 16 || each == 64) && (int64_t)grid * each >= x.n && (int64_t)(grid - 1) * each < x.n);
+  const uint64_t columns = c.block.d == 1 ? 1 : std::min<int64_t>((2 * (int64_t)c.hkv + 3) / 4, std::max<int64_t>(1, (1 << 23) / grid));
   if (!launched(grid * columns, 256)) return;
   const int d = 16 << c.log_head_chunks;
   for (int64_t t = 0; t < x.n; t++) {

@@ -181,6 +181,23 @@ def test_append_and_read(io, d, page, block, layout):
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("block", [1, 2, 32])
+@pytest.mark.parametrize("tokens", [1025, 17000])
+def test_append_of_many_tokens(io, block, tokens):
+    """The forms of many tokens, whose workgroups have some or many of them; the last block of a sequence is partly full and begins the next append's."""
+    import torch
+    page, d, hkv = 64, 32, 3
+    cache = P.Cache.empty(1, tokens // 32 + 8, page, hkv, d, 3, tokens // page + 4, torch.float8_e4m3fn, scale_block=block, io_dtype=dtype_of(io))
+    held = Held(cache)
+    x, y = randn((tokens, hkv, d), io, 1), randn((tokens, hkv, d), io, 2, 5.0)
+    grow(cache, held, [2, -1, 0], [tokens - 40, 0, 40], x, y)
+    same_cache(cache, held)
+    more = tokens // 2
+    grow(cache, held, [0, 2], [more, 5], y[: more + 5], x[: more + 5])
+    same_cache(cache, held)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
 def test_append_every_bf16_number(io):
     """Each alone in its block: the scale of every size, rounding, infinities and NaN."""
     import torch
