@@ -31,7 +31,7 @@ def randn(shape, io, seed, scale=1.0):
 
 def make_cache(lens, page, block, hkv, d, io="bf16", layers=1, spare=3, extra_seqs=1, width=None, seed=0, layout="token"):
     """A cache whose sequences lie on pages in any order; slots without a token hold NaN, blocks without one scales that are no scales.  layout as
-    in the tests of the other dtypes.  -> (Cache, sequences of `lens`)"""
+    in the tests of the other dtypes, or "mixed": K as "token", V as "head".  -> (Cache, sequences of `lens`)"""
     import torch
     rng = np.random.default_rng(seed)
     used = [-(-n // page) for n in lens]
@@ -49,13 +49,13 @@ def make_cache(lens, page, block, hkv, d, io="bf16", layers=1, spare=3, extra_se
         at += used[s]
     ref[where[:at]] = 1
     tensors = []
-    for _ in range(2):
+    for which in range(2):
         x = rng.standard_normal((layers, n_pages, page, hkv, d)) * 100
         codes = np.where(filled[None, :, :, None, None], e4m3.encode(np.clip(x, -448, 448)), 0x7f).astype(np.uint8)
         scales = np.where(filled.reshape(n_pages, blocks, block).any(2)[None, :, :, None], rng.integers(118, 122, (layers, n_pages, blocks, hkv)),
                           rng.choice([0, 255], (layers, n_pages, blocks, hkv))).astype(np.uint8)
         codes = torch.from_numpy(codes)
-        if layout == "head":
+        if layout == "head" or (layout == "mixed" and which):
             y = torch.empty((layers, n_pages, hkv, page, d), dtype=torch.uint8, device="cuda").transpose(2, 3)
         elif layout == "gaps":
             y = torch.full((layers, n_pages, page, hkv + 1, d + 16), 0x7f, dtype=torch.uint8, device="cuda")[:, :, :, :hkv, :d]

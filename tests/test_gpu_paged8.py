@@ -58,7 +58,7 @@ def test_attend_window_and_sink(io, d, window, sink):
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
-@pytest.mark.parametrize("layout", ["token", "head", "gaps"])
+@pytest.mark.parametrize("layout", ["token", "head", "gaps", "mixed"])
 def test_attend_layouts_layers_and_strided_queries(io, layout):
     cache, names = make_cache([40, 333, 3], 16, 8, 3, 64, io, layers=3, layout=layout)
     q = randn((3, 9, 72), io, 4)[:, ::1, :64]
@@ -131,25 +131,25 @@ def same_cache(cache, held):
         assert np.array_equal(got.cpu().numpy(), want)
 
 
-def grow(cache, held, seqs, new, k_new, v_new, layer=0):
-    """reserve and append, here and in the oracle"""
+def grow(cache, held, seqs, new, k_new, v_new, layers=(0,)):
+    """reserve, and append in some layers, here and in the oracle"""
     import torch
     cu = np.concatenate([[0], np.cumsum(new)])
     status = ints([9] * len(seqs))
     P.dcp_cache_reserve(cache, ints(seqs), status, n_new=ints(new))
-    P.dcp_cache_append(cache, k_new, v_new, seqs=ints(seqs), cu_new=ints(cu), status=status, layer=layer)
+    for layer in layers:
+        P.dcp_cache_append(cache, k_new, v_new, seqs=ints(seqs), cu_new=ints(cu), status=status, layer=layer)
     torch.cuda.synchronize()
     m = held.map()
-    was = [held.length[s] if 0 <= s < len(held.length) else 0 for s in seqs]
     codes = m.reserve(seqs, new)
     assert status.tolist() == codes
-    e4m3.append(m, held.ks, held.vs, held.block, seqs, cu, f64(k_new), f64(v_new), codes, layer)
-    return was
+    for layer in layers:
+        e4m3.append(m, held.ks, held.vs, held.block, seqs, cu, f64(k_new), f64(v_new), codes, layer)
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [128, 64, 32])
-@pytest.mark.parametrize("page,block,layout", [(1, 1, "token"), (16, 16, "head"), (20, 10, "gaps"), (37, 37, "token"), (64, 8, "token"), (256, 256, "token")])
+@pytest.mark.parametrize("page,block,layout", [(1, 1, "token"), (16, 16, "head"), (20, 10, "gaps"), (37, 37, "token"), (64, 8, "mixed"), (64, 1, "gaps"), (256, 256, "token")])
 def test_append_and_read(io, d, page, block, layout):
     import torch
     lens, new = [0, 1, 5, 16, 37, 63, 64, 300, 7], [1, 40, 0, 3, 300, 1, 2, 17, 5]
@@ -159,7 +159,7 @@ def test_append_and_read(io, d, page, block, layout):
     k_new, v_new = randn((sum(new), 3, d), io, 1, 3.0), randn((sum(new), 3, d + 16), io, 2)[:, :, :d]
     k_new[::7] *= 2.0 ** -9      # below the normal codes
     k_new[::5, 1] = 0
-    grow(cache, held, seqs, new, k_new, v_new, layer=1)
+    grow(cache, held, seqs, new, k_new, v_new, layers=(1,))
     same_cache(cache, held)
     # back, more tokens than were new, and more than some sequences have
     back = [min(n + 9, held.length[s] + 2) if s >= 0 else 0 for n, s in zip(new, seqs)]
@@ -312,6 +312,61 @@ def test_fork_free_and_compact_take_the_scales_along(page, block, hkv, d):
             sc[:, to] = sc[:, p]
     assert counts.tolist() == m.compact()
     same_cache(cache, held)
+
+
+@pytest.mark.parametrize("page,block,io", [(8, 4, "bf16"), (5, 1, "f32"), (12, 12, "bf16")])
+def test_a_random_life_of_a_cache(page, block, io):
+    """Steps in any order, refused ones among them: codes, scales and map against the oracle's after each."""
+    import torch
+    rng = np.random.default_rng(page)
+    layers, hkv, d, n_pages = 2, 2, 32, 40
+    cache = P.Cache.empty(layers, n_pages, page, hkv, d, 8, 9, torch.float8_e4m3fn, scale_block=block, io_dtype=dtype_of(io))
+    cache.k.view(torch.uint8).fill_(0x7f)
+    cache.v.view(torch.uint8).fill_(0x7f)
+    held = Held(cache)
+    for step in range(60):
+        kind = rng.integers(0, 6)
+        m = held.map()
+        if kind <= 2:
+            seqs = [int(x) for x in rng.permutation(9)[:4] - 1]
+            new = [int(x) for x in rng.integers(0, 2 * page, 4)]
+            k, v = (randn((sum(new), hkv, d), io, 3 * step + x, float(rng.choice([0.01, 1, 30]))) for x in (0, 1))
+            grow(cache, held, seqs, new, k, v, layers=range(layers))
+        elif kind == 3:
+            src, dst = [int(x) for x in rng.integers(-1, 8, 3)], [int(x) for x in rng.integers(0, 8, 3)]
+            status, was = ints([9] * 3), held.length.copy()
+            P.dcp_cache_fork(cache, ints(src), ints(dst), status)
+            codes = m.fork(src, dst)
+            assert status.tolist() == codes
+            for a, b, code in zip(src, dst, codes):
+                if a >= 0 and code == 0 and was[a] % page:
+                    n = -(-(int(was[a]) % page) // block)
+                    for sc in (held.ks, held.vs):
+                        sc[:, held.table[b, was[a] // page], :n] = sc[:, held.table[a, was[a] // page], :n]
+        elif kind == 4:
+            seqs = [int(x) for x in rng.integers(-1, 8, 2)]
+            P.dcp_cache_free(cache, ints(seqs))
+            m.free(seqs)
+        else:
+            counts, ws = ints([0, 0]), torch.empty(P.dcp_cache_workspace_bytes(cache), dtype=torch.uint8, device="cuda")
+            P.dcp_cache_compact(cache, counts, ws)
+            used = int((held.ref > 0).sum())
+            moves = list(zip([p for p in range(used, n_pages) if held.ref[p] > 0], [p for p in range(used) if held.ref[p] == 0]))
+            for p, to in moves:
+                for sc in (held.ks, held.vs):
+                    sc[:, to] = sc[:, p]
+            assert counts.tolist() == m.compact()
+        torch.cuda.synchronize()
+        # entries of the table behind the pages that a sequence holds may be anything
+        got = cache.page_table.cpu().numpy()
+        for s in range(8):
+            held.table[s, m.held(s):] = got[s, m.held(s):]
+        same_cache(cache, held)
+        live = [s for s in range(8) if held.length[s]]
+        if live and step % 3 == 0:
+            q = randn((len(live), 4, d), io, step)
+            out, lse = attend(cache, q, 0.2, ints(live))
+            check_rows(cache, q, out, lse, 0.2, last_tokens(cache, live), held=held)
 
 
 def test_offsets_past_32_bits():

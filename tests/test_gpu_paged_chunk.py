@@ -87,10 +87,11 @@ def test_window_and_sink(io, d, window, sink, new):
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
-@pytest.mark.parametrize("layout", ["token", "head", "gaps"])
-def test_layouts_layers_and_strides(io, layout):
+@pytest.mark.parametrize("layout", ["token", "head", "gaps", "mixed"])
+@pytest.mark.parametrize("new", [[30, 40, 3], [3, 4, 1]])
+def test_layouts_layers_and_strides(io, layout, new):
     import torch
-    lens, new = [40, 333, 3], [30, 40, 3]
+    lens = [40, 333, 3]
     cache, names = make_cache(lens, 16, 8, 3, 64, io, layers=3, layout=layout)
     places, cu = batch(lens, new, names)
     q = randn((cu[-1], 9, 72), io, 4)[:, :, :64]
@@ -216,6 +217,77 @@ def test_items_that_many_workgroups_share(io, new):
     assert not torch.isnan(out).any() and not torch.isnan(lse).any()
     out[~keep], lse[:, ~keep] = NAN, NAN
     check_rows(cache, q, out, lse, 0.088, some, weights=WEIGHTS)
+
+
+@pytest.mark.parametrize("new", [40, 5])
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_nan_in_items_that_one_workgroup_has_whole(io, new):
+    """So many items that most are walked by one workgroup, from the first key tile to the last."""
+    import torch
+    places, d, hkv = 64, 64, 8
+    cache, names = make_cache([200] * places, 16, 16, hkv, d, io)
+    v, length = cache.v.view(torch.uint8), 200
+    pages = cache.page_table[torch.from_numpy(np.asarray(names)).cuda().long()]
+    v[0, pages[:, (length - 3) // 16].long(), (length - 3) % 16, :, 7] = 0x7f
+    q = randn((places * new, 4 * hkv, d), io, 8)
+    out, lse = chunk(cache, q, d ** -0.5, [new * i for i in range(places + 1)], ints(names))
+    o = f64(out).reshape(places, new, 4 * hkv, d)
+    assert np.isnan(o[:, new - 3:, :, 7]).all() and np.isfinite(o[:, : new - 3]).all() and np.isfinite(np.delete(o, 7, 3)).all() and np.isfinite(f64(lse)).all()
+    # what is finite is what it is without the NaN
+    v[0, pages[:, (length - 3) // 16].long(), (length - 3) % 16, :, 7] = 0
+    clean, _ = chunk(cache, q, d ** -0.5, [new * i for i in range(places + 1)], ints(names))
+    c = f64(clean).reshape(places, new, 4 * hkv, d)
+    assert np.array_equal(np.delete(c, 7, 3), np.delete(o, 7, 3)) and np.array_equal(c[:, : new - 3], o[:, : new - 3])
+
+
+def test_a_sequence_in_several_places():
+    cache, names = make_cache([300, 50], 16, 16, 2, 64)
+    a, b = (int(s) for s in names)
+    places, cu = [a, b, a, a], [0, 40, 50, 51, 60]
+    q = randn((60, 4, 64), "bf16", 3)
+    out, lse = chunk(cache, q, 0.125, cu, ints(places))
+    check_rows(cache, q, out, lse, 0.125, rows_of(cache.seq_len.tolist(), places, cu, 60), weights=WEIGHTS)
+
+
+def test_binding_refuses():
+    import torch
+    cache, names = make_cache([30, 20], 16, 8, 2, 64)
+    q = randn((5, 4, 64), "bf16", 1)
+    out, lse, cu = torch.empty_like(q), torch.empty((4, 5), device="cuda"), ints([0, 3, 5])
+    ws = torch.empty(P.dcp_paged_attn_chunk_workspace_bytes(cache, 2, 5, 4), dtype=torch.uint8, device="cuda")
+    good = dict(q=q, out=out, lse=lse, softmax_scale=0.1, workspace=ws, cu_new=cu, seqs=ints(names))
+    P.dcp_paged_attn_chunk_fwd(cache, **good)
+    for bad in (dict(q=q.float()), dict(out=out[:4]), dict(lse=lse[:, :4]), dict(lse=lse.double()), dict(lse=torch.empty((5, 4), device="cuda").t()),
+                dict(cu_new=cu.long()), dict(cu_new=cu.cpu()), dict(seqs=ints([1])), dict(q=q[:, :, ::2]), dict(workspace=ws.cpu()), dict(status=ints([0]))):
+        with pytest.raises(Exception):
+            P.dcp_paged_attn_chunk_fwd(cache, **dict(good, **bad))
+    k = torch.empty((5, 2, 64), dtype=torch.bfloat16, device="cuda")
+    for a, b in ((k.float(), k.float()), (k, k[:4]), (k[:, :1], k[:, :1]), (k.cpu(), k), (k, k)):
+        with pytest.raises(Exception):
+            P.dcp_cache_read(cache, a, b, cu_new=ints([0, 5]))
+    # caches
+    e4m3fn, scales = torch.float8_e4m3fn, torch.zeros((1, 4, 2, 2), dtype=torch.uint8, device="cuda")
+    kv = torch.zeros((1, 4, 16, 2, 64), dtype=torch.uint8, device="cuda").view(e4m3fn)
+    ref, table, length = ints([0] * 4), ints([-1] * 6).view(2, 3), ints([0, 0])
+    P.Cache(kv, kv, ref, table, length, k_scale=scales, v_scale=scales)
+    for kw in (dict(), dict(k_scale=scales), dict(k_scale=scales, v_scale=scales[:, :, :1]), dict(k_scale=scales.float(), v_scale=scales.float()),
+               dict(k_scale=scales.cpu(), v_scale=scales.cpu()), dict(k_scale=scales.repeat(1, 1, 2, 1)[:, :, :3].contiguous(), v_scale=scales.repeat(1, 1, 2, 1)[:, :, :3].contiguous()),
+               dict(k_scale=scales, v_scale=scales.transpose(2, 3)), dict(k_scale=scales[:, :3].contiguous(), v_scale=scales[:, :3].contiguous())):
+        with pytest.raises(ValueError):
+            P.Cache(kv, kv, ref, table, length, **kw)
+    with pytest.raises(TypeError):
+        P.Cache(kv, kv, ref, table, length, k_scale=scales, v_scale=scales, io_dtype=torch.float16)
+    half = kv.view(torch.uint8).to(torch.bfloat16)
+    for kw in (dict(k_scale=scales), dict(io_dtype=torch.float32)):
+        with pytest.raises(ValueError):
+            P.Cache(half, half, ref, table, length, **kw)
+    with pytest.raises(ValueError):
+        P.Cache.empty(1, 4, 16, 2, 64, 2, 3, e4m3fn, scale_block=5)
+    with pytest.raises(ValueError):
+        P.Cache.empty(1, 4, 16, 2, 64, 2, 3, torch.bfloat16, scale_block=16)
+    other = P.Cache.empty(1, 4, 16, 2, 64, 2, 3, torch.bfloat16)
+    with pytest.raises(Exception, match="dcp_block_attn_fwd"):
+        P.dcp_paged_attn_chunk_fwd(other, **good)
 
 
 def test_thousands_of_places():
