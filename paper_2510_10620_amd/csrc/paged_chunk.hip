@@ -21,7 +21,9 @@ __device__ __forceinline__ ChunkPlace chunk_place(const KCache& c, const ChunkAr
 
 // One workgroup lists the items with their key tiles and where every worker begins.  Bound by latency, 5 to 8 us: two dependent trips to memory for the places, a search for the workers.
 __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(KCache c, ChunkArgs a, ChunkPlan plan) {
-  __shared__ int32_t upto[DCP_CACHE_MAX_SEQS], wave_sum[kPlanThreads / 64];
+  // In LDS what is looked up: of every place the items up to it, of the first kPlanThreads places what they have, of the first kPlanThreads items the key tiles before them.
+  __shared__ int32_t upto[DCP_CACHE_MAX_SEQS], wave_sum[kPlanThreads / 64], s_before[kPlanThreads];
+  __shared__ int4 s_place[kPlanThreads];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // inclusive sums over the workgroup, cut at cap
   auto block_sum = [&](int x, int cap, int* total) {
@@ -46,7 +48,11 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(KCache c, Chun
   for (int base = 0; base < a.n; base += kPlanThreads) {
     const int i = base + tid;
     int mine = 0, all;
-    if (i < a.n) mine = (int)(((int64_t)chunk_place(c, a, i, &seq).count * a.group.d + a.rows - 1) / a.rows);
+    if (i < a.n) {
+      const ChunkPlace p = chunk_place(c, a, i, &seq);
+      mine = (int)(((int64_t)p.count * a.group.d + a.rows - 1) / a.rows);
+      if (base == 0) s_place[tid] = make_int4(seq, p.first, p.pos, p.count);
+    }
     const int x = block_sum(min(mine, a.max_items), a.max_items, &all);   // cu_new that is not ascending may name more rows than there are: what is beyond max_items is left out
     if (i < a.n) upto[i] = add_capped(n_items, x, a.max_items);
     n_items = add_capped(n_items, all, a.max_items);
@@ -65,14 +71,20 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(KCache c, Chun
         else lo = mid + 1;
       }
       const int place = lo, tile = i - (lo ? upto[lo - 1] : 0);
-      const ChunkPlace p = chunk_place(c, a, place, &seq);
-      item = ChunkItem{seq, p.first, p.pos, p.count * (int)a.group.d, tile * a.rows, 0, 0, 0};
-      item.tiles = chunk_tiles(p.pos + a.group.quot(item.row0), p.pos + a.group.quot(min(item.row0 + a.rows, item.rows) - 1), a.window, a.sink, a.tile).count;
+      if (place < kPlanThreads) {
+        const int4 p = s_place[place];
+        item = ChunkItem{p.x, p.y, p.z, p.w * (int)a.group.d, tile * a.rows, 0, 0, 0};
+      } else {
+        const ChunkPlace p = chunk_place(c, a, place, &seq);
+        item = ChunkItem{seq, p.first, p.pos, p.count * (int)a.group.d, tile * a.rows, 0, 0, 0};
+      }
+      item.tiles = chunk_tiles(item.pos + a.group.quot(item.row0), item.pos + a.group.quot(min(item.row0 + a.rows, item.rows) - 1), a.window, a.sink, a.tile).count;
     }
     const int x = block_sum(item.tiles, INT_MAX, &all);   // the host has seen to it that the sum is below 2^31
     if (i < n_items) {
       item.before = tiles + x - item.tiles;
       plan.items[i] = item;
+      if (base == 0) s_before[tid] = item.before;
     }
     tiles += all;
   }
@@ -86,10 +98,10 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(KCache c, Chun
       int lo = 0, hi = n_items - 1;   // the last item that begins at or before it
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (plan.items[mid].before <= rel) lo = mid;
+        if ((mid < kPlanThreads ? s_before[mid] : plan.items[mid].before) <= rel) lo = mid;
         else hi = mid - 1;
       }
-      plan.starts[tid] = make_int4(head, lo, rel - plan.items[lo].before, 0);
+      plan.starts[tid] = make_int4(head, lo, rel - (lo < kPlanThreads ? s_before[lo] : plan.items[lo].before), 0);
     }
   }
 }
