@@ -446,7 +446,8 @@ typedef struct {
  *   io_dtype          of what the calls take and give beside it: k_new, v_new, q, out, k_out, v_out
  * A code is the value x 2^(127 - scale), rounded once to nearest, ties to even.  The scale is the least one, from 10 on (so that all values are normal
  * numbers of bf16 and fp32), with which the largest finite of the block's values reaches 448 units at most.  Blocks are filled in several appends, in a
- * step token by token: where later tokens need a larger scale, the codes of the block's earlier tokens are rounded again, from the values that they stand for.  NaN
+ * step token by token: the scale is never below the one that the block has with its earlier tokens; where later tokens need a larger one, the earlier tokens' codes are
+ * rounded again, from the values that they stand for.  Forked and moved pages take their scales along.  NaN
  * stays NaN, and an infinity becomes one (the format has none); neither counts for the scale.  What stands for more than the largest number of io_dtype, as values
  * within 2^-5 of it may after rounding, is an infinity there. */
 
@@ -521,7 +522,7 @@ dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t
  * dcp_paged_attn_fwd; rows whose position is negative, that no place has or that are not below n_tokens are not written.
  *   args     n places; q, out [n_tokens, hq, d], lse float [hq, n_tokens]
  *   cu_new   int32 [n + 1], device, ascending
- *   workspace  device, >= dcp_paged_attn_chunk_workspace_bytes, 256-byte aligned, as there.  Three launches.
+ *   workspace  device, >= dcp_paged_attn_chunk_workspace_bytes, 256-byte aligned, as there.  Three launches, or two.
  * DCP_ERR_UNSUPPORTED: another dtype; n_tokens above 2^25; n_tokens * hq of 2^31 - 128 or more; hkv times (ceil(n_tokens * hq / hkv / r) + n) times
  * ceil(max_pages * page_size / 32) of 2^31 or more, with r = 16 where n_tokens * hq / hkv is at most 24 * n, else 128. */
 size_t dcp_paged_attn_chunk_workspace_bytes(const dcp_cache_t* cache, int32_t n, int64_t n_tokens, int32_t hq);

@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256, sizeof(IO) == 4 ? 2 : 4) void append8_kernel(K
     const int64_t t = t0 + threadIdx.x;
     const TokenPlace p = token_place(c, seqs, begins, n, status, t, x.n);
     const int in_block = p.page < 0 ? 0 : c.block.rem(p.slot, c.block.quot(p.slot));
-    const bool begins_block = p.page >= 0 && (in_block == 0 || t == p.first);
+    const bool begins_block = p.page >= 0 && (in_block == 0 || t == max(p.first, 0));   // of what cu_new names below 0 there is nothing to write
     page_of[threadIdx.x] = begins_block ? p.page : -1;
     slot_of[threadIdx.x] = p.slot;
     rows_of[threadIdx.x] = (int)min((int64_t)min(p.behind, (int)c.block.d - in_block), x.n - t);

@@ -249,6 +249,25 @@ def test_append_leaves_out_what_has_no_place():
     same_cache(cache, held)
 
 
+def test_append_from_a_begin_below_zero_writes_the_tokens_that_are_there():
+    import torch
+    cache, names = make_cache([25, 40], 16, 16, 2, 64)
+    a, before = int(names[0]), Held(cache)
+    x, y = randn((3, 2, 64), "bf16", 1), randn((3, 2, 64), "bf16", 2)
+    P.dcp_cache_append(cache, x, y, seqs=ints([a]), cu_new=ints([-2, 3]))
+    torch.cuda.synchronize()
+    after = Held(cache)
+    j, k, v = after.values(a, np.arange(25))
+    # a code is off by half a step, 2^-4 of it, or 2^-10 units where it is below the normal codes
+    for got, want, scales in ((k, x, after.ks), (v, y, after.vs)):
+        unit = 2.0 ** (scales[0, after.table[a][1], 0].astype(np.float64) - 127)[None, :, None]
+        assert (np.abs(got[22:] - f64(want)) <= np.maximum(2.0 ** -4 * np.abs(f64(want)), 2.0 ** -10 * unit)).all()
+    _, k0, v0 = before.values(a, np.arange(22))
+    for got, want, scales in ((k, k0, after.ks), (v, v0, after.vs)):
+        unit = 2.0 ** (scales[0, after.table[a][1], 0].astype(np.float64) - 127)[None, :, None]
+        assert (np.abs(got[:22] - want) <= np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10 * unit)).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d,page", [(128, 16), (32, 20)])
 def test_read_of_the_other_caches_copies(dtype, d, page):
