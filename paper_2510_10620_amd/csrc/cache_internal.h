@@ -75,7 +75,7 @@ inline bool is_aligned(const void* p, uintptr_t n) { return (reinterpret_cast<ui
 // 8 192 tokens: 6 rows 21.4 / 20.3, 38.9 / 32.2, 94 / 65; 12 rows 22.6 / 22.4, 41.0 / 34.6, 93 / 73; 24 rows 25.9 / 22.5, 43.9 / 39.4, 102 / 93; 30 rows 27.2 / 25.8, 45.3 / 42.5,
 // 103 / 119; 39 rows 29.2 / 27.7, 45.5 / 48.3, 103 / 150; 80 rows 37.5 / 34.7, 51.4 / 70.5, 115 / 229; two sequences, 24 rows 17.9 / 16.9, 30.2 / 23.2, 38.7 / 35.1; 16/4 heads of 64,
 // 16 sequences, 24 rows 16.5 / 18.2, 28.3 / 25.3, 47.7 / 44.4, 39 rows 17.9 / 18.8, 31.2 / 28.3, 48.9 / 72.5.  Items of 32 rows in registers were between the two.
-static constexpr int kChunkRows = 128, kChunkKeys = 64, kFewRows = 24, kFewItem = 16;
+static constexpr int kChunkRows = 128, kChunkKeys = 64, kFewRows = 24, kFewItem = 16, kOwnItems = 256;
 struct ChunkArgs {
   const char* q;
   char* out;

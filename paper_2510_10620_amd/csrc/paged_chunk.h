@@ -5,6 +5,15 @@
 
 namespace dcp {
 
+__device__ __forceinline__ ChunkPlace chunk_place(const KCache& c, const ChunkArgs& a, int i, int32_t* seq) {
+  const int s = a.seqs ? a.seqs[i] : i, code = a.status ? a.status[i] : DCP_PLACE_OK;
+  *seq = code == DCP_PLACE_OK && c.is_seq(s) ? s : -1;
+  return *seq < 0 ? ChunkPlace(0, 0, 0, 0) : ChunkPlace(a.cu[i], a.cu[i + 1], a.n_tokens, c.length(s));
+}
+
+// Whether the walk's workgroups make the plan for themselves.
+inline bool plans_itself(const ChunkArgs& a) { return a.rows == kFewItem && a.max_items <= kOwnItems; }
+
 // A row of an item, as its lanes hold it.
 struct ChunkRow {
   bool real;

@@ -13,12 +13,6 @@ namespace {
 constexpr int kThreads = 256, kPlanThreads = 1024;
 constexpr float kLazyChunk = 8.f;   // the running maximum is raised when a tile exceeds it by more than 2^8
 
-__device__ __forceinline__ ChunkPlace chunk_place(const KCache& c, const ChunkArgs& a, int i, int32_t* seq) {
-  const int s = a.seqs ? a.seqs[i] : i, code = a.status ? a.status[i] : DCP_PLACE_OK;
-  *seq = code == DCP_PLACE_OK && c.is_seq(s) ? s : -1;
-  return *seq < 0 ? ChunkPlace(0, 0, 0, 0) : ChunkPlace(a.cu[i], a.cu[i + 1], a.n_tokens, c.length(s));
-}
-
 // One workgroup lists the items with their key tiles and where every worker begins.  Bound by latency, 5 to 8 us: two dependent trips to memory for the places, a search for the workers.
 __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(KCache c, ChunkArgs a, ChunkPlan plan) {
   // In LDS what is looked up: of every place the items up to it, of the first kPlanThreads places what they have, of the first kPlanThreads items the key tiles before them.
@@ -485,7 +479,7 @@ template <typename IO> void launch_io(int32_t d, const KCache& c, const ChunkArg
 }  // namespace
 
 void launch_chunk(int32_t d, const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, hipStream_t s) {
-  hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, a, plan);
+  if (!plans_itself(a)) hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, a, plan);
   if (c.io_bytes == 4) launch_io<float>(d, c, a, plan, s);
   else launch_io<bf16_t>(d, c, a, plan, s);
 }

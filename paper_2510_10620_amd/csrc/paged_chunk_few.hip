@@ -1,10 +1,111 @@
 // Attention of the last tokens of every sequence over a paged key-value cache in 8 bits, where they are few: tokens to be verified.
+#include "mfma_common.h"
 #include "paged_chunk.h"
 #include "paged_tile8.h"
 
 using namespace dcp;
 
 namespace dcp {
+
+namespace {
+
+// The plan, as a workgroup of the walk makes it for itself where there are at most kOwnItems items (and so places): a launch less than with chunk_plan_kernel, whose records take
+// as many trips to memory to read as the places themselves (whole calls, us: the case below 38.7 -> 35.4, 4 sequences of up to 900 tokens, fp32, D 64 15.8 -> 12.3; with keys in LDS,
+// where the walk became 18 us longer on 1 130, the launch stays).
+struct OwnPlan {
+  int4 place[kOwnItems];   // sequence, first token, its position, rows
+  int4 item[kOwnItems];    // place, first row, key tiles, those of the items before
+  int32_t upto[kOwnItems], wave_sum[2][4], start;
+};
+struct ChunkShare {
+  int n_items, tiles, hk, item, t0, left;
+  // What worker w has; left 0: nothing.  For all of a workgroup of 256; plan.joins[w] becomes "nothing to join".
+  __device__ __forceinline__ ChunkShare(const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, OwnPlan& own, int w) : hk(0), item(0), t0(0), left(0) {
+    const int tid = threadIdx.x;
+    if (a.max_items > kOwnItems) {
+      const int4 head = *plan.head, start = plan.starts[w];
+      n_items = uni(head.x);
+      tiles = uni(head.y);
+      const Shares<kLogWorkers> sh(tiles * c.hkv);
+      if (w >= sh.workers) return;
+      hk = uni(start.x);
+      item = uni(start.y);
+      t0 = uni(start.z);
+      left = sh.start(w + 1) - sh.start(w);
+      return;
+    }
+    if (tid == 0) plan.joins[w] = ChunkJoin{0, 0, -1, 0, 0, 0, 0, 0};
+    auto sums = [&](int x, int which, int* total) {   // inclusive, over the workgroup
+      const int lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+      }
+      if (lane == 63) own.wave_sum[which][wave] = x;
+      __syncthreads();
+      *total = 0;
+#pragma unroll
+      for (int y = 0; y < 4; y++) {
+        if (y < wave) x += own.wave_sum[which][y];
+        *total += own.wave_sum[which][y];
+      }
+      return x;
+    };
+    int mine = 0;
+    if (tid < a.n) {
+      int32_t seq;
+      const ChunkPlace p = chunk_place(c, a, tid, &seq);
+      own.place[tid] = make_int4(seq, p.first, p.pos, p.count * (int)a.group.d);
+      mine = (int)min(((int64_t)p.count * a.group.d + a.rows - 1) / a.rows, (int64_t)a.max_items);   // what is beyond max_items is left out, as by chunk_plan_kernel
+    }
+    const int upto = min(sums(mine, 0, &n_items), a.max_items);
+    if (tid < a.n) own.upto[tid] = upto;
+    n_items = uni(min(n_items, a.max_items));
+    __syncthreads();
+    int count = 0;
+    if (tid < n_items) {
+      int lo = 0, hi = a.n - 1;   // the first place whose sum is above the item
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (own.upto[mid] > tid) hi = mid;
+        else lo = mid + 1;
+      }
+      const int4 p = own.place[lo];
+      const int row0 = (tid - (lo ? own.upto[lo - 1] : 0)) * a.rows;
+      count = chunk_tiles(p.z + a.group.quot(row0), p.z + a.group.quot(min(row0 + a.rows, p.w) - 1), a.window, a.sink, a.tile).count;
+      own.item[tid] = make_int4(lo, row0, count, 0);
+    }
+    const int before = sums(count, 1, &tiles) - count;
+    tiles = uni(tiles);
+    if (tiles == 0) return;
+    const Shares<kLogWorkers> sh(tiles * c.hkv);
+    if (w >= sh.workers) return;
+    const int at = sh.start(w);
+    hk = uni((int)((uint32_t)at / (uint32_t)tiles));
+    const int rel = at - hk * tiles;
+    if (tid < n_items) {
+      own.item[tid].w = before;
+      if (before <= rel && rel < before + count) own.start = tid;   // one: items have a tile or more
+    }
+    __syncthreads();
+    item = uni(own.start);
+    t0 = rel - uni(own.item[item].w);
+    left = sh.start(w + 1) - at;
+  }
+  __device__ __forceinline__ ChunkItem at(const ChunkArgs& a, const ChunkPlan& plan, const OwnPlan& own, int x) const {
+    ChunkItem it;
+    if (a.max_items > kOwnItems) {
+      it = plan.items[x];
+    } else {
+      const int4 i = own.item[x], p = own.place[i.x];
+      it = ChunkItem{p.x, p.y, p.z, p.w, i.y, i.z, i.w, 0};
+    }
+    return ChunkItem{uni(it.seq), uni(it.first), uni(it.pos), uni(it.rows), uni(it.row0), uni(it.tiles), uni(it.before), 0};
+  }
+};
+
+}  // namespace
 
 // The walk of paged_attn_kernel over the items of the plan: 16 rows in place of the query heads of one token, a column of the matrix tile each with keys of its own; the
 // four waves take an item's key tiles in turn.  Every wave multiplies, where the kernel with keys in LDS would leave three of four without rows.  Bound by the
@@ -18,19 +119,16 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
   __shared__ int32_t s_odd[2];   // by turns: the last piece of work that met a number of V that is not finite where not every row sees it
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
   const int w = (blockIdx.x & 7) * (kWorkers / 8) + (blockIdx.x >> 3);   // an XCD's workers have neighbouring shares
-  const int4 head = *plan.head;
-  const int n_items = head.x, tiles = head.y;
-  if (n_items == 0) return;
-  const Shares<kLogWorkers> sh(tiles * c.hkv);
-  if (w >= sh.workers) return;
-  const int4 start = plan.starts[w];
-  int hk = start.x, item = start.y, t0 = start.z, left = sh.start(w + 1) - sh.start(w);
+  __shared__ OwnPlan own;
+  const ChunkShare share(c, a, plan, own, w);
+  if (share.left == 0) return;
+  int hk = share.hk, item = share.item, t0 = share.t0, left = share.left;
   if (tid < 2) s_odd[tid] = -1;
   __syncthreads();
   constexpr int turns = kPagedWaves;
   const int turn = wave;
   for (int piece = 0; left > 0; piece++) {
-    const ChunkItem it = plan.items[item];
+    const ChunkItem it = share.at(a, plan, own, item);
     const int end = min(it.row0 + a.rows, it.rows), count = it.tiles;
     const int lo = it.pos + a.group.quot(it.row0), hi = it.pos + a.group.quot(end - 1);
     const KeyTiles keys = chunk_tiles(lo, hi, a.window, a.sink, TT::kKeys);
@@ -154,10 +252,10 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
     }
     __syncthreads();   // s_acc is free
     if (t0 == 0 && t1 < count && tid == 0)
-      plan.joins[w] = ChunkJoin{hk, w, sh.worker_of(hk * tiles + it.before + count - 1), 0, it.first, it.rows, it.row0, 0};
+      plan.joins[w] = ChunkJoin{hk, w, Shares<kLogWorkers>(share.tiles * c.hkv).worker_of(hk * share.tiles + it.before + count - 1), 0, it.first, it.rows, it.row0, 0};
     left -= t1 - t0;
     t0 = 0;
-    if (++item == n_items) { item = 0; hk++; }
+    if (++item == share.n_items) { item = 0; hk++; }
   }
 }
 

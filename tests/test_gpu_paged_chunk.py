@@ -300,6 +300,23 @@ def test_thousands_of_places():
     check_rows(cache, q, out, lse, 0.2, rows_of(cache.seq_len.tolist(), places, cu, cu[-1]), weights=WEIGHTS)
 
 
+@pytest.mark.parametrize("io,window", [("bf16", 0), ("f32", 70)])
+def test_few_tokens_in_batches_padded_to_any_size(io, window):
+    """Few items are listed by the walk itself, more by a launch before it: the shares, and so the bits, are the same."""
+    lens, new = [3 + 53 * i % 700 for i in range(40)], [1 + i % 5 for i in range(40)]
+    lens = [n + m for n, m in zip(lens, new)]
+    cache, names = make_cache(lens, 16, 16, 2, 64, io, seed=3)
+    q = randn((sum(new), 8, 64), io, 1)
+    seen = []
+    for pad in (0, 150, 180, 220, 260, 1500):   # 480 rows are 30 items of 16, and one more a place: 70 to 1 570 items at most
+        places, cu = batch(lens, new, names, pad)
+        out, lse = chunk(cache, q, 0.125, cu, seqs=ints(places), window=window)
+        if not seen:
+            check_rows(cache, q, out, lse, 0.125, rows_of(cache.seq_len.tolist(), places, cu, cu[-1]), window=window)
+        seen.append((f64(out), f64(lse)))
+        assert np.array_equal(seen[0][0], seen[-1][0]) and np.array_equal(seen[0][1], seen[-1][1])
+
+
 def test_begins_that_are_not_ascending_stay_inside():
     """What the rows get is not said; nothing outside q, out and lse is touched, and the call ends."""
     import torch
@@ -309,6 +326,21 @@ def test_begins_that_are_not_ascending_stay_inside():
     lse = torch.full((3, 4, 64), 7.0, device="cuda")
     for cu in ([50, 10, 64, 2], [-2 ** 31, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1], [0, 64, 0, 64]):
         ws = torch.empty(P.dcp_paged_attn_chunk_workspace_bytes(cache, 3, 64, 4), dtype=torch.uint8, device="cuda")
+        P.dcp_paged_attn_chunk_fwd(cache, q, room[1], lse[1], 0.1, ws, ints(cu), seqs=ints(names))
+        torch.cuda.synchronize()
+    assert bool((room[0] == 7).all()) and bool((room[2] == 7).all()) and bool((lse[0] == 7).all()) and bool((lse[2] == 7).all())
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_few_tokens_with_begins_that_are_not_ascending_stay_inside(io):
+    """As above, with the items of 16 rows: places that name more rows between them than there are."""
+    import torch
+    cache, names = make_cache([300, 300, 300, 5, 0, 90], 16, 16, 2, 64, io)
+    q = randn((64, 4, 64), io, 11)
+    room = torch.full((3, 64, 4, 64), 7.0, dtype=q.dtype, device="cuda")
+    lse = torch.full((3, 4, 64), 7.0, device="cuda")
+    for cu in ([50, 10, 64, 2, 64, 0, 64], [-2 ** 31, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1, 0, 64, -5], [0, 64, 0, 64, 0, 64, 0], [64, 0, 0, 0, 0, 0, 0]):
+        ws = torch.empty(P.dcp_paged_attn_chunk_workspace_bytes(cache, 6, 64, 4), dtype=torch.uint8, device="cuda")
         P.dcp_paged_attn_chunk_fwd(cache, q, room[1], lse[1], 0.1, ws, ints(cu), seqs=ints(names))
         torch.cuda.synchronize()
     assert bool((room[0] == 7).all()) and bool((room[2] == 7).all()) and bool((lse[0] == 7).all()) and bool((lse[2] == 7).all())
