@@ -30,6 +30,15 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t four, uint32_t scale) {
 }
 __device__ __forceinline__ uint32_t without(uint32_t four, uint32_t signs) { return four & ~((signs >> 7) * 0xffu); }   // those as 0
 
+// fp32 numbers go into products as three bf16 parts of 8 significant bits each: the upper half of the number, and of what is left.  What these give is what is left of part x of
+// the number `of`; instead of nothing 2^-30 of the number, far below what fp32 sums hold, as an infinity that the parts multiply would become NaN with a part of 0.
+__device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ __forceinline__ float left_of_weight(float x, float of) { return fmaxf(x - upper(x), of * 0x1p-30f); }   // not negative
+__device__ __forceinline__ float left_of_query(float x, float of) {                                                // may be infinite: all its parts are
+  const float left = x - upper(x);
+  return fabsf(of) == INFINITY ? of : left == 0.f ? of * 0x1p-30f : left;
+}
+
 // The least scale, from 10 on, whose 448 units reach a number with these bits (no sign, finite): 448 = 1.75 x 2^8.
 __device__ __forceinline__ uint32_t least_scale(uint32_t bits) {
   const int32_t s = (int32_t)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u);

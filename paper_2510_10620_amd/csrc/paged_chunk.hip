@@ -117,6 +117,22 @@ __device__ __forceinline__ void store_row(char* out, const f32x16 (&o)[D / 32], 
     }
 }
 
+// Registers 8 c .. 8 c + 7 of a tile of weights as three bf16 operands.
+__device__ __forceinline__ void pack_weights(const f32x16& s, int c, bf16x8 (&part)[3]) {
+  float x[8];
+#pragma unroll
+  for (int y = 0; y < 8; y++) x[y] = s[8 * c + y];
+#pragma unroll
+  for (int k = 0; k < 3; k++) {
+    uint32_t w[4];
+#pragma unroll
+    for (int y = 0; y < 4; y++) w[y] = __builtin_amdgcn_perm(__float_as_uint(x[2 * y + 1]), __float_as_uint(x[2 * y]), 0x07060302u);
+    part[k] = as_frag(make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+    for (int y = 0; y < 8; y++) x[y] = left_of_weight(x[y], s[8 * c + y]);
+  }
+}
+
 // The keys and values of a tile of 64 on their way into LDS: thread t has 4 (D 32: 2) words of 16 (8) codes at a time of key t / 4.
 template <int D> struct Staged {
   static constexpr int kPieces = D >= 64 ? D / 64 : 1, kWords = D >= 64 ? 4 : 2;
@@ -246,16 +262,16 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
           q[0][ks] = as_frag(*(const uint4*)(qp + 2 * (16 * ks + 8 * lh)));
         } else {
           const float4 u = *(const float4*)(qp + 4 * (16 * ks + 8 * lh)), v = *(const float4*)(qp + 4 * (16 * ks + 8 * lh + 4));
-          float x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+          float x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w}, all[8];
 #pragma unroll
-          for (int y = 0; y < 8; y++) x[y] = x[y] == x[y] ? x[y] : NAN;   // whose upper half is NaN too
+          for (int y = 0; y < 8; y++) all[y] = x[y] = x[y] == x[y] ? x[y] : NAN;   // whose upper half is NaN too
 #pragma unroll
           for (int part = 0; part < 3; part++) {
             uint32_t words[4];
 #pragma unroll
             for (int y = 0; y < 4; y++) words[y] = __builtin_amdgcn_perm(__float_as_uint(x[2 * y + 1]), __float_as_uint(x[2 * y]), 0x07060302u);
 #pragma unroll
-            for (int y = 0; y < 8; y++) x[y] = fabsf(x[y]) < INFINITY ? x[y] - __uint_as_float(__float_as_uint(x[y]) & 0xffff0000u) : 0.f;   // what is not finite is one part
+            for (int y = 0; y < 8; y++) x[y] = left_of_query(x[y], all[y]);
             q[part][ks] = as_frag(make_uint4(words[0], words[1], words[2], words[3]));
           }
         }
@@ -360,7 +376,7 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
             for (int cc = 0; cc < 2; cc++) {
               bf16x8 pf[kParts];
               if constexpr (kParts == 1) pf[0] = pack_frag(s[kt], cc);
-              else pack_split(s[kt], cc, pf);
+              else pack_weights(s[kt], cc, pf);
 #pragma unroll
               for (int dt = 0; dt < L::DT; dt++) {
                 const bf16x8 vf = fa.cols(v_lds, 2 * kt + cc, dt);

@@ -5,9 +5,6 @@
 
 namespace dcp {
 
-// A finite number's parts of 8 significant bits each, whose sum it is: the upper half of it, and of what is left.
-__device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
-
 // A wave's walk as in paged_attn.hip (the same lanes hold the same keys and columns), in tiles of 32 keys: a lane has 16 bytes of a key's row, 16 of its
 // numbers, and D / 16 bytes of each of eight rows of V.  (Tiles of 64 keys, as many bytes as 32 in bf16, took longer: 32 places of 512 to 8 192 tokens, 32/8 heads of 128, 48.7
 // and 47.5 us, one of 300 tokens 7.9 and 7.6.)  Codes become bf16 numbers with their scale in one conversion for two of them, without
@@ -79,12 +76,12 @@ template <typename IO, int D> struct Tile8 {
       if constexpr (!kF32) {
         q.x[0][f] = __builtin_bit_cast(bf16x8, real ? *(const uint4*)(p + 2 * at) : make_uint4(0, 0, 0, 0));
       } else {
-        float x[8];
+        float x[8], all[8];
 #pragma unroll
         for (int y = 0; y < 8; y += 4) {
           const f32x4 u = real ? *(const f32x4*)(p + 4 * (at + y)) : f32x4{0, 0, 0, 0};
 #pragma unroll
-          for (int z = 0; z < 4; z++) x[y + z] = u[z] == u[z] ? u[z] : NAN;   // whose upper half is NaN too
+          for (int z = 0; z < 4; z++) all[y + z] = x[y + z] = u[z] == u[z] ? u[z] : NAN;   // whose upper half is NaN too
         }
 #pragma unroll
         for (int part = 0; part < 3; part++) {
@@ -94,7 +91,7 @@ template <typename IO, int D> struct Tile8 {
           for (int y = 0; y < 8; y += 2) {
             words[y / 2] = __builtin_amdgcn_perm(__float_as_uint(x[y + 1]), __float_as_uint(x[y]), 0x07060302u);
 #pragma unroll
-            for (int z = y; z < y + 2; z++) x[z] = fabsf(x[z]) < INFINITY ? x[z] - upper(x[z]) : 0.f;   // what is not finite is one part
+            for (int z = y; z < y + 2; z++) x[z] = left_of_query(x[z], all[z]);
           }
           q.x[part][f] = __builtin_bit_cast(bf16x8, w);
         }
@@ -134,7 +131,7 @@ template <typename IO, int D> struct Tile8 {
 #pragma unroll
         for (int j = 0; j < 8; j += 2) words[j / 2] = __builtin_amdgcn_perm(__float_as_uint(x[j + 1]), __float_as_uint(x[j]), 0x07060302u);
 #pragma unroll
-        for (int j = 0; j < 8; j++) x[j] -= upper(x[j]);
+        for (int j = 0; j < 8; j++) x[j] = left_of_weight(x[j], p[j]);
       }
     } else {
       float hi[8], lo[8];

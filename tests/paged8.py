@@ -66,6 +66,19 @@ def make_cache(lens, page, block, hkv, d, io="bf16", layers=1, spare=3, extra_se
     return P.Cache(k, v, *(torch.from_numpy(a).cuda() for a in (ref, table, length)), k_scale=ks, v_scale=vs, io_dtype=dtype_of(io)), names
 
 
+def infinite_at(cache, s, pos):
+    """Token `pos` of sequence s stands for infinities in number 3 (+) and 4 (-) of V and in number 5 (+) of K, and for zeros else; so do the others of its block."""
+    import torch
+    page, block = cache.k.shape[2], cache.k.shape[2] // cache.k_scale.shape[2]
+    p, slot = int(cache.page_table[s, pos // page]), pos % page
+    at = slice(slot // block * block, slot // block * block + block)
+    k, v = cache.k.view(torch.uint8), cache.v.view(torch.uint8)
+    k[0, p, at], v[0, p, at] = 0, 0
+    cache.k_scale[0, p, slot // block], cache.v_scale[0, p, slot // block] = 247, 247
+    k[0, p, slot, :, 5], v[0, p, slot, :, 3], v[0, p, slot, :, 4] = 0x7e, 0x7e, 0xfe
+    return p, slot
+
+
 class Held:
     """A cache's contents on the host: codes, scales and the page map."""
 

@@ -5,7 +5,7 @@ import pytest
 
 import paper_2510_10620_amd as P
 from oracle import e4m3
-from tests.paged8 import NAN, Held, check_rows, dtype_of, f64, ints, make_cache, randn
+from tests.paged8 import NAN, Held, check_rows, dtype_of, f64, infinite_at, ints, make_cache, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -106,6 +106,35 @@ def test_attend_nan_and_infinite_queries_reach_who_sees_them(io):
     assert np.isfinite(o[2]).all()
     assert np.isnan(o[3, 2]).all() and np.isfinite(np.delete(o[3], 2, 0)).all()
     assert np.isnan(o[4, 1]).all() and np.isfinite(np.delete(o[4], 1, 0)).all()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [128, 64, 32])
+@pytest.mark.parametrize("n", [40, 5000])
+def test_attend_infinite_keys_and_values(io, d, n):
+    """With queries of few bits, whose lower parts are zero, as are those of a weight of one."""
+    import torch
+    cache, names = make_cache([n, n], 16, 16, 1, d, io)
+    k, v = cache.k.view(torch.uint8), cache.v.view(torch.uint8)
+    a, b = (int(s) for s in names)
+    k[0, cache.page_table[a].long()] = 0                       # every key weighs the same
+    p, slot = infinite_at(cache, a, 20)
+    k[0, p, slot] = 0
+    p, slot = infinite_at(cache, b, 20)
+    v[0, p, slot] = 0
+    q = randn((2, 4, d), io, 1)
+    q[1, :, 5] = -1.0
+    out, lse = attend(cache, q, 0.1, ints(names))
+    o = f64(out)
+    assert (o[0, :, 3] == np.inf).all() and (o[0, :, 4] == -np.inf).all() and np.isfinite(np.delete(o[0], [3, 4], 1)).all()
+    # a score of -inf weighs what -2^127 weighs
+    cache.k_scale[0, p, slot // 16] = 245
+    o2, l2 = attend(cache, q, 0.1, ints(names))
+    assert np.isfinite(o[1]).all() and np.isfinite(f64(lse)[:, 1]).all() and torch.equal(out[1], o2[1]) and torch.equal(lse[:, 1], l2[:, 1])
+    cache.k_scale[0, p, slot // 16] = 247
+    q[1, :, 5] = 1.0
+    out, lse = attend(cache, q, 0.1, ints(names))
+    assert np.isnan(f64(out)[1]).all()
 
 
 def test_attend_many_places_and_one_long_sequence():

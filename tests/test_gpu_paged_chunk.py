@@ -6,7 +6,7 @@ import pytest
 import paper_2510_10620_amd as P
 from oracle import e4m3
 from oracle import paged as OP
-from tests.paged8 import NAN, Held, check_rows, dtype_of, f64, ints, make_cache, randn
+from tests.paged8 import NAN, Held, check_rows, dtype_of, f64, infinite_at, ints, make_cache, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -14,8 +14,22 @@ pytestmark = pytest.mark.gpu
 WEIGHTS = 2.0 ** -8
 
 
-def chunk(cache, q, scale, cu, seqs=None, window=0, sink=0, layer=0, status=None, ws=None):
+# Few rows, of a place or of the whole batch, are walked with the keys in registers, more with the keys in LDS.
+BOTH = pytest.mark.parametrize("in_lds", [False, True])
+
+
+def behind(n, hq, hkv):
+    """Rows behind those of the places, which no place has, with which a batch counts as one of many rows."""
+    return 1024 // hq + 24 * n * hkv // hq + 2
+
+
+def chunk(cache, q, scale, cu, seqs=None, window=0, sink=0, layer=0, status=None, ws=None, in_lds=False):
     import torch
+    if in_lds:
+        t, more = q.shape[0], behind(len(cu) - 1, q.shape[1], cache.k.shape[3])
+        out, lse = chunk(cache, torch.cat([q, torch.full((more, *q.shape[1:]), NAN, dtype=q.dtype, device="cuda")]), scale, cu, seqs, window, sink, layer, status)
+        assert bool(torch.isnan(out[t:]).all()) and bool(torch.isnan(lse[:, t:]).all())
+        return out[:t].contiguous(), lse[:, :t].contiguous()
     out, lse = torch.full_like(q, NAN), torch.full((q.shape[1], q.shape[0]), NAN, dtype=torch.float32, device="cuda")
     if ws is None:
         ws = torch.empty(P.dcp_paged_attn_chunk_workspace_bytes(cache, len(cu) - 1, q.shape[0], q.shape[1]), dtype=torch.uint8, device="cuda").random_()
@@ -65,30 +79,32 @@ def test_few_tokens(io, d, page, block, hq):
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 3), (4, 1), (6, 2), (7, 1), (16, 1), (40, 1), (64, 2), (130, 1), (24, 8)])
-def test_heads(io, hq, hkv):
+@BOTH
+def test_heads(io, hq, hkv, in_lds):
     lens, new = [5, 300, 64], [5, 17, 3]
     cache, names = make_cache(lens, 16, 16, hkv, 64, io, seed=hq)
     places, cu = batch(lens, new, names)
     q = randn((cu[-1], hq, 64), io, 2)
-    out, lse = chunk(cache, q, 0.125, cu, ints(places))
+    out, lse = chunk(cache, q, 0.125, cu, ints(places), in_lds=in_lds)
     check_rows(cache, q, out, lse, 0.125, rows_of(cache.seq_len.tolist(), places, cu, cu[-1]), weights=WEIGHTS)
 
 
 @pytest.mark.parametrize("io,d", [("bf16", 128), ("f32", 64)])
 @pytest.mark.parametrize("window,sink", [(1, 0), (1, 1), (5, 3), (16, 40), (64, 0), (100, 64), (33, 31), (5000, 7), (2 ** 31 - 1, 2 ** 31 - 1), (0, 9)])
 @pytest.mark.parametrize("new", [[1, 20, 9, 100, 80], [1, 5, 9, 4, 6]])
-def test_window_and_sink(io, d, window, sink, new):
+@BOTH
+def test_window_and_sink(io, d, window, sink, new, in_lds):
     lens = [1, 20, 64, 130, 700]
     cache, names = make_cache(lens, 32, 16, 2, d, io)
     places, cu = batch(lens, new, names)
     q = randn((cu[-1], 4, d), io, 3)
-    out, lse = chunk(cache, q, d ** -0.5, cu, ints(places), window=window, sink=sink)
+    out, lse = chunk(cache, q, d ** -0.5, cu, ints(places), window=window, sink=sink, in_lds=in_lds)
     check_rows(cache, q, out, lse, d ** -0.5, rows_of(cache.seq_len.tolist(), places, cu, cu[-1]), window, sink, weights=WEIGHTS)
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
 @pytest.mark.parametrize("layout", ["token", "head", "gaps", "mixed"])
-@pytest.mark.parametrize("new", [[30, 40, 3], [3, 4, 1]])
+@pytest.mark.parametrize("new", [[30, 90, 3], [30, 40, 3], [3, 4, 1]])
 def test_layouts_layers_and_strides(io, layout, new):
     import torch
     lens = [40, 333, 3]
@@ -104,12 +120,13 @@ def test_layouts_layers_and_strides(io, layout, new):
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
-def test_large_scores_and_far_away_maxima(io):
+@BOTH
+def test_large_scores_and_far_away_maxima(io, in_lds):
     import torch
     cache, names = make_cache([900], 64, 16, 1, 128, io)
     cache.k_scale[:, cache.page_table[int(names[0])][::2].long()] += 4
     q = randn((200, 2, 128), io, 5, 3.0)
-    out, lse = chunk(cache, q, 0.3, [0, 200], ints(names))
+    out, lse = chunk(cache, q, 0.3, [0, 200], ints(names), in_lds=in_lds)
     check_rows(cache, q, out, lse, 0.3, rows_of(cache.seq_len.tolist(), [int(names[0])], [0, 200], 200), weights=WEIGHTS)
 
 
@@ -172,7 +189,8 @@ def test_few_tokens_nan_and_infinity_reach_who_sees_them(io, d, page, block, sha
 
 
 @pytest.mark.parametrize("io,d", [("bf16", 128), ("bf16", 32), ("f32", 64)])
-def test_nan_and_infinity_reach_who_sees_them(io, d):
+@BOTH
+def test_nan_and_infinity_reach_who_sees_them(io, d, in_lds):
     import torch
     cache, names = make_cache([200, 200, 200, 200], 16, 16, 1, d, io)
     row = {i: cache.page_table[int(s)].tolist() for i, s in enumerate(names)}
@@ -187,7 +205,7 @@ def test_nan_and_infinity_reach_who_sees_them(io, d):
     places, cu = batch([200] * 4, [40] * 4, names, 0)
     q = randn((160, 4, d), io, 8)
     q[125, 2, 5] = NAN                      # place 3, one row
-    out, lse = chunk(cache, q, d ** -0.5, cu, ints(places))
+    out, lse = chunk(cache, q, d ** -0.5, cu, ints(places), in_lds=in_lds)
     o, l = f64(out), f64(lse)
     at = lambda i: o[40 * i: 40 * i + 40]   # noqa: E731
     assert np.isnan(at(0)[25:, :, 7]).all() and np.isfinite(at(0)[:25]).all() and np.isfinite(np.delete(at(0), 7, 2)).all() and np.isfinite(l[:, :40]).all()
@@ -199,6 +217,36 @@ def test_nan_and_infinity_reach_who_sees_them(io, d):
     assert np.isfinite(np.delete(x, [3, 4, 5], 2)).all() and np.isfinite(x[:27]).all()
     assert (x[27:, :, 3] == np.inf).all() and (x[27:, :, 4] == -np.inf).all()
     assert (x[27:30, :, 5] == np.inf).all() and np.isnan(x[30:, :, 5]).all()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [128, 64, 32])
+@pytest.mark.parametrize("n", [150, 5000])
+@BOTH
+def test_infinite_keys_and_values_that_all_see(io, d, n, in_lds):
+    """With queries of few bits, whose lower parts are zero, as are those of a weight of one."""
+    import torch
+    cache, names = make_cache([n, n], 16, 16, 1, d, io)
+    k, v = cache.k.view(torch.uint8), cache.v.view(torch.uint8)
+    a, b = (int(s) for s in names)
+    k[0, cache.page_table[a].long()] = 0                       # every key weighs the same
+    p, slot = infinite_at(cache, a, 20)
+    k[0, p, slot] = 0
+    p, slot = infinite_at(cache, b, 20)
+    v[0, p, slot] = 0
+    q = randn((10, 4, d), io, 1)
+    q[5:, :, 5] = -1.0
+    out, lse = chunk(cache, q, 0.1, [0, 5, 10], ints(names), in_lds=in_lds)
+    o = f64(out)
+    assert (o[:5, :, 3] == np.inf).all() and (o[:5, :, 4] == -np.inf).all() and np.isfinite(np.delete(o[:5], [3, 4], 2)).all()
+    # a score of -inf weighs what -2^127 weighs
+    cache.k_scale[0, p, slot // 16] = 245
+    o2, l2 = chunk(cache, q, 0.1, [0, 5, 10], ints(names), in_lds=in_lds)
+    assert np.isfinite(o[5:]).all() and np.isfinite(f64(lse)[:, 5:]).all() and torch.equal(out[5:], o2[5:]) and torch.equal(lse[:, 5:], l2[:, 5:])
+    cache.k_scale[0, p, slot // 16] = 247
+    q[5:, :, 5] = 1.0
+    out, lse = chunk(cache, q, 0.1, [0, 5, 10], ints(names), in_lds=in_lds)
+    assert np.isnan(f64(out)[5:]).all()
 
 
 @pytest.mark.parametrize("io", ["bf16", "f32"])
@@ -240,12 +288,13 @@ def test_nan_in_items_that_one_workgroup_has_whole(io, new):
     assert np.array_equal(np.delete(c, 7, 3), np.delete(o, 7, 3)) and np.array_equal(c[:, : new - 3], o[:, : new - 3])
 
 
-def test_a_sequence_in_several_places():
+@BOTH
+def test_a_sequence_in_several_places(in_lds):
     cache, names = make_cache([300, 50], 16, 16, 2, 64)
     a, b = (int(s) for s in names)
     places, cu = [a, b, a, a], [0, 40, 50, 51, 60]
     q = randn((60, 4, 64), "bf16", 3)
-    out, lse = chunk(cache, q, 0.125, cu, ints(places))
+    out, lse = chunk(cache, q, 0.125, cu, ints(places), in_lds=in_lds)
     check_rows(cache, q, out, lse, 0.125, rows_of(cache.seq_len.tolist(), places, cu, 60), weights=WEIGHTS)
 
 
@@ -321,11 +370,11 @@ def test_begins_that_are_not_ascending_stay_inside():
     """What the rows get is not said; nothing outside q, out and lse is touched, and the call ends."""
     import torch
     cache, names = make_cache([300, 300, 300], 16, 16, 2, 64)
-    q = randn((64, 4, 64), "bf16", 11)
-    room = torch.full((3, 64, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
-    lse = torch.full((3, 4, 64), 7.0, device="cuda")
-    for cu in ([50, 10, 64, 2], [-2 ** 31, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1], [0, 64, 0, 64]):
-        ws = torch.empty(P.dcp_paged_attn_chunk_workspace_bytes(cache, 3, 64, 4), dtype=torch.uint8, device="cuda")
+    q = randn((300, 4, 64), "bf16", 11)
+    room = torch.full((3, 300, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((3, 4, 300), 7.0, device="cuda")
+    for cu in ([50, 10, 300, 2], [-2 ** 31, 2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1], [0, 300, 0, 300]):
+        ws = torch.empty(P.dcp_paged_attn_chunk_workspace_bytes(cache, 3, 300, 4), dtype=torch.uint8, device="cuda")
         P.dcp_paged_attn_chunk_fwd(cache, q, room[1], lse[1], 0.1, ws, ints(cu), seqs=ints(names))
         torch.cuda.synchronize()
     assert bool((room[0] == 7).all()) and bool((room[2] == 7).all()) and bool((lse[0] == 7).all()) and bool((lse[2] == 7).all())
