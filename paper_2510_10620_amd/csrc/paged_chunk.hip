@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(KCache c, Chun
   if (tid == 0) *plan.head = make_int4(n_items, tiles, 0, 0);
   if (tid < kWorkers) {
     plan.joins[tid] = ChunkJoin{0, 0, -1, 0, 0, 0, 0, 0};
-    const Shares<kLogWorkers> sh(tiles * c.hkv);   // below 2^31: the host has seen to it
+    const ChunkShares sh(tiles * c.hkv);   // below 2^31: the host has seen to it
     if (tid < sh.workers) {
       const int at = sh.start(tid), head = (int)((uint32_t)at / (uint32_t)tiles), rel = at - head * tiles;
       int lo = 0, hi = n_items - 1;   // the last item that begins at or before it
@@ -227,12 +227,11 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
   __shared__ __attribute__((aligned(8))) uint16_t s_there[2][4];
   __shared__ int32_t s_odd[2];   // by turns: the last piece of work that met a number of V that is not finite where not every row sees it
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), li = lane & 31, lh = lane >> 5;
-  // Workgroups go to the 8 XCDs round-robin: an XCD's workers have neighbouring shares, so that its L2 serves their keys.
-  const int w = (blockIdx.x & 7) * (kWorkers / 8) + (blockIdx.x >> 3);
   const int4 head = *plan.head;
   const int n_items = uni(head.x), tiles = uni(head.y);
   if (n_items == 0) return;
-  const Shares<kLogWorkers> sh(tiles * c.hkv);
+  const ChunkShares sh(tiles * c.hkv);
+  const int w = sh.worker(blockIdx.x);
   if (w >= sh.workers) return;
   const int4 start = plan.starts[w];
   int hk = uni(start.x), item = uni(start.y), t0 = uni(start.z), left = sh.start(w + 1) - sh.start(w);

@@ -6,9 +6,9 @@
 
 using namespace dcp;
 
-// Rows of an item, by the rows that places have on average; items that n places with n_tokens tokens between them can have.
-static int32_t chunk_rows(int32_t n, int64_t n_tokens, int32_t group) {
-  return n_tokens * group <= kFewRows * (int64_t)n ? kFewItem : kChunkRows;
+// Rows of an item, by the rows that places have on average and by all rows of all KV heads; items that n places with n_tokens tokens between them can have.
+static int32_t chunk_rows(int32_t n, int64_t n_tokens, int32_t group, int32_t hkv) {
+  return n_tokens * group <= kFewRows * (int64_t)n || n_tokens * group * hkv <= kFewAll ? kFewItem : kChunkRows;
 }
 static int64_t chunk_items(int32_t n, int64_t n_tokens, int32_t group, int32_t rows) { return (n_tokens * group + rows - 1) / rows + n; }
 
@@ -18,7 +18,7 @@ static size_t chunk_bytes(int64_t items, int32_t rows, int32_t d) {
 
 extern "C" size_t dcp_paged_attn_chunk_workspace_bytes(const dcp_cache_t* cache, int32_t n, int64_t n_tokens, int32_t hq) {
   if (!cache || n <= 0 || n_tokens <= 0 || n_tokens > (1 << 25) || hq <= 0 || cache->hkv <= 0 || cache->d <= 0 || hq % cache->hkv) return 0;
-  const int32_t group = hq / cache->hkv, rows = chunk_rows(n, n_tokens, group);
+  const int32_t group = hq / cache->hkv, rows = chunk_rows(n, n_tokens, group, cache->hkv);
   return chunk_bytes(chunk_items(n, n_tokens, group, rows), rows, cache->d);
 }
 
@@ -42,7 +42,7 @@ extern "C" dcp_status_t dcp_paged_attn_chunk_fwd(const dcp_cache_t* cache, const
   if (!is_aligned(t.status, 4)) return fail(DCP_ERR_INVALID_ARG, "status is misaligned");
   if (n_tokens * t.hq > INT32_MAX - kChunkRows) return fail(DCP_ERR_UNSUPPORTED, "n_tokens x hq must be below 2^31 - 128");   // a row behind an item's is counted too
   const int32_t group = t.hq / c.hkv;
-  const int32_t rows = chunk_rows(t.n, n_tokens, group), tile = rows == kChunkRows ? kChunkKeys : kPagedKeys;
+  const int32_t rows = chunk_rows(t.n, n_tokens, group, c.hkv), tile = rows == kChunkRows ? kChunkKeys : kPagedKeys;
   const int64_t items = chunk_items(t.n, n_tokens, group, rows), tiles = (c.max_len + kPagedKeys - 1) / kPagedKeys;
   if (items * tiles > INT32_MAX || items * tiles * c.hkv > INT32_MAX)
     return fail(DCP_ERR_UNSUPPORTED, "hkv x (tiles of 128 (few a place: 16) rows + n) x tiles of 32 tokens in a row of the table must be below 2^31");

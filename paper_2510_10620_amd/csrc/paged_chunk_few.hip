@@ -18,23 +18,24 @@ struct OwnPlan {
   int32_t upto[kOwnItems], wave_sum[2][4], start;
 };
 struct ChunkShare {
-  int n_items, tiles, hk, item, t0, left;
-  // What worker w has; left 0: nothing.  For all of a workgroup of 256; plan.joins[w] becomes "nothing to join".
-  __device__ __forceinline__ ChunkShare(const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, OwnPlan& own, int w) : hk(0), item(0), t0(0), left(0) {
+  int n_items, tiles, w, hk, item, t0, left;
+  // What worker w, as which the workgroup goes, has; left 0: nothing.  For all of a workgroup of 256; plan.joins[w] becomes "nothing to join".
+  __device__ __forceinline__ ChunkShare(const KCache& c, const ChunkArgs& a, const ChunkPlan& plan, OwnPlan& own) : hk(0), item(0), t0(0), left(0) {
     const int tid = threadIdx.x;
     if (a.max_items > kOwnItems) {
-      const int4 head = *plan.head, start = plan.starts[w];
+      const int4 head = *plan.head;
       n_items = uni(head.x);
       tiles = uni(head.y);
-      const Shares<kLogWorkers> sh(tiles * c.hkv);
+      const ChunkShares sh(tiles * c.hkv);
+      w = sh.worker(blockIdx.x);
       if (w >= sh.workers) return;
+      const int4 start = plan.starts[w];
       hk = uni(start.x);
       item = uni(start.y);
       t0 = uni(start.z);
       left = sh.start(w + 1) - sh.start(w);
       return;
     }
-    if (tid == 0) plan.joins[w] = ChunkJoin{0, 0, -1, 0, 0, 0, 0, 0};
     auto sums = [&](int x, int which, int* total) {   // inclusive, over the workgroup
       const int lane = tid & 63, wave = tid >> 6;
 #pragma unroll
@@ -78,8 +79,9 @@ struct ChunkShare {
     }
     const int before = sums(count, 1, &tiles) - count;
     tiles = uni(tiles);
-    if (tiles == 0) return;
-    const Shares<kLogWorkers> sh(tiles * c.hkv);
+    const ChunkShares sh(tiles * c.hkv);
+    w = sh.worker(blockIdx.x);
+    if (tid == 0) plan.joins[w] = ChunkJoin{0, 0, -1, 0, 0, 0, 0, 0};
     if (w >= sh.workers) return;
     const int at = sh.start(w);
     hk = uni((int)((uint32_t)at / (uint32_t)tiles));
@@ -109,7 +111,7 @@ struct ChunkShare {
 
 // The walk of paged_attn_kernel over the items of the plan: 16 rows in place of the query heads of one token, a column of the matrix tile each with keys of its own; the
 // four waves take an item's key tiles in turn.  Every wave multiplies, where the kernel with keys in LDS would leave three of four without rows.  Bound by the
-// trips to memory: 16 sequences of 512 to 8 192 tokens, up to five new ones each, 32/8 heads of 128, 39.6 us of which plan and join are 10, 92 MB of codes (49.5 with keys in LDS).
+// trips to memory: 16 sequences of 512 to 8 192 tokens, up to five new ones each, 32/8 heads of 128, 35.4 us of which the join is 5, 92 MB of codes (49.5 with keys in LDS; 46.4, when it was 38.3, with loads past the caches: items of a place read the same keys).
 template <typename TT, bool GROUPED>
 __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, ChunkArgs a, ChunkPlan plan) {
   typedef typename TT::Out IO;
@@ -118,9 +120,9 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
   __shared__ float s_acc[kPagedWaves - 1][TT::kAcc * 4 + 2][64];
   __shared__ int32_t s_odd[2];   // by turns: the last piece of work that met a number of V that is not finite where not every row sees it
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
-  const int w = (blockIdx.x & 7) * (kWorkers / 8) + (blockIdx.x >> 3);   // an XCD's workers have neighbouring shares
   __shared__ OwnPlan own;
-  const ChunkShare share(c, a, plan, own, w);
+  const ChunkShare share(c, a, plan, own);
+  const int w = share.w;
   if (share.left == 0) return;
   int hk = share.hk, item = share.item, t0 = share.t0, left = share.left;
   if (tid < 2) s_odd[tid] = -1;
@@ -252,7 +254,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
     }
     __syncthreads();   // s_acc is free
     if (t0 == 0 && t1 < count && tid == 0)
-      plan.joins[w] = ChunkJoin{hk, w, Shares<kLogWorkers>(share.tiles * c.hkv).worker_of(hk * share.tiles + it.before + count - 1), 0, it.first, it.rows, it.row0, 0};
+      plan.joins[w] = ChunkJoin{hk, w, ChunkShares(share.tiles * c.hkv).worker_of(hk * share.tiles + it.before + count - 1), 0, it.first, it.rows, it.row0, 0};
     left -= t1 - t0;
     t0 = 0;
     if (++item == share.n_items) { item = 0; hk++; }

@@ -155,7 +155,7 @@ static void limits() {
               const size_t bytes = dcp_paged_attn_chunk_workspace_bytes(&c, n, tokens, a.hq);
               g_fake_ws = at(uint64_t(1) << 40); g_fake_ws_end = g_fake_ws + bytes;
               const __int128 rows = (__int128)tokens * group;
-              const int r = rows <= 24 * (__int128)n ? 16 : 128;
+              const int r = rows <= 24 * (__int128)n || rows * hkv <= 1024 ? 16 : 128;
               const __int128 tiles = ((int64_t)c.max_pages * c.page_size + 31) / 32;
               const bool ok = (__int128)tokens * a.hq < ((int64_t)1 << 31) - 128 && ((rows + r - 1) / r + n) * tiles * hkv <= INT_MAX;
               EXPECT(bytes > 0 && dcp_paged_attn_chunk_fwd(&c, &a, ints, tokens, g_fake_ws, bytes, nullptr) == (ok ? DCP_OK : DCP_ERR_UNSUPPORTED));
