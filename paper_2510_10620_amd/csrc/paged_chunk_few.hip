@@ -166,13 +166,15 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
       next.template load_k<false>(c, t, kb, i, hk);
 #pragma unroll
       for (int j = 0; j < TT::kGroup; j++) s[j] *= a.scale_log2e;
-      if (!seen_by_all(base) || !__all(now.all_there())) {
+      const bool edge = !seen_by_all(base);
+      if (edge || !__all(now.all_there())) {
 #pragma unroll
         for (int j = 0; j < TT::kGroup; j++) {
           const int key = base + g * TT::kGroup + j;
           s[j] = row.sees(key) & now.there(j) ? s[j] : -INFINITY;
           t.keep_v(j, (key <= hi) & now.there(j));
-          odd |= t.clean_v(j);
+          // What is left out here is added at the end, in edge tiles: with the keys of a page that does not exist alone, the others' numbers stay in the products.
+          if (edge) odd |= t.clean_v(j);
         }
       }
       float top = s[0];
