@@ -173,9 +173,12 @@ __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, C
           const int key = base + g * TT::kGroup + j;
           s[j] = row.sees(key) & now.there(j) ? s[j] : -INFINITY;
           t.keep_v(j, (key <= hi) & now.there(j));
-          // What is left out here is added at the end, in edge tiles: with the keys of a page that does not exist alone, the others' numbers stay in the products.
-          if (edge) odd |= t.clean_v(j);
         }
+      }
+      // What is left out here is added at the end, in edge tiles: where a page does not exist, the other pages' numbers stay in the products.
+      if (edge) {
+#pragma unroll
+        for (int j = 0; j < TT::kGroup; j++) odd |= t.clean_v(j);
       }
       float top = s[0];
 #pragma unroll
