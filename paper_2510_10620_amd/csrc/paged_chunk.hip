@@ -352,7 +352,8 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
           for (int y = 1; y < 16; y++) mx = fmaxf(fmaxf(mx, s[0][y]), s[1][y]);
           mx = xhalf_max(mx);
           const bool raise = (mx - m) * a.scale_log2e > kLazyChunk;
-          const float m_new = raise ? mx : m, m_use = m_new == -INFINITY ? 0.f : m_new, mc = m_use * a.scale_log2e;
+          const float m_new = raise ? mx : m, m_use = m_new == -INFINITY ? 0.f : m_new;
+          float mc = m_use * a.scale_log2e;
           if (__any(raise)) {
             const float alpha = raise ? __builtin_amdgcn_exp2f((m - m_use) * a.scale_log2e) : 1.f;
             l *= alpha;
@@ -362,6 +363,14 @@ __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kerne
               for (int y = 0; y < 16; y++) o[dt][y] *= alpha;
           }
           m = m_new;
+          // mc is rounded, a score times the scale below is not: so large that half a step of mc is more than 2^0.5 in a weight, the maximum goes off first.
+          if (__any(fabsf(mc) >= 0x1p24f)) {
+#pragma unroll
+            for (int kt = 0; kt < 2; kt++)
+#pragma unroll
+              for (int y = 0; y < 16; y++) s[kt][y] -= m_use;
+            mc = 0.f;
+          }
 #pragma unroll
           for (int kt = 0; kt < 2; kt++) {
             float sum = 0.f;
