@@ -522,7 +522,8 @@ dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t
  * dcp_paged_attn_fwd; rows whose position is negative, that no place has or that are not below n_tokens are not written.
  *   args     n places; q, out [n_tokens, hq, d], lse float [hq, n_tokens]
  *   cu_new   int32 [n + 1], device, ascending
- *   workspace  device, >= dcp_paged_attn_chunk_workspace_bytes, 256-byte aligned, as there.  Three launches, or two.
+ *   workspace  device, >= dcp_paged_attn_chunk_workspace_bytes, 256-byte aligned, as there.  The size grows with n and with n_tokens: one that was taken for
+ *              the largest batch does for smaller ones.  Three launches, or two.
  * DCP_ERR_UNSUPPORTED: another dtype; n_tokens above 2^25; n_tokens * hq of 2^31 - 128 or more; hkv times (ceil(n_tokens * hq / hkv / r) + n) times
  * ceil(max_pages * page_size / 32) of 2^31 or more, with r = 16 where n_tokens * hq / hkv is at most 24 * n or n_tokens * hq at most 1 024, else 128. */
 size_t dcp_paged_attn_chunk_workspace_bytes(const dcp_cache_t* cache, int32_t n, int64_t n_tokens, int32_t hq);

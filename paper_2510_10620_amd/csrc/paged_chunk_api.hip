@@ -1,4 +1,5 @@
 // The host's half of dcp_paged_attn_chunk_fwd, as cache_api.hip is that of the other calls on a paged cache.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 
@@ -16,10 +17,15 @@ static size_t chunk_bytes(int64_t items, int32_t rows, int32_t d) {
   return sizeof(int4) * (1 + kWorkers) + sizeof(ChunkJoin) * kWorkers + sizeof(ChunkItem) * (size_t)items + 2 * (size_t)kWorkers * rows * (sizeof(float2) + d * sizeof(float));
 }
 
+// What every call with up to n places and n_tokens tokens needs, so that a workspace for the largest batch does for smaller ones: where many places go by kFewItem, as many
+// tokens of fewer places go by kChunkRows, whose parts take 8 times as much.
 extern "C" size_t dcp_paged_attn_chunk_workspace_bytes(const dcp_cache_t* cache, int32_t n, int64_t n_tokens, int32_t hq) {
   if (!cache || n <= 0 || n_tokens <= 0 || n_tokens > (1 << 25) || hq <= 0 || cache->hkv <= 0 || cache->d <= 0 || hq % cache->hkv) return 0;
-  const int32_t group = hq / cache->hkv, rows = chunk_rows(n, n_tokens, group, cache->hkv);
-  return chunk_bytes(chunk_items(n, n_tokens, group, rows), rows, cache->d);
+  const int32_t group = hq / cache->hkv;
+  const int64_t few = std::min<int64_t>(n_tokens, std::max(kFewRows * (int64_t)n / group, (int64_t)kFewAll / hq));   // tokens that go by kFewItem at most
+  size_t bytes = few ? chunk_bytes(chunk_items(n, few, group, kFewItem), kFewItem, cache->d) : 0;
+  if (chunk_rows(1, n_tokens, group, cache->hkv) == kChunkRows) bytes = std::max(bytes, chunk_bytes(chunk_items(n, n_tokens, group, kChunkRows), kChunkRows, cache->d));
+  return bytes;
 }
 
 extern "C" dcp_status_t dcp_paged_attn_chunk_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t* args, const int32_t* cu_new, int64_t n_tokens,
@@ -46,7 +52,7 @@ extern "C" dcp_status_t dcp_paged_attn_chunk_fwd(const dcp_cache_t* cache, const
   const int64_t items = chunk_items(t.n, n_tokens, group, rows), tiles = (c.max_len + kPagedKeys - 1) / kPagedKeys;
   if (items * tiles > INT32_MAX || items * tiles * c.hkv > INT32_MAX)
     return fail(DCP_ERR_UNSUPPORTED, "hkv x (tiles of 128 (few a place: 16) rows + n) x tiles of 32 tokens in a row of the table must be below 2^31");
-  if (!workspace || workspace_bytes < chunk_bytes(items, rows, cache->d))
+  if (!workspace || workspace_bytes < dcp_paged_attn_chunk_workspace_bytes(cache, t.n, n_tokens, t.hq))
     return fail(DCP_ERR_WORKSPACE, "workspace is NULL or smaller than dcp_paged_attn_chunk_workspace_bytes");
   if (!is_aligned(workspace, 256)) return fail(DCP_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   const int64_t e = c.io_bytes;
