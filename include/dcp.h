@@ -520,12 +520,17 @@ dcp_status_t dcp_paged_attn_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t
  * [cu_new[i], cu_new[i + 1]) of q and out, as in dcp_cache_append, which wrote their keys and values before; the row of the token at position p sees key j iff j <= p
  * and, with window > 0, p - j < window or j < sink.  Lengths stay on the device; the call may be captured.  Everything else as in
  * dcp_paged_attn_fwd; rows whose position is negative, that no place has or that are not below n_tokens are not written.
+ * Rows, a token and query head each, are taken 16 at a time where they are few, n_tokens * hq / hkv at most 24 * n or n_tokens * hq at most 1 024, else 128 at a time: all
+ * places of a call alike, and n counts padding.  With io_dtype DCP_BF16 the weights that multiply the values are held to 2^-15 of themselves in the first case and are rounded to bf16, by
+ * 2^-8 at most, in the second (as in dcp_block_attn_fwd; their sum is not): the rest of the batch, padding included, decides about a row's last bits and about its speed.  Behind 8 192
+ * tokens, 32/8 heads of 128: a piece of 512 with 63 single tokens beside it takes 413 us, the two in calls of their own 357; the piece alone 120, padded to 128 places 245.
+ * A row is a sum in fp32 that is divided by its weights' sum at the end, weights up to 2^8: it becomes infinite where the sum passes fp32's largest number on the way.
  *   args     n places; q, out [n_tokens, hq, d], lse float [hq, n_tokens]
  *   cu_new   int32 [n + 1], device, ascending
  *   workspace  device, >= dcp_paged_attn_chunk_workspace_bytes, 256-byte aligned, as there.  The size grows with n and with n_tokens: one that was taken for
  *              the largest batch does for smaller ones.  Three launches, or two.
  * DCP_ERR_UNSUPPORTED: another dtype; n_tokens above 2^25; n_tokens * hq of 2^31 - 128 or more; hkv times (ceil(n_tokens * hq / hkv / r) + n) times
- * ceil(max_pages * page_size / 32) of 2^31 or more, with r = 16 where n_tokens * hq / hkv is at most 24 * n or n_tokens * hq at most 1 024, else 128. */
+ * ceil(max_pages * page_size / 32) of 2^31 or more, with r = 16 or 128, the rows that are taken at a time. */
 size_t dcp_paged_attn_chunk_workspace_bytes(const dcp_cache_t* cache, int32_t n, int64_t n_tokens, int32_t hq);
 dcp_status_t dcp_paged_attn_chunk_fwd(const dcp_cache_t* cache, const dcp_paged_attn_t* args, const int32_t* cu_new, int64_t n_tokens, void* workspace,
                                       size_t workspace_bytes, void* stream);

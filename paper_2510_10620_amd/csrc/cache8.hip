@@ -34,8 +34,9 @@ template <> struct Piece<float> {
   static __device__ __forceinline__ uint32_t finite(uint32_t word) { return (word & 0x7f800000u) == 0x7f800000u ? 0u : word; }
 };
 
-// A wave takes a block of tokens of one head of K or V: the largest of the new values, the scale, the codes.  Bound by HBM where there are many tokens (49 714, 8 KV heads of 128,
-// blocks of 64: 60.5 us, 5.0 TB/s read and written); few are bound by the trips to memory: cu_new, seqs, seq_len, page_table, the tokens and the block's scale.
+// A wave takes a block of tokens of one head of K or V: the largest of the new values, the scale, the codes.  Bound by HBM where there are many tokens in blocks of 32 or 64 (49 714, 8 KV heads of 128,
+// blocks of 64: 61 us, 5.0 TB/s read and written); with shorter blocks by the waves' trips to memory, as most of a wave's registers are empty, and longer ones are read twice.  Blocks of 2, 4, 5, 8, 16,
+// 32, 64, 128 and 256: bf16 292, 163, 148, 104, 73, 64, 61, 69, 83 us; fp32, of which 32 rows are held, 394, 235, 206, 153, 121, 113, 169, 219, 261.  Few tokens are bound by the trips to memory: cu_new, seqs, seq_len, page_table, the tokens and the block's scale.
 //   rows   new tokens of the block, the first of them x (stride x_st), to the codes at `to` (stride to_st); behind `older` tokens that it has already
 template <typename IO, int D>
 __device__ __forceinline__ void append_block(const char* x, int64_t x_st, char* to, int64_t to_st, uint8_t* scale, int rows, int older) {
@@ -109,7 +110,7 @@ __device__ __forceinline__ void append_block(const char* x, int64_t x_st, char* 
 }
 
 // The same where every token has scales of its own: a row's lanes find its largest value and its scale between them, kAhead rows in flight.  49 714 tokens, 8 KV heads of 128:
-// 63.7 us, 4.8 TB/s read and written (a wave a block: 506).
+// 63 us, 4.9 TB/s read and written (a wave a block: 506); fp32 95 us, 5.4 TB/s.
 template <typename IO, int D, int TOKENS>
 __global__ __launch_bounds__(256) void append8_rows_kernel(KCache c, int32_t layer, const int32_t* __restrict__ seqs, const int32_t* __restrict__ cu, int32_t n,
                                                            const int32_t* __restrict__ status, NewTokens x) {
@@ -198,7 +199,8 @@ __global__ __launch_bounds__(256, sizeof(IO) == 4 ? 2 : 4) void append8_kernel(K
 }
 
 // A workgroup reads TOKENS tokens; a lane makes 16 bytes of k_out and of v_out at a time.  IO: 0 copies (bf16 and fp32 caches), else the bytes of a number that codes
-// become.  Bound by HBM where there are many (115 760 tokens, 8 KV heads of 128, to bf16: 119 us, 6.0 TB/s read and written).
+// become.  Bound by HBM where there are many (115 760 tokens, 8 KV heads of 128, read and written: to bf16 114 to 122 us, by where the pages lie, 5.8 to 6.3 TB/s; to fp32, one sequence, 172, 6.9;
+// out of a cache in bf16 170, 5.6, in fp32 351, 5.4).
 template <int IO, int TOKENS>
 __global__ __launch_bounds__(256) void read_kernel(KCache c, int32_t layer, const int32_t* __restrict__ seqs, const int32_t* __restrict__ cu, int32_t n,
                                                    const int32_t* __restrict__ status, ReadTokens x, int32_t log_pieces) {

@@ -106,6 +106,8 @@ static size_t moves_bytes(int32_t n_pages) { return 4 * (64 + 2 * (size_t)n_page
 // 300 tokens 12.6 and 12.8; 64 of 90 13.6 and 20.1, of 380 27.5 and 29.0; 16 of 380, 2 KV heads 15.4 and 13.4; with one more
 // round 16 of 500 18.9 and 16.7.  Where they nearly fill the chip, cutting gains little and costs the joins and a start in the middle: 200 of 150
 // tokens, 8 KV heads 33 and 42, 256 of 1 to 200 34 and 41, of 200 44 and 46, 64 of 1 to 700 36.5 and 34; with 160 items fewer 40 of 1 to 700 33 and 27.
+// In 8 bits, 8 KV heads, one of 30 6.2 and 8.6, of 300 9.6 and 10.5; 64 of 90 8.6 and 13.3, of 380 16.8 and 19.8; 16 of 380, 2 KV heads 10.6 and 10.2, of 500 11.9 and 10.3; 200 of 150 18.9 and
+// 29.3, 256 of 1 to 200 20.7 and 31, of 200 24.7 and 26.7, 64 of 1 to 700 22.0 and 22.9; 40 of 1 to 700 19.7 and 19.2.
 static constexpr int kWholeRounds = 3, kWholeRoundsFull = 8, kFullItems = kWorkers * 3 / 4;
 
 // How the query heads are taken: see PagedArgs.

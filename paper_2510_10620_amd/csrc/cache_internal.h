@@ -71,12 +71,15 @@ inline bool is_aligned(const void* p, uintptr_t n) { return (reinterpret_cast<ui
 
 // dcp_paged_attn_chunk_fwd: the rows of a place and KV head (token after token, of each the query heads that share it) are taken in tiles, the items; kWorkers
 // workgroups share all items' key tiles, KV head after KV head, evenly.  Tiles have 128 rows and 64 keys in LDS, or, where places have kFewRows between
-// them on average at most or all heads of all tokens are kFewAll at most, 16 rows and 32 keys in registers, as for one token.  Whole calls, us, with keys in LDS / in registers, 32/8 heads of
+// them on average at most or all heads of all tokens are kFewAll at most, 16 rows and 32 keys in registers, as for one token.  Whole calls in a graph, us, with keys in LDS / in registers, 32/8 heads of
 // 128, 16 sequences of 300, 2 048 and 8 192 tokens: 6 rows 20.7 / 16.0, 38.4 / 27.8, 92 / 61; 12 rows 22.0 / 17.9, 40.0 / 30.3, 93 / 68; 24 rows 25.2 / 17.9, 42.8 / 34.6, 100 / 87; 39 rows
 // 28.9 / 23.3, 45.0 / 43.8, 103 / 143; 80 rows 36.7 / 29.6, 50.6 / 63.7, 116 / 240; 16/4 heads of 64, 39 rows 17.4 / 14.6, 29.8 / 23.4, 48 / 67.  By all heads of all tokens, sequences of 300, 4 096 and
 // 32 768 tokens: 32/8 of 128, one, 1 088 21.4 / 17.7, 40.0 / 30.0, 91 / 93; two, 800 18.1 / 14.3, 37.2 / 28.8, 83 / 91; four, 1 056 18.1 / 14.3, 36.7 / 30.2, 106 / 129; 2 528 21.9 / 19.7, 42.9 / 39.3,
 // 134 / 220; 16/1 of 128, one, 848 20.1 / 16.1, 55.6 / 28.0, 78 / 71 (few items of many parts, which are long to join); 128 18.3 / 11.8, 49.7 / 25.7, 242 / 46; 64/2 of 64, two, 768 16.6 / 12.0, 50.1 / 19.6,
 // 73 / 64; 1 216 17.0 / 12.2, 47.0 / 21.1, 62 / 75.  Items of 32 rows in registers were between the two.
+// These are batches of places that are alike.  The rule knows no others: places that are padding count, and all go the same way.  32/8 heads of 128 behind 8 192 tokens, a piece of 300 new
+// tokens alone 84, padded to 64 places, where it goes by registers, 152; of 512 120, padded to 128 245; 63 single tokens alone 237, with a piece of 300 beside them 358 (registers, 37 more
+// than the two alone), of 512 413 (LDS, 56 more), of 2 048 691 (64 more).
 static constexpr int kChunkRows = 128, kChunkKeys = 64, kFewRows = 24, kFewItem = 16, kFewAll = 1024, kOwnItems = 256;
 struct ChunkArgs {
   const char* q;

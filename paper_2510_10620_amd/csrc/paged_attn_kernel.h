@@ -385,6 +385,8 @@ __global__ __launch_bounds__(THREADS) void paged_join_kernel(KCache c, PagedArgs
 // 30 000 tokens 27.9 / 32.8 / 62.3, 2 of 131 067 93.6 / 95.3 / 110, 3 of 30 000 44.7 / 45.3 / -, 5 63.3 / 63.1 / -, 8 of 20 000 66.0 / 65.3 / 69.1, 16 of
 // 2 048 26.2 / 24.9 / 26.3, 31 of 4 096 55.8 / 54.3 / 55.5, 70 of 2 048 65.9 / 62.5 / 61.7; D 64, 1 of 8 000 14.7 / 13.5 / -, of 30 000 20.8 / 21.1 / 37.3, 3 of
 // 30 000 28.9 / 27.2 / -, 16 of 2 048 18.1 / 16.7 / 16.8, 31 of 4 096 33.9 / 32.8 / 32.5; fp32 with D 64, 8 of 1 to 4 096 18.2 / 15.8 / 18.9.
+// In 8 bits with 16/4 heads the same: D 128, 1 entry of 30 000 tokens 21.8 / 26.6 / 55.8, 2 of 131 067 58.0 / 59.6 / 73.1, 3 of 30 000 31.3 / 31.5 / 41.8, 5 39.0 / 39.0 / 45.2, 8 of 20 000 39.6 / 39.3 / 43.2,
+// 16 of 2 048 17.5 / 16.2 / 17.6, 31 of 4 096 34.8 / 33.3 / 34.5, 70 of 2 048 43.2 / 39.8 / 39.1; D 64, 1 of 30 000 17.4 / 17.4 / 33.8, 3 20.1 / 20.1 / 25.8, 31 of 4 096 22.2 / 22.1 / 21.8.
 static constexpr unsigned kWideJoins = 3, kMiddleJoins = 31;
 
 template <typename TT, int COLS, bool ONCE>

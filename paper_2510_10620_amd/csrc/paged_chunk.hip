@@ -216,8 +216,10 @@ template <int D> struct Staged {
 
 // O = sum_j exp(s_j - m) v_j / l, LSE = m + ln l as for one token, in one pass over a row tile's key tiles of 64, which the four waves of 32 rows share in LDS as bf16
 // numbers: codes and scales become them without a rounding on the way.  Scores are computed transposed, S^T = K Q^T, so that a lane owns a row, and P^T is the B operand
-// of O^T += V^T P^T as it stands (see mfma_common.h).  bf16: weights are rounded to bf16, their sum is not.  fp32: queries and weights go in as three bf16 parts.
-// Bound by issue: 1 799 tokens behind 30 720, 32/8 heads of 128, 1 130 us, 825 TFLOP/s; 9.8 vector instructions a matrix instruction (softmax; the conversion of codes, a tenth; addresses),
+// of O^T += V^T P^T as it stands (see mfma_common.h).  bf16: weights are rounded to bf16, their sum is not, as in dcp_block_attn_fwd: beside the
+// rounding of the output the error against 64 bits grows from 1.66e-3 to 2.3e-3 of the norm.  In two parts, as the walk with keys in registers has them, it did not, but the case below took
+// 1 453 us instead of 1 122, seven prompts of up to 1 500 tokens with a window of 1 024, 16/4 heads of 64, 99 instead of 86.  fp32: queries and weights go in as three bf16 parts (3 160 us).
+// Bound by issue: 1 799 tokens behind 30 720, 32/8 heads of 128, 1 126 us in a graph, 829 TFLOP/s; 9.8 vector instructions a matrix instruction (softmax; the conversion of codes, a tenth; addresses),
 // matrix pipes busy 36 % of the time, vector units 49 %.  Two workgroups on a CU (fp32: one); with heads of 64 three gained nothing.
 template <typename IO, int D>
 __global__ __launch_bounds__(kThreads, sizeof(IO) == 4 ? 1 : 2) void chunk_kernel(KCache c, ChunkArgs a, ChunkPlan plan) {

@@ -10,7 +10,7 @@ namespace dcp {
 namespace {
 
 // The plan, as a workgroup of the walk makes it for itself where there are at most kOwnItems items (and so places): a launch less than with chunk_plan_kernel, whose records take
-// as many trips to memory to read as the places themselves (whole calls, us: the case below 38.7 -> 35.4, 4 sequences of up to 900 tokens, fp32, D 64 15.8 -> 12.3; with keys in LDS,
+// as many trips to memory to read as the places themselves (whole calls in a graph, us: the case below 38.7 -> 35.4, 4 sequences of up to 900 tokens, fp32, D 64 15.8 -> 12.3; with keys in LDS,
 // where the walk became 18 us longer on 1 130, the launch stays).
 struct OwnPlan {
   int4 place[kOwnItems];   // sequence, first token, its position, rows
@@ -111,7 +111,7 @@ struct ChunkShare {
 
 // The walk of paged_attn_kernel over the items of the plan: 16 rows in place of the query heads of one token, a column of the matrix tile each with keys of its own; the
 // four waves take an item's key tiles in turn.  Every wave multiplies, where the kernel with keys in LDS would leave three of four without rows.  Bound by the
-// trips to memory: 16 sequences of 512 to 8 192 tokens, up to five new ones each, 32/8 heads of 128, 35.4 us of which the join is 5, 92 MB of codes (49.5 with keys in LDS; 46.4, when it was 38.3, with loads past the caches: items of a place read the same keys).
+// trips to memory: 16 sequences of 512 to 8 192 tokens, up to five new ones each, 32/8 heads of 128, 35.4 us in a graph (37.8 launched among others) of which the join is 5, 92 MB of codes (49.5 with keys in LDS; 46.4, when it was 38.3, with loads past the caches: items of a place read the same keys).
 template <typename TT, bool GROUPED>
 __global__ __launch_bounds__(kPagedThreads, 2) void chunk_few_kernel(KCache c, ChunkArgs a, ChunkPlan plan) {
   typedef typename TT::Out IO;
